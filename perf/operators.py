@@ -227,9 +227,9 @@ def _own_keep(s):
 
 
 def _scale_of(amax):
-    """The smallest power of two s with amax / s <= 448, at least 2^-100."""
+    """The smallest power of two s with amax / s <= 448, at least 2^-64."""
     m, e = torch.frexp(amax)                                     # amax = m 2^e, 0.5 <= m < 1; 448 = 0.875 2^9
-    return torch.ldexp(torch.ones_like(amax), torch.where(amax > 0, e - 9 + (m > 0.875).int(), -100).clamp(min=-100))
+    return torch.ldexp(torch.ones_like(amax), torch.where(amax > 0, e - 9 + (m > 0.875).int(), -64).clamp(min=-64))
 
 
 def _codes(x):
@@ -418,10 +418,10 @@ def _grid64(x):
 
 
 def _scale64(amax):
-    """2^e with the smallest e >= -100 that brings amax to 448 or less."""
-    e = torch.ceil(torch.log2(amax.clamp(min=1e-60) / 448.0)).clamp(min=-100)
+    """2^e with the smallest e >= -64 that brings amax to 448 or less."""
+    e = torch.ceil(torch.log2(amax.clamp(min=1e-60) / 448.0)).clamp(min=-64)
     e = torch.where(amax > 448.0 * torch.exp2(e), e + 1, e)
-    e = torch.where((e > -100) & (amax <= 448.0 * torch.exp2(e - 1)), e - 1, e)
+    e = torch.where((e > -64) & (amax <= 448.0 * torch.exp2(e - 1)), e - 1, e)
     return torch.exp2(e)
 
 

@@ -68,13 +68,22 @@ typedef enum { BS_UCB = 0, BS_EXP3 = 1, BS_UCB_REWARD = 2 } bs_alg;
 #define BS_DEV_DRAFT_MISSING 16    /* bs_softmax_verify_drafted: a draft row below gamma_b was not produced by
                                       bs_draft_sample on this workspace; every draft of the sequence was rejected */
 #define BS_DEV_BAD_TREE      32    /* bs_tree_verify_greedy: a node's parent is not an earlier node; the node counts as
-                                      hanging under the prompt and never passes */
+                                      hanging under the prompt and never passes.  bs_cache_attention: the same reading;
+                                      bs_cache_keep_path: a path whose nodes do not ascend, nothing was moved */
+#define BS_DEV_BAD_LENGTH    64    /* bs_cache_*: a length that is negative, longer than the sequence's blocks or than its
+                                      row of the block table; the sequence got no new tokens / was left out */
+#define BS_DEV_NO_BLOCKS     128   /* bs_cache_plan: not enough free blocks; the sequence got no new tokens */
+#define BS_DEV_NO_ROOM       256   /* bs_cache_plan: its tokens do not fit slot_map; the sequence got no new tokens */
+#define BS_DEV_BAD_BLOCK     512   /* bs_cache_attention / bs_cache_keep_path: a block id outside [0, n_blocks) */
+#define BS_DEV_TIMEOUT       1024  /* bs_cache_attention: a bounded wait gave up; every output of the call is undefined and
+                                      its workspace has to be cleared with bs_workspace_init */
 
 /* Limits of this implementation. */
 #define BS_MAX_GAMMA   31      /* Gmax <= 31 (one warp scans the accept flags) */
 #define BS_MAX_ARMS    32      /* K <= 32 (one lane per arm) */
 #define BS_MAX_BATCH   4096    /* B <= 4096 */
 #define BS_MAX_VOCAB   (1 << 20) /* V <= 1048576 */
+#define BS_MAX_SEQ_BLOCKS (1 << 18) /* blocks of one sequence in the key / value cache */
 
 const char* bs_status_string(bs_status s);
 
@@ -329,6 +338,110 @@ bs_status bs_lmhead_verify(const void* H_t, const void* W_t, int d_t, const void
                            float* logits_t_out, float* logits_d_out,
                            int32_t* accept_len, float* p_tok, float* q_tok,
                            void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---- the key / value cache of a round ------------------------------------------------------
+ *
+ * The target model evaluates the pending token and all drafts of a sequence in one pass (Algorithm 6,
+ * second line), which in a transformer is an attention of 1 + gamma_b new tokens (a chain) or 1 + n_b (a tree;
+ * row 0 is the root, row n node n) over the tokens so far.  These four calls keep those tokens' keys and values:
+ *
+ *   bs_cache_plan       block tables, slots and positions of the round's new tokens
+ *   bs_cache_append     their keys and values into the cache (each layer)
+ *   bs_cache_attention  attention of the new tokens over the cache (each layer)
+ *   bs_cache_keep_path  trees only, after the verification: the accepted path to the front (each layer)
+ *
+ * Rejected tokens need no call: the next bs_cache_plan is told how many of them stay (`kept`, the out_len of the
+ * verification) and their slots are written again.
+ *
+ * The cache is held in 8 bits: codes [n_blocks, Hkv, block_tokens, d] e4m3 and scales [n_blocks, Hkv] fp32, for the
+ * keys and for the values; value = code * scale.  A block holds block_tokens (16, 32, 64 or 128) consecutive
+ * tokens of one sequence.  d is 64 or 128.  block_table [B, max_blocks] int32 lists the blocks of every sequence in
+ * order; entries behind those it holds are never read.  New tokens are packed: those of sequence b are rows
+ * cu_new[b] .. cu_new[b + 1] - 1 of the query, key and value arrays.  block table, lengths and slots are the same
+ * for all layers.  `status` [B] int32 or NULL: bs_cache_plan writes its BS_DEV_* bits, the other calls add theirs. */
+
+/* Block tables and slot maps from lengths that are on the device.  One launch.
+ *
+ *  seq_len     [B] in / out: tokens of every sequence in the cache.  kept[b] tokens of the round before are added first
+ *  kept        [B] or NULL (= 0)
+ *  n_new       [B]; n_new[b] + extra new tokens come (gamma and extra = 1 for a round, prompt lengths and 0 for prompts)
+ *  active      [B] uint8 or NULL (= all); an inactive sequence keeps nothing, gets nothing and returns what it does not need
+ *  block_table [B, max_blocks] in / out, n_held [B] in / out: the blocks every sequence holds
+ *  free_blocks [n_blocks] in / out, n_free [1] in / out: the stack of free blocks, its top at n_free - 1
+ *  kv_len      [B] out: seq_len + new tokens, what bs_cache_attention reads
+ *  cu_new      [B + 1] out: prefix sums of the new tokens
+ *  slot_map    [T] out: block * block_tokens + offset of every new token, -1 behind the last one
+ *  positions   [T] out or NULL: position of every new token in its sequence, -1 behind the last one
+ *
+ * Afterwards sequence b holds ceil((seq_len + new) / block_tokens) blocks: surplus blocks are returned (a sequence
+ * with seq_len = 0 and no new tokens returns all), missing ones taken, in the order of the sequences.  If the stack runs
+ * out (or slot_map is full) at some sequence, it and every later one that needs a block (a slot) gets no new tokens
+ * and keeps what it held: BS_DEV_NO_BLOCKS (BS_DEV_NO_ROOM).  A sequence whose lengths make no sense
+ * (BS_DEV_BAD_LENGTH) is left as it is, with kv_len 0.  Freed entries of block_table are set to -1.  A plan whose
+ * tokens are all given back restores the stack. */
+bs_status bs_cache_plan(int32_t* seq_len, const int32_t* kept, const int32_t* n_new, int extra, const uint8_t* active,
+                        int B, int block_tokens, int32_t* block_table, int max_blocks, int32_t* n_held,
+                        int32_t* free_blocks, int n_blocks, int32_t* n_free, int32_t* kv_len, int32_t* cu_new,
+                        int32_t* slot_map, int32_t* positions, int T, int32_t* status, void* stream);
+
+/* Writes the new tokens' keys and values into their slots, quantised.
+ *
+ *  k, v      [T, Hkv, d] dtype, d contiguous; strides of a token and of a head in elements, multiples of 16 bytes,
+ *            16-byte aligned (views of a fused projection are fine)
+ *  slot_map  [T]: tokens with slot -1, or outside the cache, are skipped
+ *
+ * The scale of a (block, head) is the smallest power of two >= 2^-64 that brings the largest finite magnitude among
+ * the new tokens to 448 or less, and no smaller than the block's present scale if the first new token is not the
+ * first of its block; the codes of older tokens then follow (rounded once more only where they become subnormal).
+ * Codes are rounded to nearest even, infinities become +-448 scales, NaN stays NaN.  The new tokens of a block must be
+ * consecutive rows with consecutive slots, as bs_cache_plan gives them; two separate runs in one block, in
+ * one call, are not supported. */
+bs_status bs_cache_append(const void* k, const void* v, bs_dtype dtype, long long k_stride_t, long long k_stride_h,
+                          long long v_stride_t, long long v_stride_h, const int32_t* slot_map, int T, int Hkv, int d,
+                          void* k_cache, float* k_scale, void* v_cache, float* v_scale, int n_blocks, int block_tokens,
+                          void* stream);
+
+/* Bytes of scratch bs_cache_attention needs on the current device for these heads (any batch and length);
+ * 0 for unsupported ones.  Clear it once with bs_workspace_init. */
+size_t bs_cache_workspace_bytes(int Hq, int Hkv, int d);
+
+/* Attention of the new tokens over the cache: out_i = sum_j softmax_j(softmax_scale * q_i . k_j) v_j.
+ *
+ *  q, out       [T, Hq, d] bf16, d contiguous; strides of a token and of a head in elements, multiples of 8, 16-byte
+ *               aligned.  Query head i reads key head i / (Hq / Hkv); Hq / Hkv <= 64
+ *  cu_new, kv_len, block_table  from bs_cache_plan; kv_len includes the new tokens
+ *  node_parent  NULL: a chain, new token i of sequence b sees positions <= kv_len[b] - n_new_b + i.
+ *               [B, Nmax] (Nmax <= 31): trees as in bs_tree_verify_greedy, new token n sees the tokens before the tree,
+ *               its ancestors and itself
+ *  max_new      the largest number of new tokens of a sequence, as far as known on the host: chooses the tile, any
+ *               value >= 1 gives the same result up to rounding
+ *  workspace    bs_cache_workspace_bytes bytes, 256-byte aligned, cleared once; calls that may overlap need one each
+ *
+ * Keys and values enter the tensor cores as the e4m3 codes they are; a bf16 query is split into two e4m3 numbers, which
+ * holds it exactly down to 2^-10 of its row's largest element; probabilities are split the same way, relative error at
+ * most 2^-8 where they are within 2^-10 of the largest of their 128-token tile and absolute error 2^-18 of that
+ * below.  Products accumulate in fp32, tiles are joined in fp32.  Scales of V within a tile should lie within 2^126 of one another.
+ * A token that sees nothing (kv_len < its position) gets zeros.  Rows of out behind cu_new[B] are left as they are, and so
+ * are the rows of a sequence with BS_DEV_BAD_LENGTH (lengths outside the block table, cu_new not ascending or
+ * above T; trees: more than Nmax + 1 new tokens).  BS_DEV_BAD_BLOCK: the rows of that sequence are undefined.
+ * Results do not depend on the order in which CTAs run. */
+bs_status bs_cache_attention(const void* q, long long q_stride_t, long long q_stride_h, const int32_t* cu_new,
+                             const int32_t* kv_len, const int32_t* block_table, int max_blocks,
+                             const int32_t* node_parent, int Nmax, const void* k_cache, const float* k_scale,
+                             const void* v_cache, const float* v_scale, int n_blocks, int block_tokens, int B, int T, int Hq,
+                             int Hkv, int d, int max_new, float softmax_scale, void* out, long long out_stride_t,
+                             long long out_stride_h, int32_t* status, void* workspace, size_t workspace_bytes, void* stream);
+
+/* After bs_tree_verify_greedy: moves the accepted path to the front of its tree, token seq_len + out_nodes[b, j] to
+ * position seq_len + 1 + j for j < accept_len[b] (the root is in place), keys and values of one layer.
+ *
+ *  out_nodes [B, Nmax] and accept_len [B] from bs_tree_verify_greedy; seq_len [B] from bs_cache_plan of the round (tokens
+ *  before the tree).
+ * A destination block's scale becomes the largest of its own and those of the blocks its tokens come from.  A sequence
+ * with BS_DEV_BAD_LENGTH, BS_DEV_BAD_TREE (nodes that do not ascend) or BS_DEV_BAD_BLOCK is left as it is. */
+bs_status bs_cache_keep_path(const int32_t* out_nodes, const int32_t* accept_len, const int32_t* seq_len, int B, int Nmax,
+                             const int32_t* block_table, int max_blocks, int Hkv, int d, void* k_cache, float* k_scale,
+                             void* v_cache, float* v_scale, int n_blocks, int block_tokens, int32_t* status, void* stream);
 
 /* ---- arm selection (Algorithm 3, select and history lines) ---------------------------- */
 

@@ -28,9 +28,10 @@ BS_F32, BS_BF16 = 0, 1
 BS_UCB, BS_EXP3, BS_UCB_REWARD = 0, 1, 2
 BS_DEV_BAD_GAMMA, BS_DEV_BAD_TOKEN, BS_DEV_NONFINITE, BS_DEV_RESIDUAL_FALLBACK, BS_DEV_DRAFT_MISSING = 1, 2, 4, 8, 16
 BS_DEV_BAD_TREE = 32
-BS_MAX_GAMMA, BS_MAX_ARMS, BS_MAX_BATCH = 31, 32, 4096
+BS_DEV_BAD_LENGTH, BS_DEV_NO_BLOCKS, BS_DEV_NO_ROOM, BS_DEV_BAD_BLOCK, BS_DEV_TIMEOUT = 64, 128, 256, 512, 1024
+BS_MAX_GAMMA, BS_MAX_ARMS, BS_MAX_BATCH, BS_MAX_SEQ_BLOCKS = 31, 32, 4096, 1 << 18
 
-_vp, _i, _f, _d, _sz = C.c_void_p, C.c_int, C.c_float, C.c_double, C.c_size_t
+_vp, _i, _f, _d, _sz, _ll = C.c_void_p, C.c_int, C.c_float, C.c_double, C.c_size_t, C.c_longlong
 
 # name -> (restype, argtypes); must list every symbol the header declares
 SIGNATURES = {
@@ -52,6 +53,12 @@ SIGNATURES = {
     "bs_lmhead_workspace_bytes": (_sz, [_i, _i, _i]),
     "bs_lmhead_verify": (_i, [_vp, _vp, _i, _vp, _vp, _i, _vp, _vp, _vp, _f, _i, _i, _i, _vp, _vp, _vp, _vp, _vp,
                               _vp, _sz, _vp]),
+    "bs_cache_plan": (_i, [_vp, _vp, _vp, _i, _vp, _i, _i, _vp, _i, _vp, _vp, _i, _vp, _vp, _vp, _vp, _vp, _i, _vp, _vp]),
+    "bs_cache_append": (_i, [_vp, _vp, _i, _ll, _ll, _ll, _ll, _vp, _i, _i, _i, _vp, _vp, _vp, _vp, _i, _i, _vp]),
+    "bs_cache_workspace_bytes": (_sz, [_i, _i, _i]),
+    "bs_cache_attention": (_i, [_vp, _ll, _ll, _vp, _vp, _vp, _i, _vp, _i, _vp, _vp, _vp, _vp, _i, _i, _i, _i, _i, _i, _i,
+                                _i, _f, _vp, _ll, _ll, _vp, _vp, _sz, _vp]),
+    "bs_cache_keep_path": (_i, [_vp, _vp, _vp, _i, _i, _vp, _i, _i, _i, _vp, _vp, _vp, _vp, _i, _i, _vp, _vp]),
     "bs_bandit_state_bytes": (_sz, [_i, _i, _i]),
     "bs_bandit_init": (_i, [_vp, _sz, _i, _i, _i, _vp, _d, _vp]),
     "bs_bandit_select": (_i, [_vp, _sz, _i, _i, _i, _vp, _vp, _vp, _vp, _vp, _vp]),
@@ -306,6 +313,113 @@ def bs_lmhead_verify(H_t, W_t, H_d, W_d, draft_tokens, gamma, u_accept, temperat
                                  _ptr(gamma), _ptr(u_accept), float(temperature), B, Gmax, V,
                                  _ptr(logits_t_out), _ptr(logits_d_out), _ptr(accept_len), _ptr(p_tok), _ptr(q_tok),
                                  _ptr(workspace), workspace.numel(), _stream(stream)), "bs_lmhead_verify")
+
+
+# ---- the key / value cache of a round ----------------------------------------------------------
+
+def _i32(t, *shape) -> Optional[int]:
+    """Pointer of an int32 tensor of this shape (None stays NULL)."""
+    if t is None:
+        return None
+    assert t.dtype == torch.int32 and tuple(t.shape) == shape, f"int32 {shape} expected, got {t.dtype} {tuple(t.shape)}"
+    return _ptr(t)
+
+
+class _on:
+    """Makes the device of `t` the current one for a call."""
+
+    def __init__(self, t: torch.Tensor):
+        self.guard = torch.cuda.device(t.device) if t.device.index != torch.cuda.current_device() else None
+
+    def __enter__(self):
+        if self.guard is not None:
+            self.guard.__enter__()
+
+    def __exit__(self, *a):
+        if self.guard is not None:
+            self.guard.__exit__(*a)
+
+
+def _cache_args(k_cache, k_scale, v_cache, v_scale):
+    n_blocks, Hkv, bt, d = k_cache.shape
+    assert k_cache.element_size() == 1 and v_cache.element_size() == 1 and v_cache.shape == k_cache.shape
+    assert k_scale.dtype == v_scale.dtype == torch.float32
+    assert tuple(k_scale.shape) == tuple(v_scale.shape) == (n_blocks, Hkv)
+    return n_blocks, Hkv, bt, d
+
+
+def new_cache(n_blocks: int, Hkv: int, block_tokens: int, d: int, device="cuda"):
+    """(codes, scales) of keys or values: float8_e4m3fn [n_blocks, Hkv, block_tokens, d], float32 [n_blocks, Hkv]."""
+    return (torch.zeros(n_blocks, Hkv, block_tokens, d, dtype=torch.float8_e4m3fn, device=device),
+            torch.ones(n_blocks, Hkv, dtype=torch.float32, device=device))
+
+
+def bs_cache_plan(seq_len, kept, n_new, extra: int, active, block_tokens: int, block_table, n_held, free_blocks, n_free,
+                  kv_len, cu_new, slot_map, positions, status, stream=None) -> None:
+    """Block tables, slots and positions of a round's new tokens; seq_len, block_table, n_held, free_blocks and n_free
+    are updated in place."""
+    B, W = block_table.shape
+    n_blocks, T = free_blocks.numel(), slot_map.numel()
+    assert active is None or (active.dtype == torch.uint8 and active.numel() == B)
+    with _on(seq_len):
+        _check(_lib.bs_cache_plan(_i32(seq_len, B), _i32(kept, B), _i32(n_new, B), int(extra), _ptr(active), B,
+                                  int(block_tokens), _i32(block_table, B, W), W, _i32(n_held, B), _i32(free_blocks, n_blocks),
+                                  n_blocks, _i32(n_free, 1), _i32(kv_len, B), _i32(cu_new, B + 1), _i32(slot_map, T),
+                                  _i32(positions, T), T, _i32(status, B), _stream(stream)), "bs_cache_plan")
+
+
+def bs_cache_append(k, v, slot_map, k_cache, k_scale, v_cache, v_scale, stream=None) -> None:
+    """k, v [T, Hkv, d] (bf16 or fp32, last dimension contiguous) into their slots."""
+    n_blocks, Hkv, bt, d = _cache_args(k_cache, k_scale, v_cache, v_scale)
+    T = slot_map.numel()
+    assert tuple(k.shape) == tuple(v.shape) == (T, Hkv, d) and k.dtype == v.dtype
+    assert k.stride(2) == 1 and v.stride(2) == 1, "the last dimension must be contiguous"
+    with _on(k_cache):
+        _check(_lib.bs_cache_append(k.data_ptr(), v.data_ptr(), _dtype_code(k), k.stride(0), k.stride(1), v.stride(0),
+                                    v.stride(1), _i32(slot_map, T), T, Hkv, d, _ptr(k_cache), _ptr(k_scale), _ptr(v_cache),
+                                    _ptr(v_scale), n_blocks, bt, _stream(stream)), "bs_cache_append")
+
+
+def new_cache_workspace(Hq: int, Hkv: int, d: int, device="cuda") -> torch.Tensor:
+    """Scratch of bs_cache_attention, cleared."""
+    with torch.cuda.device(device):
+        n = int(_lib.bs_cache_workspace_bytes(Hq, Hkv, d))
+        if n == 0:
+            raise BanditSpecError(BS_ERR_UNSUPPORTED, "bs_cache_workspace_bytes")
+        ws = torch.empty(n, dtype=torch.uint8, device=device)
+        bs_workspace_init(ws)
+    return ws
+
+
+def bs_cache_attention(q, cu_new, kv_len, block_table, node_parent, k_cache, k_scale, v_cache, v_scale, max_new: int,
+                       softmax_scale: float, out, status, workspace, stream=None) -> None:
+    """q, out [T, Hq, d] bf16 (last dimension contiguous): attention of the new tokens over the cache.  node_parent
+    None: chains; [B, Nmax] int32: trees of drafts."""
+    n_blocks, Hkv, bt, d = _cache_args(k_cache, k_scale, v_cache, v_scale)
+    B, W = block_table.shape
+    T, Hq = q.shape[0], q.shape[1]
+    assert q.dtype == out.dtype == torch.bfloat16 and q.shape[2] == d and out.shape == q.shape
+    assert q.stride(2) == 1 and out.stride(2) == 1, "the last dimension must be contiguous"
+    Nmax = 0 if node_parent is None else node_parent.shape[1]
+    with _on(k_cache):
+        _check(_lib.bs_cache_attention(q.data_ptr(), q.stride(0), q.stride(1), _i32(cu_new, B + 1), _i32(kv_len, B),
+                                       _i32(block_table, B, W), W, _i32(node_parent, B, Nmax), Nmax, _ptr(k_cache),
+                                       _ptr(k_scale), _ptr(v_cache), _ptr(v_scale), n_blocks, bt, B, T, Hq, Hkv, d,
+                                       int(max_new), float(softmax_scale), out.data_ptr(), out.stride(0), out.stride(1),
+                                       _i32(status, B), _ptr(workspace), workspace.numel(), _stream(stream)),
+               "bs_cache_attention")
+
+
+def bs_cache_keep_path(out_nodes, accept_len, seq_len, block_table, k_cache, k_scale, v_cache, v_scale, status,
+                       stream=None) -> None:
+    """The accepted path of bs_tree_verify_greedy to the front of its tree."""
+    n_blocks, Hkv, bt, d = _cache_args(k_cache, k_scale, v_cache, v_scale)
+    B, W = block_table.shape
+    Nmax = out_nodes.shape[1]
+    with _on(k_cache):
+        _check(_lib.bs_cache_keep_path(_i32(out_nodes, B, Nmax), _i32(accept_len, B), _i32(seq_len, B), B, Nmax,
+                                       _i32(block_table, B, W), W, Hkv, d, _ptr(k_cache), _ptr(k_scale), _ptr(v_cache),
+                                       _ptr(v_scale), n_blocks, bt, _i32(status, B), _stream(stream)), "bs_cache_keep_path")
 
 
 # ---- bandits ---------------------------------------------------------------------------

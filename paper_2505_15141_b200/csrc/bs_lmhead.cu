@@ -32,8 +32,7 @@
 #include <atomic>
 #include "bs_verify_common.cuh"
 #include "bs_pipeline.cuh"
-
-#include <cuda.h>          // CUtensorMap and its enums; the encoder is looked up at run time
+#include "bs_tensor.cuh"
 
 namespace bs {
 
@@ -87,9 +86,6 @@ __device__ __forceinline__ void tma_store_wait_read() {        // the stores iss
 __device__ __forceinline__ void tma_store_wait_all() {         // ... and have been written
     asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
 }
-__device__ __forceinline__ void sts128(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
-    asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
-}
 __device__ __forceinline__ uint64_t policy_evict_first() {
     uint64_t p;
     asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(p));
@@ -104,11 +100,6 @@ __device__ __forceinline__ uint64_t policy_evict_last() {
     uint64_t p;
     asm volatile("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(p));
     return p;
-}
-__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tc_commit(uint32_t bar) {       // arrives on `bar` when all earlier MMAs are done
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
 // D[tmem] (+)= A[smem] * B[smem], one 128 x N x 16 step
 __device__ __forceinline__ void tc_mma_bf16(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
@@ -209,9 +200,7 @@ lmhead_gemm_kernel(const __grid_constant__ CUtensorMap tm_h0, const __grid_const
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 1) {                                          // tensor memory: whole warp allocates
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
-                     ::"r"(smem_u32(&s_tmem_base)), "r"(kLmTmemCols) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        tc_alloc(smem_u32(&s_tmem_base), kLmTmemCols);
     }
     tc_fence_before();
     __syncthreads();
@@ -411,7 +400,7 @@ lmhead_gemm_kernel(const __grid_constant__ CUtensorMap tm_h0, const __grid_const
     if (warp == 1) {
         tc_fence_after();
         __syncwarp();
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(kLmTmemCols) : "memory");
+        tc_free(tmem_base, kLmTmemCols);
     }
 }
 
@@ -478,24 +467,6 @@ __global__ void __launch_bounds__(kThreads) lmhead_finalize_kernel(const VerifyP
 }
 
 // ---- host side ------------------------------------------------------------------------------
-
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-static EncodeTiledFn encode_tiled_fn() {
-    static EncodeTiledFn fn = nullptr;
-    if (!fn) {
-        void* ptr = nullptr;
-        cudaDriverEntryPointQueryResult q;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &ptr, cudaEnableDefault, &q) == cudaSuccess &&
-            q == cudaDriverEntryPointSuccess)
-            fn = reinterpret_cast<EncodeTiledFn>(ptr);
-        else
-            cudaGetLastError();
-    }
-    return fn;
-}
 
 // bf16 matrix [rows, cols] with cols contiguous; boxes of box_rows x 64 columns, 128-byte swizzle,
 // elements outside the matrix read as zero.

@@ -317,35 +317,37 @@ def bs_lmhead_verify(H_t, W_t, H_d, W_d, draft_tokens, gamma, u_accept, temperat
 
 # ---- the key / value cache of a round ----------------------------------------------------------
 
-def _i32(t, *shape) -> Optional[int]:
-    """Pointer of an int32 tensor of this shape (None stays NULL)."""
+# These calls are made once or more per layer: their checks are kept to a few attribute look-ups each.
+
+_raw_stream = torch._C._cuda_getCurrentRawStream
+
+
+def _i32(t, n: int) -> Optional[int]:
+    """Pointer of a contiguous int32 tensor of n elements (None stays NULL)."""
     if t is None:
         return None
-    assert t.dtype == torch.int32 and tuple(t.shape) == shape, f"int32 {shape} expected, got {t.dtype} {tuple(t.shape)}"
-    return _ptr(t)
+    assert t.dtype is torch.int32 and t.numel() == n and t.is_contiguous(), f"contiguous int32 of {n} elements expected, got {t.dtype} {tuple(t.shape)}"
+    return t.data_ptr()
 
 
-class _on:
-    """Makes the device of `t` the current one for a call."""
-
-    def __init__(self, t: torch.Tensor):
-        self.guard = torch.cuda.device(t.device) if t.device.index != torch.cuda.current_device() else None
-
-    def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
-
-    def __exit__(self, *a):
-        if self.guard is not None:
-            self.guard.__exit__(*a)
+def _call(fn, where: str, device: torch.device, stream, *args) -> None:
+    """fn(*args, stream) with the tensors' device current, on `stream` or that device's current stream."""
+    index = device.index
+    if index == torch.cuda.current_device():
+        code = fn(*args, _raw_stream(index) if stream is None else stream.cuda_stream)
+    else:
+        with torch.cuda.device(device):
+            code = fn(*args, _raw_stream(index) if stream is None else stream.cuda_stream)
+    if code != BS_OK:
+        raise BanditSpecError(code, where)
 
 
 def _cache_args(k_cache, k_scale, v_cache, v_scale):
-    n_blocks, Hkv, bt, d = k_cache.shape
-    assert k_cache.element_size() == 1 and v_cache.element_size() == 1 and v_cache.shape == k_cache.shape
-    assert k_scale.dtype == v_scale.dtype == torch.float32
-    assert tuple(k_scale.shape) == tuple(v_scale.shape) == (n_blocks, Hkv)
-    return n_blocks, Hkv, bt, d
+    shape = k_cache.shape
+    assert k_cache.element_size() == 1 and v_cache.element_size() == 1 and v_cache.shape == shape
+    assert k_scale.dtype is torch.float32 and v_scale.dtype is torch.float32 and k_scale.shape == v_scale.shape == shape[:2]
+    assert k_cache.is_contiguous() and v_cache.is_contiguous() and k_scale.is_contiguous() and v_scale.is_contiguous()
+    return shape
 
 
 def new_cache(n_blocks: int, Hkv: int, block_tokens: int, d: int, device="cuda"):
@@ -360,24 +362,23 @@ def bs_cache_plan(seq_len, kept, n_new, extra: int, active, block_tokens: int, b
     are updated in place."""
     B, W = block_table.shape
     n_blocks, T = free_blocks.numel(), slot_map.numel()
-    assert active is None or (active.dtype == torch.uint8 and active.numel() == B)
-    with _on(seq_len):
-        _check(_lib.bs_cache_plan(_i32(seq_len, B), _i32(kept, B), _i32(n_new, B), int(extra), _ptr(active), B,
-                                  int(block_tokens), _i32(block_table, B, W), W, _i32(n_held, B), _i32(free_blocks, n_blocks),
-                                  n_blocks, _i32(n_free, 1), _i32(kv_len, B), _i32(cu_new, B + 1), _i32(slot_map, T),
-                                  _i32(positions, T), T, _i32(status, B), _stream(stream)), "bs_cache_plan")
+    assert active is None or (active.dtype is torch.uint8 and active.numel() == B and active.is_contiguous())
+    _call(_lib.bs_cache_plan, "bs_cache_plan", seq_len.device, stream, _i32(seq_len, B), _i32(kept, B), _i32(n_new, B), extra,
+          None if active is None else active.data_ptr(), B, block_tokens, _i32(block_table, B * W), W, _i32(n_held, B),
+          _i32(free_blocks, n_blocks), n_blocks, _i32(n_free, 1), _i32(kv_len, B), _i32(cu_new, B + 1), _i32(slot_map, T),
+          _i32(positions, T), T, _i32(status, B))
 
 
 def bs_cache_append(k, v, slot_map, k_cache, k_scale, v_cache, v_scale, stream=None) -> None:
     """k, v [T, Hkv, d] (bf16 or fp32, last dimension contiguous) into their slots."""
     n_blocks, Hkv, bt, d = _cache_args(k_cache, k_scale, v_cache, v_scale)
     T = slot_map.numel()
-    assert tuple(k.shape) == tuple(v.shape) == (T, Hkv, d) and k.dtype == v.dtype
-    assert k.stride(2) == 1 and v.stride(2) == 1, "the last dimension must be contiguous"
-    with _on(k_cache):
-        _check(_lib.bs_cache_append(k.data_ptr(), v.data_ptr(), _dtype_code(k), k.stride(0), k.stride(1), v.stride(0),
-                                    v.stride(1), _i32(slot_map, T), T, Hkv, d, _ptr(k_cache), _ptr(k_scale), _ptr(v_cache),
-                                    _ptr(v_scale), n_blocks, bt, _stream(stream)), "bs_cache_append")
+    assert k.shape == v.shape == (T, Hkv, d) and k.dtype is v.dtype
+    kt, kh, k1 = k.stride()
+    vt, vh, v1 = v.stride()
+    assert k1 == 1 and v1 == 1, "the last dimension must be contiguous"
+    _call(_lib.bs_cache_append, "bs_cache_append", k_cache.device, stream, k.data_ptr(), v.data_ptr(), _dtype_code(k), kt, kh, vt, vh,
+          _i32(slot_map, T), T, Hkv, d, k_cache.data_ptr(), k_scale.data_ptr(), v_cache.data_ptr(), v_scale.data_ptr(), n_blocks, bt)
 
 
 def new_cache_workspace(Hq: int, Hkv: int, d: int, device="cuda") -> torch.Tensor:
@@ -397,17 +398,16 @@ def bs_cache_attention(q, cu_new, kv_len, block_table, node_parent, k_cache, k_s
     None: chains; [B, Nmax] int32: trees of drafts."""
     n_blocks, Hkv, bt, d = _cache_args(k_cache, k_scale, v_cache, v_scale)
     B, W = block_table.shape
-    T, Hq = q.shape[0], q.shape[1]
-    assert q.dtype == out.dtype == torch.bfloat16 and q.shape[2] == d and out.shape == q.shape
-    assert q.stride(2) == 1 and out.stride(2) == 1, "the last dimension must be contiguous"
+    T, Hq, dq = q.shape
+    assert q.dtype is torch.bfloat16 and out.dtype is torch.bfloat16 and dq == d and out.shape == q.shape
+    qt, qh, q1 = q.stride()
+    ot, oh, o1 = out.stride()
+    assert q1 == 1 and o1 == 1, "the last dimension must be contiguous"
     Nmax = 0 if node_parent is None else node_parent.shape[1]
-    with _on(k_cache):
-        _check(_lib.bs_cache_attention(q.data_ptr(), q.stride(0), q.stride(1), _i32(cu_new, B + 1), _i32(kv_len, B),
-                                       _i32(block_table, B, W), W, _i32(node_parent, B, Nmax), Nmax, _ptr(k_cache),
-                                       _ptr(k_scale), _ptr(v_cache), _ptr(v_scale), n_blocks, bt, B, T, Hq, Hkv, d,
-                                       int(max_new), float(softmax_scale), out.data_ptr(), out.stride(0), out.stride(1),
-                                       _i32(status, B), _ptr(workspace), workspace.numel(), _stream(stream)),
-               "bs_cache_attention")
+    _call(_lib.bs_cache_attention, "bs_cache_attention", k_cache.device, stream, q.data_ptr(), qt, qh, _i32(cu_new, B + 1),
+          _i32(kv_len, B), _i32(block_table, B * W), W, _i32(node_parent, B * Nmax), Nmax, k_cache.data_ptr(), k_scale.data_ptr(),
+          v_cache.data_ptr(), v_scale.data_ptr(), n_blocks, bt, B, T, Hq, Hkv, d, max_new, softmax_scale, out.data_ptr(), ot, oh,
+          _i32(status, B), workspace.data_ptr(), workspace.numel())
 
 
 def bs_cache_keep_path(out_nodes, accept_len, seq_len, block_table, k_cache, k_scale, v_cache, v_scale, status,
@@ -416,10 +416,9 @@ def bs_cache_keep_path(out_nodes, accept_len, seq_len, block_table, k_cache, k_s
     n_blocks, Hkv, bt, d = _cache_args(k_cache, k_scale, v_cache, v_scale)
     B, W = block_table.shape
     Nmax = out_nodes.shape[1]
-    with _on(k_cache):
-        _check(_lib.bs_cache_keep_path(_i32(out_nodes, B, Nmax), _i32(accept_len, B), _i32(seq_len, B), B, Nmax,
-                                       _i32(block_table, B, W), W, Hkv, d, _ptr(k_cache), _ptr(k_scale), _ptr(v_cache),
-                                       _ptr(v_scale), n_blocks, bt, _i32(status, B), _stream(stream)), "bs_cache_keep_path")
+    _call(_lib.bs_cache_keep_path, "bs_cache_keep_path", k_cache.device, stream, _i32(out_nodes, B * Nmax), _i32(accept_len, B),
+          _i32(seq_len, B), B, Nmax, _i32(block_table, B * W), W, Hkv, d, k_cache.data_ptr(), k_scale.data_ptr(), v_cache.data_ptr(),
+          v_scale.data_ptr(), n_blocks, bt, _i32(status, B))
 
 
 # ---- bandits ---------------------------------------------------------------------------

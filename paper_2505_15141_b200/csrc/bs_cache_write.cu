@@ -24,23 +24,30 @@ struct CacheAppendParams {
 constexpr int kApThreads = 256;
 constexpr int kApSteps = 8;           // 16-byte pieces of a run a lane holds
 
-template <typename T> __device__ __forceinline__ void load8(const T* p, float (&f)[8]);
-template <> __device__ __forceinline__ void load8<__nv_bfloat16>(const __nv_bfloat16* p, float (&f)[8]) {
-    Elem<__nv_bfloat16>::unpack(ld_stream(reinterpret_cast<const uint4*>(p)), f);
-}
-template <> __device__ __forceinline__ void load8<float>(const float* p, float (&f)[8]) {
-    float a[4], b[4];
-    Elem<float>::unpack(ld_stream(reinterpret_cast<const uint4*>(p)), a);
-    Elem<float>::unpack(ld_stream(reinterpret_cast<const uint4*>(p) + 1), b);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) { f[i] = a[i]; f[4 + i] = b[i]; }
-}
+// Eight values as they were loaded.
+template <typename T> struct Raw8;
+template <> struct Raw8<__nv_bfloat16> {
+    uint4 v;
+    __device__ __forceinline__ void load(const __nv_bfloat16* p) { v = ld_stream(reinterpret_cast<const uint4*>(p)); }
+    __device__ __forceinline__ void unpack(float (&f)[8]) const { Elem<__nv_bfloat16>::unpack(v, f); }
+};
+template <> struct Raw8<float> {
+    uint4 v, w;
+    __device__ __forceinline__ void load(const float* p) {
+        v = ld_stream(reinterpret_cast<const uint4*>(p));
+        w = ld_stream(reinterpret_cast<const uint4*>(p) + 1);
+    }
+    __device__ __forceinline__ void unpack(float (&f)[8]) const {
+        f[0] = __uint_as_float(v.x); f[1] = __uint_as_float(v.y); f[2] = __uint_as_float(v.z); f[3] = __uint_as_float(v.w);
+        f[4] = __uint_as_float(w.x); f[5] = __uint_as_float(w.y); f[6] = __uint_as_float(w.z); f[7] = __uint_as_float(w.w);
+    }
+};
 
 // A run is a maximal stretch of tokens whose slots are consecutive within one block.  A group of warps owns the
 // runs that begin among `unit` consecutive tokens, for one head of the keys or of the values.  A run is held in
 // registers whole (eight tokens' 16-byte pieces per lane: 16 tokens of 128 values per warp, as many warps as the
-// block needs), so the input is read once: maximum, scale, codes.  One pass over the data, bound by HBM on
-// prompts, by latency on a round.
+// block needs), so the input is read once: maximum, scale, codes.  Bound by HBM on prompts, by latency on a round.  The
+// loads of a run are unconditional (tokens behind it repeat its last one) so that all of them are in flight at once.
 template <typename T, int D>
 __global__ void __launch_bounds__(kApThreads) cache_append_kernel(const CacheAppendParams p) {
     constexpr int kLanes = D / 8;                             // lanes that hold a token
@@ -50,9 +57,10 @@ __global__ void __launch_bounds__(kApThreads) cache_append_kernel(const CacheApp
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int nw = 1 << p.warps_log2;
     const int group = warp >> p.warps_log2, w = warp & (nw - 1);
-    const long long unit = (long long)blockIdx.x * (kApThreads / 32 >> p.warps_log2) + group;
-    const int hk = (int)(unit % (2 * p.Hkv));
-    const long long first = (unit / (2 * p.Hkv)) << p.unit_log2;
+    const unsigned unit = blockIdx.x * (unsigned)(kApThreads / 32 >> p.warps_log2) + group;
+    const unsigned heads = 2u * p.Hkv, chunk = unit / heads;
+    const int hk = (int)(unit - chunk * heads);
+    const long long first = (long long)chunk << p.unit_log2;
     if (first >= p.T) return;                                 // whole groups leave: group barriers stay matched
     const int kv = hk >= p.Hkv, h = hk - kv * p.Hkv;
     const T* x = static_cast<const T*>(kv ? p.x[1] : p.x[0]) + (long long)h * (kv ? p.stride_h[1] : p.stride_h[0]);
@@ -68,8 +76,8 @@ __global__ void __launch_bounds__(kApThreads) cache_append_kernel(const CacheApp
     for (int i0 = (int)first; i0 < last; i0 += 32) {
         const int ti = i0 + lane;
         const int slot = ti < last ? __ldg(p.slot_map + ti) : -1;
+        const int before = ti < last && ti > 0 ? __ldg(p.slot_map + ti - 1) : -2;
         const bool ok = slot >= 0 && slot < nslots;
-        const int before = ok && ti > 0 ? __ldg(p.slot_map + ti - 1) : -2;
         unsigned leaders = __ballot_sync(0xffffffffu, ok && (before + 1 != slot || (slot & mask) == 0));
         while (leaders) {
             const int src = __ffs(leaders) - 1;
@@ -77,35 +85,43 @@ __global__ void __launch_bounds__(kApThreads) cache_append_kernel(const CacheApp
             const int i = i0 + src;
             const int slot0 = __shfl_sync(0xffffffffu, slot, src);
             const int blk = slot0 >> p.bt_log2, off0 = slot0 & mask;
-            int n = 0;                                        // length of the run
-            for (int j0 = 0; j0 < p.bt - off0; j0 += 32) {
-                const int j = j0 + lane;
-                const bool in = j < p.bt - off0 && i + j < p.T && __ldg(p.slot_map + i + j) == slot0 + j;
-                const unsigned m = __ballot_sync(0xffffffffu, in);
-                n += m == 0xffffffffu ? 32 : __ffs(~m) - 1;
-                if (m != 0xffffffffu) break;
+            // length of the run: up to 128 slots, all loads at once
+            int n = 0;
+            {
+                int z[4];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int j = q * 32 + lane;
+                    z[q] = j < p.bt - off0 && i + j < p.T ? __ldg(p.slot_map + i + j) : -1;
+                }
+                bool whole = true;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const unsigned m = __ballot_sync(0xffffffffu, z[q] == slot0 + q * 32 + lane);
+                    if (whole) n += m == 0xffffffffu ? 32 : __ffs(~m) - 1;
+                    whole = whole && m == 0xffffffffu;
+                }
             }
             float* sc = scales + (size_t)blk * p.Hkv + h;
             uint8_t* block = cache + (((size_t)blk * p.Hkv + h) << p.bt_log2) * D;
             const float old = off0 ? __ldcg(sc) : 0.f;
-            float v[kApSteps][8];
-            uint2 was[kApSteps];
+            Raw8<T> v[kApSteps];
+            const T* row0 = x + (long long)i * st + piece;
+#pragma unroll
+            for (int s = 0; s < kApSteps; ++s) {
+                const int j = ((((s << p.warps_log2) + w) * kPer) + sub) - off0;
+                v[s].load(row0 + (long long)min(max(j, 0), n - 1) * st);
+            }
             float mx = 0.f;
 #pragma unroll
-            for (int s = 0; s < kApSteps; ++s) {
-                const int off = (((s << p.warps_log2) + w) * kPer) + sub;
-                if (off >= off0 && off < off0 + n) load8<T>(x + (long long)(i + off - off0) * st + piece, v[s]);
-                else if (off < off0) was[s] = __ldcg(reinterpret_cast<const uint2*>(block + off * D + piece));
-            }
+            for (int s = 0; s < kApSteps; ++s) {              // the repeated tokens do not change the maximum
+                float f[8];
+                v[s].unpack(f);
 #pragma unroll
-            for (int s = 0; s < kApSteps; ++s) {
-                const int off = (((s << p.warps_log2) + w) * kPer) + sub;
-                if (off >= off0 && off < off0 + n)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {             // infinities and NaN do not set the scale
-                        const float a = fabsf(v[s][e]);
-                        if (a <= 3.402823466e38f) mx = fmaxf(mx, a);
-                    }
+                for (int e = 0; e < 8; ++e) {                 // infinities and NaN do not set the scale
+                    const float a = fabsf(f[e]);
+                    mx = fmaxf(mx, a <= 3.402823466e38f ? a : 0.f);
+                }
             }
             mx = warp_max(mx);
             if (nw > 1) {
@@ -118,16 +134,27 @@ __global__ void __launch_bounds__(kApThreads) cache_append_kernel(const CacheApp
             const float now = off0 ? fmaxf(old, fresh) : fresh;
             const float inv = 1.f / now;                      // exact: a power of two
             const bool grow = off0 && fresh > old;
-            const float again = old * inv;
 #pragma unroll
             for (int s = 0; s < kApSteps; ++s) {
                 const int off = (((s << p.warps_log2) + w) * kPer) + sub;
-                uint2* dst = reinterpret_cast<uint2*>(block + off * D + piece);
-                if (off >= off0 && off < off0 + n)
-                    *dst = make_uint2(e4m3x4(v[s][0] * inv, v[s][1] * inv, v[s][2] * inv, v[s][3] * inv),
-                                      e4m3x4(v[s][4] * inv, v[s][5] * inv, v[s][6] * inv, v[s][7] * inv));
-                else if (off < off0 && grow)
-                    *dst = make_uint2(rescale_codes(was[s].x, again), rescale_codes(was[s].y, again));
+                if (off >= off0 && off < off0 + n) {
+                    float f[8];
+                    v[s].unpack(f);
+                    *reinterpret_cast<uint2*>(block + off * D + piece) =
+                        make_uint2(e4m3x4(f[0] * inv, f[1] * inv, f[2] * inv, f[3] * inv),
+                                   e4m3x4(f[4] * inv, f[5] * inv, f[6] * inv, f[7] * inv));
+                }
+            }
+            if (grow) {                                       // older tokens of the block follow its scale
+                const float again = old * inv;
+                for (int s = 0; s < kApSteps; ++s) {
+                    const int off = (((s << p.warps_log2) + w) * kPer) + sub;
+                    if (off < off0) {
+                        uint2* q = reinterpret_cast<uint2*>(block + off * D + piece);
+                        const uint2 c = __ldcg(q);
+                        *q = make_uint2(rescale_codes(c.x, again), rescale_codes(c.y, again));
+                    }
+                }
             }
             if (w == 0 && lane == 0 && (grow || !off0)) *sc = now;
         }
@@ -281,7 +308,7 @@ extern "C" bs_status bs_cache_append(const void* k, const void* v, bs_dtype dtyp
     const long long units = (((long long)T + (1ll << p.unit_log2) - 1) >> p.unit_log2) * 2 * Hkv;
     const int per = kApThreads / 32 >> p.warps_log2;
     const long long grid = (units + per - 1) / per;
-    if (grid > 0x7fffffffLL) return BS_ERR_UNSUPPORTED;
+    if (units > 0x7fffffffLL) return BS_ERR_UNSUPPORTED;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (dtype == BS_F32)
         return cuda_status(d == 64 ? launch_pdl(cache_append_kernel<float, 64>, (unsigned)grid, kApThreads, 0, st, p)

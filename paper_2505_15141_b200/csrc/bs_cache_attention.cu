@@ -50,8 +50,8 @@ __device__ __forceinline__ float ca_row_sums16(float (&x)[16], int lane) {
 }
 
 template <int N, int D> struct CaLayout {
-    static constexpr int kGroups = 2;                         // softmax groups
-    static constexpr int kWarps = 8 + 4 * kGroups + 2;        // 2 producers, 2 MMA issuers, 4 accumulator, softmax, 2 query warps
+    static constexpr int kGroups = 2;                         // softmax groups = tiles in flight
+    static constexpr int kWarps = 8 + 4 * kGroups;            // 2 producers, MMA issuer, queries, 4 accumulator, softmax
     static constexpr int kThreads = 32 * kWarps;
     // An MMA costs the same for 16 to 64 rows: the two terms of the split operand are one operand of twice the rows
     // (results in columns of their own, added when they are read), half the instructions.
@@ -68,7 +68,7 @@ template <int N, int D> struct CaLayout {
     static constexpr int kRing = kSlotsFit / 2 > 6 ? 6 : kSlotsFit / 2;   // tiles in the ring of K, and in that of V
     static constexpr int kDynamic = 2 * kRing * kTileBytes + kFixed + 1024;
     static constexpr int kPiece = N * D + 2 * N;              // floats of a partial result
-    static_assert(kRing >= 3 && kRing < kCaScaleRing, "ring");
+    static_assert(kRing >= 3 && kRing + 2 <= kCaScaleRing, "ring");
     static_assert(kColsUsed <= 512, "tensor memory");
     static_assert(N % 16 == 0 && N <= 32, "rows");
 };
@@ -86,8 +86,8 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_co
     unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(ca_smem_raw) + 1023) & ~(uintptr_t)1023);
     unsigned char* s_q = smem + 2 * RING * L::kTileBytes;        // [2 buffers][2 terms]
     unsigned char* s_p = s_q + 4 * L::kQBytes;                // [2 groups][2 terms]
-    __shared__ __align__(8) unsigned long long b_full[2][RING], b_empty[2][RING], b_qfull[2], b_qempty[2], b_s[NG], b_p[NG],
-        b_o[NG], b_ofree[NG], b_mt[NG][2], b_l[2], b_lfree[2], b_drain[2];
+    __shared__ __align__(8) unsigned long long b_full[2][RING], b_empty[2][RING], b_scale[kCaScaleRing], b_qfull[2], b_qempty[2], b_s[NG], b_p[NG],
+        b_o[NG], b_ofree[NG], b_mt[NG][2], b_l[2], b_lfree[2], b_drain;
     __shared__ __align__(16) float s_red[NG][4][N];           // maxima of the warps of a softmax group
     __shared__ __align__(16) float s_lred[NG][4][N];          // sums of the warps of a softmax group
     __shared__ __align__(16) float s_m[4 * NG][N];            // per softmax warp: 8 - the tile's maximum
@@ -106,13 +106,12 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_co
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     if (tid == 0) {
-        ca_init_rings<RING>(b_full, b_empty);
+        ca_init_rings<RING>(b_full, b_empty, b_scale);
         for (int a = 0; a < 2; ++a) {
-            mbar_init(smem_u32(&b_qfull[a]), 2);              // the two query warps
+            mbar_init(smem_u32(&b_qfull[a]), 1);
             mbar_init(smem_u32(&b_qempty[a]), 1 + 4 * NG);    // the MMAs and the softmax warps
             mbar_init(smem_u32(&b_l[a]), 4 * NG);
             mbar_init(smem_u32(&b_lfree[a]), 4);
-            mbar_init(smem_u32(&b_drain[a]), 1);
             s_nan_any[a] = 0;
         }
         for (int g = 0; g < NG; ++g) {
@@ -123,6 +122,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_co
             mbar_init(smem_u32(&b_mt[g][0]), 1);
             mbar_init(smem_u32(&b_mt[g][1]), 1);
         }
+        mbar_init(smem_u32(&b_drain), 1);
         s_abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -140,84 +140,69 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_co
 
     if (warp < 2) {
         // K: warp 0, V: warp 1
-        ca_produce<D, RING>(p, cur, warp, warp ? &tm_v : &tm_k, smem + warp * RING * L::kTileBytes, b_full[warp], b_empty[warp], s_scale, &s_abort);
+        ca_produce<D, RING>(p, cur, warp, warp ? &tm_v : &tm_k, smem + warp * RING * L::kTileBytes, b_full[warp], b_empty[warp], b_scale, s_scale, &s_abort);
     } else if (warp == 2) {
-        // ============================ MMA issuer of S^T = K Q^T ============================
-        // runs NG tiles ahead: S of tile j is issued when that of tile j - NG has been taken out of tensor memory
-        constexpr int kN = L::kCols;
-        constexpr uint32_t idesc = (1u << 4) | ((uint32_t)(kN >> 3) << 17) | ((uint32_t)(kCaTile >> 4) << 24);
+        // ================================= MMA issuer =================================
+        // S of tiles 0 and 1, then, whenever the probabilities of a tile are there: S of the tile two further on, whose
+        // place in tensor memory they have left, and O of the tile itself.
+        constexpr uint32_t id_s = (1u << 4) | ((uint32_t)(L::kCols >> 3) << 17) | ((uint32_t)(kCaTile >> 4) << 24);
+        constexpr uint32_t id_o = (1u << 4) | (1u << 15) | (1u << 16) | ((uint32_t)(L::kCols >> 3) << 17) | ((uint32_t)(D >> 4) << 24);
         const uint32_t elected = ca_elect();
-        uint32_t j = 0, slot = 0, ph = 0;
-        int item = 0;
+        const uint32_t total = (uint32_t)(cur.end - cur.x);
+        uint32_t ks = 0, kph = 0, vs = 0, vph = 0;            // places in the rings of K and V
+        int item = -1, left = 0;                              // tiles of the item whose S is still to be issued
         bool ok = true;
 #pragma unroll 1
-        while (cur.x < cur.end && ok) {
-            const int nt = ca_tiles_here(cur);
-            ok = ca_wait(smem_u32(&b_qfull[item & 1]), (uint32_t)((item >> 1) & 1));
-            const uint64_t dq = ca_desc(smem_u32(s_q + (item & 1) * 2 * L::kQBytes), 128, 8 * D, 0);
-#pragma unroll 1
-            for (int t = 0; t < nt && ok; ++t, ++j) {
-                const uint32_t g = j % NG;
-                if ((j >= NG && !ca_wait(smem_u32(&b_p[g]), (j / NG - 1) & 1)) || !ca_wait(smem_u32(&b_full[0][slot]), ph) ||
+        for (uint32_t j = 0; j < total + 2 && ok; ++j) {      // S of tile j, O of tile j - 2
+            const uint32_t u = j & 1;
+            if (j >= 2) ok = ca_wait(smem_u32(&b_p[u]), ((j >> 1) - 1) & 1);
+            if (ok && j < total) {
+                if (left == 0) {
+                    if (item >= 0) ca_advance(p, cur, ca_tiles_here(cur));
+                    ++item;
+                    left = ca_tiles_here(cur);
+                    ok = ca_wait(smem_u32(&b_qfull[item & 1]), (uint32_t)((item >> 1) & 1));
+                }
+                ok = ok && ca_wait(smem_u32(&b_full[0][ks]), kph) && !__any_sync(0xffffffffu, s_abort);
+                if (!ok) break;
+                tc_fence_after();
+                const uint64_t dk = ca_desc(smem_u32(smem + ks * L::kTileBytes), 16, 8 * D, kSw);
+                const uint64_t dq = ca_desc(smem_u32(s_q + (item & 1) * 2 * L::kQBytes), 128, 8 * D, 0);
+#pragma unroll
+                for (int s = 0; s < D / 32; ++s)
+                    ca_mma(tmem + u * L::kCols, dk + ((s * 32) >> 4), dq + ((s * 256) >> 4), id_s, s ? 1u : 0u, elected);
+                ca_commit(smem_u32(&b_s[u]), elected);
+                ca_commit(smem_u32(&b_empty[0][ks]), elected);
+                if (--left == 0) ca_commit(smem_u32(&b_qempty[item & 1]), elected);
+                if (++ks == RING) { ks = 0; kph ^= 1u; }
+            }
+            if (ok && j >= 2) {
+                const uint32_t k = j - 2;
+                if (!ca_wait(smem_u32(&b_full[1][vs]), vph) || (k >= 2 && !ca_wait(smem_u32(&b_ofree[u]), ((k >> 1) - 1) & 1)) ||
                     __any_sync(0xffffffffu, s_abort)) {
                     ok = false;
                     break;
                 }
                 tc_fence_after();
-                const uint64_t dk = ca_desc(smem_u32(smem + slot * L::kTileBytes), 16, 8 * D, kSw);
+                const uint64_t dv = ca_desc(smem_u32(smem + (RING + vs) * L::kTileBytes), 0, 8 * D, kSw);
+                const uint64_t dp = ca_desc(smem_u32(s_p + u * 2 * L::kPBytes), 128, 2048, 0);
 #pragma unroll
-                for (int s = 0; s < D / 32; ++s)
-                    ca_mma(tmem + g * L::kCols, dk + ((s * 32) >> 4), dq + ((s * 256) >> 4), idesc, s ? 1u : 0u, elected);
-                ca_commit(smem_u32(&b_s[g]), elected);
-                ca_commit(smem_u32(&b_empty[0][slot]), elected);
-                if (++slot == RING) { slot = 0; ph ^= 1u; }
+                for (int s = 0; s < kCaTile / 32; ++s)
+                    ca_mma(tmem + L::kColO + u * L::kCols, dv + ((s * 32 * D) >> 4), dp + ((s * 512) >> 4), id_o, s ? 1u : 0u, elected);
+                ca_commit(smem_u32(&b_o[u]), elected);
+                ca_commit(smem_u32(&b_empty[1][vs]), elected);
+                if (++vs == RING) { vs = 0; vph ^= 1u; }
             }
-            if (ok) ca_commit(smem_u32(&b_qempty[item & 1]), elected);
-            ++item;
-            ca_advance(p, cur, nt);
         }
         if (!ok) {
             if (lane == 0) ca_give_up(p, &s_abort);
             __syncwarp();
-            ca_commit(smem_u32(&b_drain[0]), elected);        // leave no MMA in flight behind
-            ca_wait(smem_u32(&b_drain[0]), 0);
+            ca_commit(smem_u32(&b_drain), elected);           // leave no MMA in flight behind
+            ca_wait(smem_u32(&b_drain), 0);
         }
         __syncwarp();
     } else if (warp == 3) {
-        // =========================== MMA issuer of O^T = V^T P^T ===========================
-        constexpr int kN = L::kCols;
-        constexpr uint32_t idesc = (1u << 4) | (1u << 15) | (1u << 16) | ((uint32_t)(kN >> 3) << 17) | ((uint32_t)(D >> 4) << 24);
-        const uint32_t elected = ca_elect();
-        const uint32_t total = (uint32_t)(cur.end - cur.x);
-        uint32_t slot = 0, ph = 0;
-        bool ok = true;
-#pragma unroll 1
-        for (uint32_t k = 0; k < total && ok; ++k) {
-            const uint32_t g = k % NG;
-            if (!ca_wait(smem_u32(&b_p[g]), (k / NG) & 1) || !ca_wait(smem_u32(&b_full[1][slot]), ph) ||
-                (k >= NG && !ca_wait(smem_u32(&b_ofree[g]), (k / NG - 1) & 1)) || __any_sync(0xffffffffu, s_abort)) {
-                ok = false;
-                break;
-            }
-            tc_fence_after();
-            const uint64_t dv = ca_desc(smem_u32(smem + (RING + slot) * L::kTileBytes), 0, 8 * D, kSw);
-            const uint64_t dp = ca_desc(smem_u32(s_p + g * 2 * L::kPBytes), 128, 2048, 0);
-#pragma unroll
-            for (int s = 0; s < kCaTile / 32; ++s)
-                ca_mma(tmem + L::kColO + g * L::kCols, dv + ((s * 32 * D) >> 4), dp + ((s * 512) >> 4), idesc, s ? 1u : 0u, elected);
-            ca_commit(smem_u32(&b_o[g]), elected);
-            ca_commit(smem_u32(&b_empty[1][slot]), elected);
-            if (++slot == RING) { slot = 0; ph ^= 1u; }
-        }
-        if (!ok) {
-            if (lane == 0) ca_give_up(p, &s_abort);
-            __syncwarp();
-            ca_commit(smem_u32(&b_drain[1]), elected);
-            ca_wait(smem_u32(&b_drain[1]), 0);
-        }
-        __syncwarp();
-    } else if (warp >= 8 + 4 * NG) {
-        ca_queries<N, D>(p, cur, tid - 32 * (8 + 4 * NG), s_q, s_c, s_anc, b_qfull, b_qempty, &s_abort);
+        ca_queries<N, D>(p, cur, s_q, s_c, s_anc, b_qfull, b_qempty, &s_abort);
     } else if (warp < 8) {
         // ================================ accumulator ================================
         // O^T of every tile into fp32 (tensor memory, 16 rows at a time in one short loop: code that does not fit the
@@ -455,11 +440,12 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_co
                 const uint32_t kk = k / NG;
                 const uint32_t vslot = k % RING;
                 const bool first = t == t_first;
-                if (ok) ok = ca_wait(smem_u32(&b_full[1][vslot]), (k / RING) & 1) &&
+                if (ok) ok = ca_wait(smem_u32(&b_scale[k % kCaScaleRing]), (k / kCaScaleRing) & 1) &&
                              (!first || ca_wait(smem_u32(&b_qfull[buf]), (uint32_t)((item >> 1) & 1))) &&   // its constants
                              !__any_sync(0xffffffffu, s_abort);
                 const int pos = t * kCaTile + tok;
                 const bool masked = (t + 1) * kCaTile > seen;
+                if (ok && masked) ok = ca_wait(smem_u32(&b_full[1][vslot]), (k / RING) & 1);   // V is looked at
                 uint32_t vis = ~0u;                           // rows that see this thread's token
                 float ks = 0.f, lsv = 0.f, isv = 0.f;
                 if (ok) {

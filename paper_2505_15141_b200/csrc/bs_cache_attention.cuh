@@ -346,10 +346,10 @@ __device__ __forceinline__ void ca_give_up(const CacheAttnParams& p, volatile in
 // ---- TMA producer: one warp for the tiles of K (kv = 0), one for those of V ----
 // One warp could not issue the copies of 16-token blocks fast enough (106 to 133 cycles each: 4.3 TB/s measured for one
 // warp, 6.5 TB/s for two).  The block numbers of up to 32 blocks are fetched one group ahead, across items, and the scales
-// travel with cp.async on V's barrier: nothing here waits for memory.
+// of a tile come with cp.async and a barrier of their own (the producer of K): nothing here waits for memory.
 template <int D, uint32_t RING>
 __device__ __forceinline__ void ca_produce(const CacheAttnParams& p, CaCursor cur, int kv, const CUtensorMap* tm, unsigned char* ring,
-                                           unsigned long long* b_full, unsigned long long* b_empty,
+                                           unsigned long long* b_full, unsigned long long* b_empty, unsigned long long* b_scale,
                                            float (*s_scale)[kCaMaxPages][2], volatile int* s_abort) {
     const int lane = threadIdx.x & 31;
     const uint32_t elected = ca_elect();
@@ -389,16 +389,16 @@ __device__ __forceinline__ void ca_produce(const CacheAttnParams& p, CaCursor cu
 #pragma unroll 1
             for (int i = 0; i < pages; ++i, dst += page_bytes)
                 ca_tma(dst, tm, __shfl_sync(0xffffffffu, ids, (j << ppt_log2) + i) * p.Hkv + cur.h, bar, elected);
-            if (kv) {
+            if (!kv) {
                 const int blk = __shfl_sync(0xffffffffu, ids, ((j << ppt_log2) + lane) & 31);
                 if (lane < pages) {
-                    // the ring of scales is deeper than that of V: its entry is free when the slot is
+                    // S of two tiles at most is ahead of the softmax, so the entry of tile - 8 has been read
                     const uint32_t at = smem_u32(s_scale[tile % kCaScaleRing][lane]);
                     const size_t e = (size_t)blk * p.Hkv + cur.h;
                     asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(at), "l"(p.k_scale + e) : "memory");
                     asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(at + 4), "l"(p.v_scale + e) : "memory");
                 }
-                asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
+                asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(b_scale + tile % kCaScaleRing)) : "memory");
             }
             if (++slot == RING) { slot = 0; ph ^= 1u; }
         }
@@ -415,26 +415,27 @@ __device__ __forceinline__ void ca_produce(const CacheAttnParams& p, CaCursor cu
         __syncwarp();
     }
 }
-// Barriers of the rings: V's also counts the lanes that bring scales.
 template <uint32_t RING>
-__device__ __forceinline__ void ca_init_rings(unsigned long long (*b_full)[RING], unsigned long long (*b_empty)[RING]) {
-    for (uint32_t s = 0; s < RING; ++s) {
-        mbar_init(smem_u32(&b_full[0][s]), 1);
-        mbar_init(smem_u32(&b_full[1][s]), 33);
-        mbar_init(smem_u32(&b_empty[0][s]), 1);
-        mbar_init(smem_u32(&b_empty[1][s]), 1);
-    }
+__device__ __forceinline__ void ca_init_rings(unsigned long long (*b_full)[RING], unsigned long long (*b_empty)[RING],
+                                              unsigned long long* b_scale) {
+    for (uint32_t s = 0; s < RING; ++s)
+        for (int kv = 0; kv < 2; ++kv) {
+            mbar_init(smem_u32(&b_full[kv][s]), 1);
+            mbar_init(smem_u32(&b_empty[kv][s]), 1);
+        }
+    for (int s = 0; s < kCaScaleRing; ++s) mbar_init(smem_u32(b_scale + s), 32);   // the producer's lanes
 }
 
-// ---- queries: two warps split them into e4m3, an item ahead ----
+// ---- queries: a warp splits them into e4m3, an item ahead ----
 // Buffer i of shared memory: hi, then lo, ROWS x D bytes each, in 8 x 16-byte core matrices.
 template <int ROWS, int D>
-__device__ __forceinline__ void ca_queries(const CacheAttnParams& p, CaCursor cur, int qt, unsigned char* s_q, float (*s_c)[ROWS],
+__device__ __forceinline__ void ca_queries(const CacheAttnParams& p, CaCursor cur, unsigned char* s_q, float (*s_c)[ROWS],
                                            uint32_t (*s_anc)[32], unsigned long long* b_qfull, unsigned long long* b_qempty,
                                            volatile int* s_abort) {
     constexpr int kLanes = D / 8;                             // lanes of a row
-    constexpr int kRows = 64 / kLanes;                        // rows per pass of the two warps
-    const int lane = qt & 31, sub = qt / kLanes, piece = (qt % kLanes) * 8;
+    constexpr int kRows = 32 / kLanes;                        // rows per pass
+    const int lane = threadIdx.x & 31, sub = lane / kLanes, piece = (lane % kLanes) * 8;
+    const int inv_g = (65536 + p.G - 1) / p.G;                // exact for r < 128, G <= 64
     int item = 0;
     bool ok = true;
 #pragma unroll 1
@@ -444,41 +445,52 @@ __device__ __forceinline__ void ca_queries(const CacheAttnParams& p, CaCursor cu
         if (!ok) break;
         const int i0 = cur.rt * p.TQ, rows = min(p.TQ, cur.n - i0) * p.G;
         unsigned char* q_hi = s_q + buf * 2 * (ROWS * D);
-#pragma unroll 4
-        for (int r0 = 0; r0 < ROWS; r0 += kRows) {
-            const int r = r0 + sub;
-            float f[8];
+        // the loads of a batch of rows first: one by one, each would wait for memory (1400 cycles a pass, measured)
+        constexpr int kBatch = ROWS / kRows < 8 ? ROWS / kRows : 8;
+#pragma unroll 1
+        for (int rb = 0; rb < ROWS; rb += kBatch * kRows) {
+            uint4 raw[kBatch];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) f[e] = 0.f;
-            if (r < rows)
-                Elem<__nv_bfloat16>::unpack(__ldg(reinterpret_cast<const uint4*>(
-                    p.q + (long long)(cur.q0 + i0 + r / p.G) * p.q_st + (long long)(cur.h * p.G + r % p.G) * p.q_sh + piece)), f);
-            float mx = 0.f;
-            bool fin = true;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                mx = fmaxf(mx, fabsf(f[e]));
-                fin = fin && fabsf(f[e]) <= 3.402823466e38f;
+            for (int z = 0; z < kBatch; ++z) {
+                const int r = min(rb + z * kRows + sub, rows - 1), i = r * inv_g >> 16;   // r / G
+                raw[z] = __ldg(reinterpret_cast<const uint4*>(p.q + (long long)(cur.q0 + i0 + i) * p.q_st +
+                                                              (long long)(cur.h * p.G + r - i * p.G) * p.q_sh + piece));
             }
 #pragma unroll
-            for (int o = kLanes / 2; o > 0; o >>= 1) {
-                mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-                fin = __shfl_xor_sync(0xffffffffu, (int)fin, o) && fin;
+            for (int z = 0; z < kBatch; ++z) {
+                const int r = rb + z * kRows + sub;
+                float f[8];
+                Elem<__nv_bfloat16>::unpack(raw[z], f);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) f[e] = r < rows ? f[e] : 0.f;
+                float mx = 0.f;
+                bool fin = true;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    mx = fmaxf(mx, fabsf(f[e]));
+                    fin = fin && fabsf(f[e]) <= 3.402823466e38f;
+                }
+#pragma unroll
+                for (int o = kLanes / 2; o > 0; o >>= 1) {
+                    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+                    fin = __shfl_xor_sync(0xffffffffu, (int)fin, o) && fin;
+                }
+                // 2^x brings the row's largest element into [128, 256)
+                int x = mx > 0.f && fin ? 7 - ((int)(__float_as_uint(mx) >> 23) - 127) : 0;
+                x = min(x, 120);
+                const float up = __uint_as_float((uint32_t)(x + 127) << 23);
+                uint2 hi, lo;
+                ca_split4(f[0] * up, f[1] * up, f[2] * up, f[3] * up, hi.x, lo.x);
+                ca_split4(f[4] * up, f[5] * up, f[6] * up, f[7] * up, hi.y, lo.y);
+                unsigned char* at = q_hi + (r >> 3) * (8 * D) + (piece >> 4) * 128 + (r & 7) * 16 + (piece & 15);
+                *reinterpret_cast<uint2*>(at) = hi;
+                *reinterpret_cast<uint2*>(at + ROWS * D) = lo;
+                // a row with an infinity or a NaN has no softmax: its scale makes every result NaN
+                if (piece == 0)
+                    s_c[buf][r] = r >= rows ? 0.f : fin ? p.scale_log2 * __uint_as_float((uint32_t)(127 - x) << 23) : __int_as_float(0x7fc00000);
             }
-            // 2^x brings the row's largest element into [128, 256)
-            int x = mx > 0.f && fin ? 7 - ((int)(__float_as_uint(mx) >> 23) - 127) : 0;
-            x = min(x, 120);
-            const float up = __uint_as_float((uint32_t)(x + 127) << 23);
-            uint2 hi, lo;
-            ca_split4(f[0] * up, f[1] * up, f[2] * up, f[3] * up, hi.x, lo.x);
-            ca_split4(f[4] * up, f[5] * up, f[6] * up, f[7] * up, hi.y, lo.y);
-            unsigned char* at = q_hi + (r >> 3) * (8 * D) + (piece >> 4) * 128 + (r & 7) * 16 + (piece & 15);
-            *reinterpret_cast<uint2*>(at) = hi;
-            *reinterpret_cast<uint2*>(at + ROWS * D) = lo;
-            // a row with an infinity or a NaN has no softmax: its scale makes every result NaN
-            if (piece == 0) s_c[buf][r] = r >= rows ? 0.f : fin ? p.scale_log2 * __uint_as_float((uint32_t)(127 - x) << 23) : __int_as_float(0x7fc00000);
         }
-        if (p.node_parent && qt < 32) {                       // ancestors-or-self of node `lane`
+        if (p.node_parent) {                       // ancestors-or-self of node `lane`
             int par = 0;
             if (lane >= 1 && lane < cur.n) {
                 par = __ldg(p.node_parent + (size_t)cur.b * p.Nmax + lane - 1);

@@ -14,7 +14,7 @@
 //
 // Tensor memory: S of two tiles, O of one, the fp32 accumulator (O * 2^(m_tile - m) is added after every tile, as there).
 //
-// Warps: 0, 1 producers, 2 MMA issuer of S, 3 of O, 4-7 accumulator, then the softmax teams, then two query warps.
+// Warps: 0, 1 producers, 2 MMA issuer, 3 queries, 4-7 accumulator, then the softmax teams.
 #include "bs_cache_attention.cuh"
 
 namespace bs {
@@ -24,7 +24,7 @@ template <int R, int D> struct CrLayout {
     static constexpr int kTeams = 2;                          // tiles in flight
     static constexpr int kHalves = 128 / R;                   // places a tile's rows can stand in
     static constexpr int kSoft = kTeams * kTeamWarps;
-    static constexpr int kWarps = 8 + kSoft + 2;
+    static constexpr int kWarps = 8 + kSoft;
     static constexpr int kThreads = 32 * kWarps;
     static constexpr int kColO = 256, kColA = 256 + D;        // S: 0-127, 128-255
     static constexpr int kTmemCols = 512;
@@ -39,7 +39,7 @@ template <int R, int D> struct CrLayout {
     static constexpr int kRing = kSlotsFit / 2 > 6 ? 6 : kSlotsFit / 2;
     static constexpr int kDynamic = 2 * kRing * kTileBytes + kFixed + 1024;
     static constexpr int kPiece = R * D + 2 * R;              // floats of a partial result
-    static_assert(kRing >= 2 && kRing < kCaScaleRing, "ring");
+    static_assert(kRing >= 2 && kRing + 2 <= kCaScaleRing, "ring");
     // Q is read from R rows before its buffer and up to R rows behind it: rings in front, P behind
     static_assert(2 * kRing * kTileBytes >= R * D && 2 * kPBufs * kPBytes >= R * D, "rows next to Q");
 };
@@ -57,8 +57,8 @@ cache_attention_rows_kernel(const __grid_constant__ CUtensorMap tm_k, const __gr
     unsigned char* s_q = smem + 2 * RING * L::kTileBytes;     // [2 buffers][2 terms]
     unsigned char* s_p = s_q + 4 * L::kQBytes;                // [buffers][2 terms]
     float* s_merge = reinterpret_cast<float*>(s_p + 2 * L::kPBufs * L::kPBytes);   // [D][R]
-    __shared__ __align__(8) unsigned long long b_full[2][RING], b_empty[2][RING], b_qfull[2], b_qempty[2], b_s[2], b_p[2], b_o[2],
-        b_ofree[2], b_mt[2][2], b_l[2], b_lfree[2], b_drain[2];
+    __shared__ __align__(8) unsigned long long b_full[2][RING], b_empty[2][RING], b_scale[kCaScaleRing], b_qfull[2], b_qempty[2], b_s[2], b_p[2], b_o[2],
+        b_ofree[2], b_mt[2][2], b_l[2], b_lfree[2], b_drain;
     __shared__ float s_c[2][R];                               // per query buffer: softmax scale of the row
     __shared__ uint32_t s_anc[2][32];                         // per query buffer: ancestors of the tree's nodes
     __shared__ float s_mt[2][2][R];                           // maxima of a team's tiles, for the accumulator
@@ -74,9 +74,9 @@ cache_attention_rows_kernel(const __grid_constant__ CUtensorMap tm_k, const __gr
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     if (tid == 0) {
-        ca_init_rings<RING>(b_full, b_empty);
+        ca_init_rings<RING>(b_full, b_empty, b_scale);
         for (int a = 0; a < 2; ++a) {
-            mbar_init(smem_u32(&b_qfull[a]), 2);              // the two query warps
+            mbar_init(smem_u32(&b_qfull[a]), 1);
             mbar_init(smem_u32(&b_qempty[a]), 1 + L::kSoft);  // the MMAs and the softmax warps
             mbar_init(smem_u32(&b_s[a]), 1);
             mbar_init(smem_u32(&b_p[a]), TW);
@@ -86,9 +86,9 @@ cache_attention_rows_kernel(const __grid_constant__ CUtensorMap tm_k, const __gr
             mbar_init(smem_u32(&b_mt[a][1]), TW);
             mbar_init(smem_u32(&b_l[a]), L::kSoft);
             mbar_init(smem_u32(&b_lfree[a]), 4);
-            mbar_init(smem_u32(&b_drain[a]), 1);
             s_nan_any[a] = 0;
         }
+        mbar_init(smem_u32(&b_drain), 1);
         s_abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -105,87 +105,73 @@ cache_attention_rows_kernel(const __grid_constant__ CUtensorMap tm_k, const __gr
 
     if (warp < 2) {
         // K: warp 0, V: warp 1
-        ca_produce<D, RING>(p, cur, warp, warp ? &tm_v : &tm_k, smem + warp * RING * L::kTileBytes, b_full[warp], b_empty[warp], s_scale, &s_abort);
+        ca_produce<D, RING>(p, cur, warp, warp ? &tm_v : &tm_k, smem + warp * RING * L::kTileBytes, b_full[warp], b_empty[warp], b_scale, s_scale, &s_abort);
     } else if (warp == 2) {
-        // ============================ MMA issuer of S = Q K^T ============================
-        constexpr uint32_t idesc = (1u << 4) | ((uint32_t)(kCaTile >> 3) << 17) | (8u << 24);
+        // ================================= MMA issuer =================================
+        // S of tiles 0 and 1, then, whenever the probabilities of a tile are there: S of the tile two further on, whose
+        // place in tensor memory they have left, and O of the tile itself.
+        constexpr uint32_t id_s = (1u << 4) | ((uint32_t)(kCaTile >> 3) << 17) | (8u << 24);
+        constexpr uint32_t id_o = (1u << 4) | (1u << 16) | ((uint32_t)(D >> 3) << 17) | (8u << 24);
         const uint32_t elected = ca_elect();
-        uint32_t j = 0, slot = 0, ph = 0;
-        int item = 0;
+        const uint32_t total = (uint32_t)(cur.end - cur.x);
+        uint32_t ks = 0, kph = 0, vs = 0, vph = 0;            // places in the rings of K and V
+        int item = -1, left = 0;                              // tiles of the item whose S is still to be issued
         bool ok = true;
 #pragma unroll 1
-        while (cur.x < cur.end && ok) {
-            const int nt = ca_tiles_here(cur);
-            ok = ca_wait(smem_u32(&b_qfull[item & 1]), (uint32_t)((item >> 1) & 1));
-            const uint32_t sq = smem_u32(s_q + (item & 1) * 2 * L::kQBytes);
-#pragma unroll 1
-            for (int t = 0; t < nt && ok; ++t, ++j) {
-                const uint32_t u = j & 1;
-                // S of tile j - 2 has been read when its P is there
-                if ((j >= 2 && !ca_wait(smem_u32(&b_p[u]), ((j >> 1) - 1) & 1)) || !ca_wait(smem_u32(&b_full[0][slot]), ph) ||
+        for (uint32_t j = 0; j < total + 2 && ok; ++j) {      // S of tile j, O of tile j - 2
+            const uint32_t u = j & 1;
+            if (j >= 2) ok = ca_wait(smem_u32(&b_p[u]), ((j >> 1) - 1) & 1);
+            if (ok && j < total) {
+                if (left == 0) {
+                    if (item >= 0) ca_advance(p, cur, ca_tiles_here(cur));
+                    ++item;
+                    left = ca_tiles_here(cur);
+                    ok = ca_wait(smem_u32(&b_qfull[item & 1]), (uint32_t)((item >> 1) & 1));
+                }
+                ok = ok && ca_wait(smem_u32(&b_full[0][ks]), kph) && !__any_sync(0xffffffffu, s_abort);
+                if (!ok) break;
+                tc_fence_after();
+                const uint64_t dk = ca_desc(smem_u32(smem + ks * L::kTileBytes), 16, 8 * D, kSw);
+                const uint64_t dq = ca_desc(smem_u32(s_q + (item & 1) * 2 * L::kQBytes) - (L::kHalves > 1 && u ? R * D : 0), 128, 8 * D, 0);
+#pragma unroll
+                for (int term = 0; term < 2; ++term)
+#pragma unroll
+                    for (int s = 0; s < D / 32; ++s)
+                        ca_mma(tmem + u * 128, dq + ((term * L::kQBytes + s * 256) >> 4), dk + ((s * 32) >> 4), id_s, (term | s) ? 1u : 0u, elected);
+                ca_commit(smem_u32(&b_s[u]), elected);
+                ca_commit(smem_u32(&b_empty[0][ks]), elected);
+                if (--left == 0) ca_commit(smem_u32(&b_qempty[item & 1]), elected);
+                if (++ks == RING) { ks = 0; kph ^= 1u; }
+            }
+            if (ok && j >= 2) {
+                const uint32_t k = j - 2;
+                if (!ca_wait(smem_u32(&b_full[1][vs]), vph) || (k >= 1 && !ca_wait(smem_u32(&b_ofree[u ^ 1]), ((k - 1) >> 1) & 1)) ||
                     __any_sync(0xffffffffu, s_abort)) {
                     ok = false;
                     break;
                 }
                 tc_fence_after();
-                const uint64_t dk = ca_desc(smem_u32(smem + slot * L::kTileBytes), 16, 8 * D, kSw);
-                const uint64_t dq = ca_desc(sq - (L::kHalves > 1 && u ? R * D : 0), 128, 8 * D, 0);
+                const uint64_t dv = ca_desc(smem_u32(smem + (RING + vs) * L::kTileBytes), 0, 8 * D, kSw);
+                const uint64_t dp = ca_desc(smem_u32(s_p + (L::kPBufs > 1 ? u * 2 * L::kPBytes : 0)), 128, 1024, 0);
 #pragma unroll
                 for (int term = 0; term < 2; ++term)
 #pragma unroll
-                    for (int s = 0; s < D / 32; ++s)
-                        ca_mma(tmem + u * 128, dq + ((term * L::kQBytes + s * 256) >> 4), dk + ((s * 32) >> 4), idesc, (term | s) ? 1u : 0u, elected);
-                ca_commit(smem_u32(&b_s[u]), elected);
-                ca_commit(smem_u32(&b_empty[0][slot]), elected);
-                if (++slot == RING) { slot = 0; ph ^= 1u; }
+                    for (int s = 0; s < kCaTile / 32; ++s)
+                        ca_mma(tmem + L::kColO, dp + ((term * L::kPBytes + s * 256) >> 4), dv + ((s * 32 * D) >> 4), id_o, (term | s) ? 1u : 0u, elected);
+                ca_commit(smem_u32(&b_o[u]), elected);
+                ca_commit(smem_u32(&b_empty[1][vs]), elected);
+                if (++vs == RING) { vs = 0; vph ^= 1u; }
             }
-            if (ok) ca_commit(smem_u32(&b_qempty[item & 1]), elected);
-            ++item;
-            ca_advance(p, cur, nt);
         }
         if (!ok) {
             if (lane == 0) ca_give_up(p, &s_abort);
             __syncwarp();
-            ca_commit(smem_u32(&b_drain[0]), elected);        // leave no MMA in flight behind
-            ca_wait(smem_u32(&b_drain[0]), 0);
+            ca_commit(smem_u32(&b_drain), elected);           // leave no MMA in flight behind
+            ca_wait(smem_u32(&b_drain), 0);
         }
         __syncwarp();
     } else if (warp == 3) {
-        // ============================ MMA issuer of O = P V ============================
-        constexpr uint32_t idesc = (1u << 4) | (1u << 16) | ((uint32_t)(D >> 3) << 17) | (8u << 24);
-        const uint32_t elected = ca_elect();
-        const uint32_t total = (uint32_t)(cur.end - cur.x);
-        uint32_t slot = 0, ph = 0;
-        bool ok = true;
-#pragma unroll 1
-        for (uint32_t k = 0; k < total && ok; ++k) {
-            const uint32_t u = k & 1;
-            if (!ca_wait(smem_u32(&b_p[u]), (k >> 1) & 1) || !ca_wait(smem_u32(&b_full[1][slot]), ph) ||
-                (k >= 1 && !ca_wait(smem_u32(&b_ofree[u ^ 1]), ((k - 1) >> 1) & 1)) || __any_sync(0xffffffffu, s_abort)) {
-                ok = false;
-                break;
-            }
-            tc_fence_after();
-            const uint64_t dv = ca_desc(smem_u32(smem + (RING + slot) * L::kTileBytes), 0, 8 * D, kSw);
-            const uint64_t dp = ca_desc(smem_u32(s_p + (L::kPBufs > 1 ? u * 2 * L::kPBytes : 0)), 128, 1024, 0);
-#pragma unroll
-            for (int term = 0; term < 2; ++term)
-#pragma unroll
-                for (int s = 0; s < kCaTile / 32; ++s)
-                    ca_mma(tmem + L::kColO, dp + ((term * L::kPBytes + s * 256) >> 4), dv + ((s * 32 * D) >> 4), idesc, (term | s) ? 1u : 0u, elected);
-            ca_commit(smem_u32(&b_o[u]), elected);
-            ca_commit(smem_u32(&b_empty[1][slot]), elected);
-            if (++slot == RING) { slot = 0; ph ^= 1u; }
-        }
-        if (!ok) {
-            if (lane == 0) ca_give_up(p, &s_abort);
-            __syncwarp();
-            ca_commit(smem_u32(&b_drain[1]), elected);
-            ca_wait(smem_u32(&b_drain[1]), 0);
-        }
-        __syncwarp();
-    } else if (warp >= 8 + L::kSoft) {
-        ca_queries<R, D>(p, cur, tid - 32 * (8 + L::kSoft), s_q, s_c, s_anc, b_qfull, b_qempty, &s_abort);
+        ca_queries<R, D>(p, cur, s_q, s_c, s_anc, b_qfull, b_qempty, &s_abort);
     } else if (warp < 8) {
         // ================================ accumulator ================================
         const int wq = warp & 3;                              // lane quarter of tensor memory
@@ -214,16 +200,28 @@ cache_attention_rows_kernel(const __grid_constant__ CUtensorMap tm_k, const __gr
                 ok = ca_wait(smem_u32(&b_o[u]), kk & 1);
                 if (!ok) continue;
                 tc_fence_after();
-#pragma unroll 2
-                for (int c = 0; c < D; c += 16) {
-                    float x[16], old[16];
-                    if (have) ca_ld16(t_acc + c, old);
-                    ca_ld16(t_lane + L::kColO + c, x);
-                    if (have) ca_ld16_wait(old);
-                    ca_ld16_wait(x);
+                float xa[16], oa[16], xb[16], ob[16];
+                auto join = [&](int c, float (&x)[16], const float (&old)[16]) {
 #pragma unroll
                     for (int i = 0; i < 16; ++i) x[i] = have ? fmaf(old[i], fa, x[i] * fb) : x[i] * fb;
                     ca_st16(t_acc + c, x);
+                };
+                ca_ld16(t_lane + L::kColO, xa);
+                ca_ld16(t_acc, oa);                           // not used before there is something
+#pragma unroll 1
+                for (int c = 0; c < D; c += 32) {
+                    ca_ld16_wait(xa);
+                    ca_ld16_wait(oa);
+                    ca_ld16(t_lane + L::kColO + c + 16, xb);
+                    ca_ld16(t_acc + c + 16, ob);
+                    join(c, xa, oa);
+                    ca_ld16_wait(xb);
+                    ca_ld16_wait(ob);
+                    if (c + 32 < D) {
+                        ca_ld16(t_lane + L::kColO + c + 32, xa);
+                        ca_ld16(t_acc + c + 32, oa);
+                    }
+                    join(c + 16, xb, ob);
                 }
                 have = true;
                 ca_st_wait();
@@ -416,7 +414,9 @@ cache_attention_rows_kernel(const __grid_constant__ CUtensorMap tm_k, const __gr
             for (int t = t_first; t < cur.t + nt && ok; t += 2) {
                 const uint32_t k = g0 + (uint32_t)(t - cur.t), kk = k >> 1;   // running tile number
                 const uint32_t vslot = k % RING;
-                ok = ca_wait(smem_u32(&b_full[1][vslot]), (k / RING) & 1) &&
+                const bool masked = (t + 1) * kCaTile > seen;
+                ok = ca_wait(smem_u32(&b_scale[k % kCaScaleRing]), (k / kCaScaleRing) & 1) &&
+                     (!masked || ca_wait(smem_u32(&b_full[1][vslot]), (k / RING) & 1)) &&   // V is looked at
                      (t != t_first || ca_wait(smem_u32(&b_qfull[buf]), (uint32_t)((item >> 1) & 1))) && !__any_sync(0xffffffffu, s_abort);
                 if (!ok) break;
                 if (t == t_first) {
@@ -426,7 +426,6 @@ cache_attention_rows_kernel(const __grid_constant__ CUtensorMap tm_k, const __gr
                     anc = p.node_parent ? s_anc[buf][i] : 0u;
                 }
                 const int pos0 = t * kCaTile;
-                const bool masked = pos0 + kCaTile > seen;
                 if (masked) {
 #pragma unroll 1
                     for (int j = tw * 32 + lane; j < kCaTile; j += TW * 32) {
@@ -460,34 +459,48 @@ cache_attention_rows_kernel(const __grid_constant__ CUtensorMap tm_k, const __gr
                     return v;
                 };
                 const float (*sc)[2] = s_scale[k % kCaScaleRing];
-                // pass 1: the row's maximum of t + log2(scale of V)
+                // pass 1: the row's maximum of t + log2(scale of V).  Tiles without a mask, nearly all of them, have short
+                // loops of their own; their tensor-memory loads run 16 tokens ahead.
                 float mx = -INFINITY;
+                auto scales16 = [&](int c, float& kx, float& sv) {
+                    const float2 z = *reinterpret_cast<const float2*>(sc[c >> p.bt_log2]);
+                    kx = z.x * cr;
+                    sv = fmaxf(z.y, 5.421010862e-20f);        // 2^-64
+                };
+                auto max16 = [&](int c, const float (&x)[16]) {
+                    float kx, sv, a[4];
+                    scales16(c, kx, sv);
+                    const float vx = __log2f(sv);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        a[i] = fmaxf(fmaxf(fmaf(x[4 * i], kx, vx), fmaf(x[4 * i + 1], kx, vx)),
+                                     fmaxf(fmaf(x[4 * i + 2], kx, vx), fmaf(x[4 * i + 3], kx, vx)));
+                    mx = fmaxf(mx, fmaxf(fmaxf(a[0], a[1]), fmaxf(a[2], a[3])));
+                };
+                float x[16], y[16];
+                if (masked) {
 #pragma unroll 1
-                for (int c = 0; c < kCaTile; c += 32) {
-                    float x[16], y[16];
-                    ca_ld16(t_s + c, x);
-                    ca_ld16(t_s + c + 16, y);
-                    const float kx = sc[c >> p.bt_log2][0] * cr, ky = sc[(c + 16) >> p.bt_log2][0] * cr;
-                    const float vx = __log2f(fmaxf(sc[c >> p.bt_log2][1], 5.421010862e-20f));       // 2^-64
-                    const float vy = __log2f(fmaxf(sc[(c + 16) >> p.bt_log2][1], 5.421010862e-20f));
-                    ca_ld16_wait(x);
-                    ca_ld16_wait(y);
-                    if (masked) {
-                        uint32_t sx = seen16(c), sy = seen16(c + 16);
-                        asm volatile("" : "+r"(sx), "+r"(sy));
+                    for (int c = 0; c < kCaTile; c += 16) {
+                        float kx, sv;
+                        scales16(c, kx, sv);
+                        const uint32_t sx = seen16(c);
+                        const float vx = __log2f(sv);
+                        ca_ld16(t_s + c, x);
+                        ca_ld16_wait(x);
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) {
+                        for (int i = 0; i < 16; ++i)
                             if ((sx >> i) & 1u) mx = fmaxf(mx, fmaf(x[i], kx, vx));
-                            if ((sy >> i) & 1u) mx = fmaxf(mx, fmaf(y[i], ky, vy));
-                        }
-                    } else {
-                        float a = -INFINITY, b = -INFINITY;
-#pragma unroll
-                        for (int i = 0; i < 16; i += 2) {
-                            a = fmaxf(a, fmaxf(fmaf(x[i], kx, vx), fmaf(x[i + 1], kx, vx)));
-                            b = fmaxf(b, fmaxf(fmaf(y[i], ky, vy), fmaf(y[i + 1], ky, vy)));
-                        }
-                        mx = fmaxf(mx, fmaxf(a, b));
+                    }
+                } else {
+                    ca_ld16(t_s, x);
+#pragma unroll 1
+                    for (int c = 0; c < kCaTile; c += 32) {
+                        ca_ld16_wait(x);
+                        ca_ld16(t_s + c + 16, y);
+                        max16(c, x);
+                        ca_ld16_wait(y);
+                        ca_ld16(t_s + ((c + 32) & (kCaTile - 1)), x);   // in the end: the first tokens, for pass 2
+                        max16(c + 16, y);
                     }
                 }
                 // The product of this team's last tile is done: its P may be overwritten, and the accumulator has taken the
@@ -505,36 +518,57 @@ cache_attention_rows_kernel(const __grid_constant__ CUtensorMap tm_k, const __gr
                 const float m8 = mx == -INFINITY ? 0.f : 8.f - mx;
                 // pass 2: probabilities (scaled by 2^8), their sum, their two e4m3 terms
                 float sum = 0.f;
-#pragma unroll 1
-                for (int c = 0; c < kCaTile; c += 16) {
-                    float x[16];
-                    ca_ld16(t_s + c, x);
-                    const float kx = sc[c >> p.bt_log2][0] * cr, sv = fmaxf(sc[c >> p.bt_log2][1], 5.421010862e-20f);
-                    const float vx = __log2f(sv) + m8;
-                    ca_ld16_wait(x);
-                    float s0 = 0.f, s1 = 0.f;
-                    if (masked) {
-                        uint32_t sx = seen16(c);
-                        asm volatile("" : "+r"(sx));
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) x[i] = (sx >> i) & 1u ? ex2(fmaf(x[i], kx, vx)) : 0.f;
-                        // blocks behind the sequence have no scale
-                        if (sx)
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) s0 += x[i];
-                        if (sx) sum = fmaf(s0, __fdividef(1.f, sv), sum);
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) x[i] = ex2(fmaf(x[i], kx, vx));
-#pragma unroll
-                        for (int i = 0; i < 16; i += 2) { s0 += x[i]; s1 += x[i + 1]; }
-                        sum = fmaf(s0 + s1, __fdividef(1.f, sv), sum);
-                    }
+                auto split16 = [&](int c, const float (&x)[16]) {   // x: probabilities
                     uint32_t hi[4], lo[4];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) ca_split4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3], hi[i], lo[i]);
                     *reinterpret_cast<uint4*>(sp + (c >> 4) * 128) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
                     *reinterpret_cast<uint4*>(sp + (c >> 4) * 128 + L::kPBytes) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+                };
+                auto prob16 = [&](int c, float (&x)[16]) {
+                    float kx, sv;
+                    scales16(c, kx, sv);
+                    const float vx = __log2f(sv) + m8;
+                    float s0 = 0.f, s1 = 0.f, s2 = 0.f, s3 = 0.f;
+#pragma unroll
+                    for (int i = 0; i < 16; i += 4) {
+                        x[i] = ex2(fmaf(x[i], kx, vx));
+                        x[i + 1] = ex2(fmaf(x[i + 1], kx, vx));
+                        x[i + 2] = ex2(fmaf(x[i + 2], kx, vx));
+                        x[i + 3] = ex2(fmaf(x[i + 3], kx, vx));
+                        s0 += x[i]; s1 += x[i + 1]; s2 += x[i + 2]; s3 += x[i + 3];
+                    }
+                    sum = fmaf((s0 + s1) + (s2 + s3), __fdividef(1.f, sv), sum);
+                    split16(c, x);
+                };
+                if (masked) {
+#pragma unroll 1
+                    for (int c = 0; c < kCaTile; c += 16) {
+                        float kx, sv, s0 = 0.f;
+                        scales16(c, kx, sv);
+                        const uint32_t sx = seen16(c);
+                        const float vx = __log2f(sv) + m8;
+                        ca_ld16(t_s + c, x);
+                        ca_ld16_wait(x);
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            x[i] = (sx >> i) & 1u ? ex2(fmaf(x[i], kx, vx)) : 0.f;
+                            s0 += x[i];
+                        }
+                        if (sx) sum = fmaf(s0, __fdividef(1.f, sv), sum);   // blocks behind the sequence have no scale
+                        split16(c, x);
+                    }
+                } else {
+#pragma unroll 1
+                    for (int c = 0; c < kCaTile; c += 32) {
+                        ca_ld16_wait(x);
+                        ca_ld16(t_s + c + 16, y);
+                        prob16(c, x);
+                        ca_ld16_wait(y);
+                        ca_ld16(t_s + ((c + 32) & (kCaTile - 1)), x);
+                        prob16(c + 16, y);
+                    }
+                    ca_ld16_wait(x);
                 }
                 l_run = fmaf(l_run, fa, sum * fb);
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");

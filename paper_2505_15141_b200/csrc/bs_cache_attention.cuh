@@ -459,33 +459,26 @@ __device__ __forceinline__ void ca_queries(const CacheAttnParams& p, CaCursor cu
 #pragma unroll
             for (int z = 0; z < kBatch; ++z) {
                 const int r = rb + z * kRows + sub;
+                // the row's largest magnitude, two bf16 at a time: their bits order as whole numbers do
+                uint32_t m2 = __vmaxu2(__vmaxu2(raw[z].x & 0x7fff7fffu, raw[z].y & 0x7fff7fffu),
+                                       __vmaxu2(raw[z].z & 0x7fff7fffu, raw[z].w & 0x7fff7fffu));
+#pragma unroll
+                for (int o = kLanes / 2; o > 0; o >>= 1) m2 = __vmaxu2(m2, __shfl_xor_sync(0xffffffffu, m2, o));
+                const uint32_t mx = max(m2 >> 16, m2 & 0xffffu);
+                const bool fin = mx < 0x7f80u;                // no infinity, no NaN
+                // 2^x brings the row's largest element into [128, 256)
+                const int x = mx && fin ? min(7 - ((int)(mx >> 7) - 127), 120) : 0;
+                const float up = __uint_as_float((uint32_t)(x + 127) << 23);
                 float f[8];
                 Elem<__nv_bfloat16>::unpack(raw[z], f);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) f[e] = r < rows ? f[e] : 0.f;
-                float mx = 0.f;
-                bool fin = true;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    mx = fmaxf(mx, fabsf(f[e]));
-                    fin = fin && fabsf(f[e]) <= 3.402823466e38f;
-                }
-#pragma unroll
-                for (int o = kLanes / 2; o > 0; o >>= 1) {
-                    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-                    fin = __shfl_xor_sync(0xffffffffu, (int)fin, o) && fin;
-                }
-                // 2^x brings the row's largest element into [128, 256)
-                int x = mx > 0.f && fin ? 7 - ((int)(__float_as_uint(mx) >> 23) - 127) : 0;
-                x = min(x, 120);
-                const float up = __uint_as_float((uint32_t)(x + 127) << 23);
                 uint2 hi, lo;
                 ca_split4(f[0] * up, f[1] * up, f[2] * up, f[3] * up, hi.x, lo.x);
                 ca_split4(f[4] * up, f[5] * up, f[6] * up, f[7] * up, hi.y, lo.y);
                 unsigned char* at = q_hi + (r >> 3) * (8 * D) + (piece >> 4) * 128 + (r & 7) * 16 + (piece & 15);
                 *reinterpret_cast<uint2*>(at) = hi;
                 *reinterpret_cast<uint2*>(at + ROWS * D) = lo;
-                // a row with an infinity or a NaN has no softmax: its scale makes every result NaN
+                // a row with an infinity or a NaN has no softmax: its scale makes every result NaN.  (Rows behind the item's
+                // last repeat it; nobody reads their results.)
                 if (piece == 0)
                     s_c[buf][r] = r >= rows ? 0.f : fin ? p.scale_log2 * __uint_as_float((uint32_t)(127 - x) << 23) : __int_as_float(0x7fc00000);
             }

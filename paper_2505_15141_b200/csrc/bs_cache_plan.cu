@@ -6,15 +6,12 @@
 // (counted over the sequences, ascending within one) becomes the (j + 1)-th from the top; then the j-th missing
 // block is the (j + 1)-th from the top.  A round that is planned and given back whole leaves the stack as it was.
 //
-// Everything is prefix sums over the batch.  They are small (B <= 4096), so every CTA computes all of them; only
-// the writes are divided.  One launch: a CTA for an ordinary round, a cluster of eight when there are many
-// slots to write, whose cluster barriers order "all have read the state", "blocks returned", "blocks taken".
+// Everything is prefix sums over the batch, which is small (B <= 4096): one CTA.  It also writes the slots of an ordinary
+// round; a large slot map (prompts) is written by a second launch over many CTAs from the finished tables.  Bound by
+// latency: a handful of dependent loads and block-wide scans.
 #include "bs_common.cuh"
 
 #include <atomic>
-#include <cooperative_groups.h>
-
-namespace cg = cooperative_groups;
 
 namespace bs {
 
@@ -33,12 +30,13 @@ struct CachePlanParams {
     int32_t* positions;        // [T] or NULL
     int32_t* status;           // [B] or NULL
     int extra, bt_log2, B, W, n_blocks, T;
+    int inline_slots;          // slot_map and positions are written here
 };
 
 constexpr int kPlanThreads = 1024;
-constexpr int kPlanCluster = 8;
-// Slots that one CTA writes; larger maps are shared by the CTAs of a cluster.
-constexpr int kPlanSlotsPerCta = 8192;
+constexpr int kSlotThreads = 256;
+// Slots that the planning CTA writes itself; larger maps take a launch of their own.
+constexpr int kPlanSlotsInline = 8192;
 
 // Inclusive prefix sum over the CTA's threads of a pair of counts; `total` is the sum over all of them.
 __device__ __forceinline__ longlong2 plan_scan(longlong2 v, longlong2* s_w, longlong2& total) {
@@ -74,9 +72,7 @@ __global__ void __launch_bounds__(kPlanThreads) cache_plan_kernel(const CachePla
     int32_t* s_delta = s_rank + p.B;                   // [B] blocks taken (> 0) or returned (< 0)
     int32_t* s_new = s_delta + p.B;                    // [B] new tokens granted
     int32_t* s_bits = s_new + p.B;                     // [B] status bits
-    cg::cluster_group cluster = cg::this_cluster();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int rank = (int)cluster.block_rank(), ncta = (int)cluster.num_blocks();
     const int bt = 1 << p.bt_log2;
     pdl_enter();
 
@@ -138,10 +134,10 @@ __global__ void __launch_bounds__(kPlanThreads) cache_plan_kernel(const CachePla
         taken += total.y;
     }
     if (tid == 0) s_cu[0] = 0;
-    cluster.sync();                                    // every CTA has read the state (and its own shared memory is complete)
+    __syncthreads();
 
     // ---- per-sequence results; surplus blocks go back ----
-    for (int b = rank * kPlanThreads + tid; b < p.B; b += ncta * kPlanThreads) {
+    for (int b = tid; b < p.B; b += kPlanThreads) {
         const int bits = s_bits[b];
         if (!(bits & BS_DEV_BAD_LENGTH)) p.seq_len[b] = s_len[b];
         p.n_held[b] = s_held[b] + s_delta[b];
@@ -149,13 +145,13 @@ __global__ void __launch_bounds__(kPlanThreads) cache_plan_kernel(const CachePla
         p.cu_new[b + 1] = s_cu[b + 1];
         if (p.status) p.status[b] = bits;
     }
-    if (rank == 0 && tid == 0) {
+    if (tid == 0) {
         p.cu_new[0] = 0;
         *p.n_free = (int)(avail - taken);
     }
     const int top = (int)avail;
     if (returned) {
-        for (int b = rank * 32 + warp; b < p.B; b += ncta * 32) {
+        for (int b = warp; b < p.B; b += kPlanThreads / 32) {
             const int give = -s_delta[b];
             for (int j = lane; j < give; j += 32) {
                 int32_t* e = p.block_table + (size_t)b * p.W + (s_held[b] - give + j);
@@ -164,11 +160,11 @@ __global__ void __launch_bounds__(kPlanThreads) cache_plan_kernel(const CachePla
                 *e = -1;
             }
         }
-        cluster.sync();
+        __syncthreads();
     }
     // ---- missing blocks are taken ----
     if (taken) {
-        for (int b = rank * 32 + warp; b < p.B; b += ncta * 32) {
+        for (int b = warp; b < p.B; b += kPlanThreads / 32) {
             const int take = s_delta[b];
             for (int j = lane; j < take; j += 32) {
                 const int at = top - 1 - (s_rank[b] + j);
@@ -178,9 +174,10 @@ __global__ void __launch_bounds__(kPlanThreads) cache_plan_kernel(const CachePla
     }
     // ---- slots: a token's block is in the table from before, or the one taken above (read from the stack, where
     //      nobody writes any more) ----
+    if (!p.inline_slots) return;
     const int T_new = s_cu[p.B];
     int b = 0;
-    for (int i = rank * kPlanThreads + tid; i < p.T; i += ncta * kPlanThreads) {
+    for (int i = tid; i < p.T; i += kPlanThreads) {
         int slot = -1, pos = -1;
         if (i < T_new) {
             int lo = b, hi = p.B;                      // the last sequence with s_cu[b] <= i; i only grows
@@ -199,6 +196,38 @@ __global__ void __launch_bounds__(kPlanThreads) cache_plan_kernel(const CachePla
                 blk = at < p.n_blocks ? __ldcg(p.free_blocks + at) : -1;
             }
             if (blk >= 0 && blk < p.n_blocks) slot = (blk << p.bt_log2) + (pos & (bt - 1));
+        }
+        p.slot_map[i] = slot;
+        if (p.positions) p.positions[i] = pos;
+    }
+}
+
+// The slots of a large map, from what cache_plan_kernel wrote: a warp takes 128 tokens, whose sequences lie close together.
+__global__ void __launch_bounds__(kSlotThreads) cache_slots_kernel(const CachePlanParams p) {
+    pdl_enter();
+    const int T_new = __ldcg(p.cu_new + p.B);
+    const int lane = threadIdx.x & 31;
+    const int first = (blockIdx.x * (kSlotThreads / 32) + (threadIdx.x >> 5)) * 128;
+    int b = 0, from = 0, to = 0;                       // tokens of the sequence looked up last
+#pragma unroll 1
+    for (int q = 0; q < 4; ++q) {
+        const int i = first + q * 32 + lane;
+        if (i >= p.T) break;
+        int slot = -1, pos = -1;
+        if (i < T_new) {
+            if (i >= to) {
+                int lo = b, hi = p.B;                  // the last sequence with cu_new[b] <= i
+                while (hi - lo > 1) {
+                    const int mid = (lo + hi) >> 1;
+                    if (__ldcg(p.cu_new + mid) <= i) lo = mid; else hi = mid;
+                }
+                b = lo;
+                from = __ldcg(p.cu_new + b);
+                to = __ldcg(p.cu_new + b + 1);
+            }
+            pos = __ldcg(p.seq_len + b) + i - from;
+            const int blk = __ldcg(p.block_table + (size_t)b * p.W + (pos >> p.bt_log2));
+            if (blk >= 0 && blk < p.n_blocks) slot = (blk << p.bt_log2) + (pos & ((1 << p.bt_log2) - 1));
         }
         p.slot_map[i] = slot;
         if (p.positions) p.positions[i] = pos;
@@ -241,19 +270,9 @@ extern "C" bs_status bs_cache_plan(int32_t* seq_len, const int32_t* kept, const 
             return cuda_status(cudaGetLastError());
         g_plan_attr[dev] = true;
     }
-    const int ncta = T > kPlanSlotsPerCta ? kPlanCluster : 1;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = ncta;
-    cfg.blockDim = kPlanThreads;
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = static_cast<cudaStream_t>(stream);
-    cudaLaunchAttribute at[2];
-    at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim.x = ncta;
-    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
-    at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[1].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = at;
-    cfg.numAttrs = 2;
-    return cuda_status(cudaLaunchKernelEx(&cfg, cache_plan_kernel, p));
+    p.inline_slots = T <= kPlanSlotsInline;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const cudaError_t e = launch_pdl(cache_plan_kernel, 1, kPlanThreads, smem, st, p);
+    if (e != cudaSuccess || p.inline_slots) return cuda_status(e);
+    return cuda_status(launch_pdl(cache_slots_kernel, (unsigned)(((long long)T + 1023) / 1024), kSlotThreads, 0, st, p));
 }

@@ -49,7 +49,7 @@ template <> struct Raw8<float> {
 // block needs), so the input is read once: maximum, scale, codes.  Bound by HBM on prompts, by latency on a round.  The
 // loads of a run are unconditional (tokens behind it repeat its last one) so that all of them are in flight at once.
 template <typename T, int D>
-__global__ void __launch_bounds__(kApThreads) cache_append_kernel(const CacheAppendParams p) {
+__global__ void __launch_bounds__(kApThreads, sizeof(T) == 2 ? 3 : 2) cache_append_kernel(const CacheAppendParams p) {
     constexpr int kLanes = D / 8;                             // lanes that hold a token
     constexpr int kPer = 32 / kLanes;                         // tokens per warp and step
     __shared__ float s_max[2][kApThreads / 32];

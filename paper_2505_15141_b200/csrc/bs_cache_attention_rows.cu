@@ -19,6 +19,24 @@
 
 namespace bs {
 
+// Pairs of fp32 in one instruction.
+__device__ __forceinline__ uint64_t pk(float lo, float hi) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ void upk(uint64_t v, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+
 template <int R, int D> struct CrLayout {
     static constexpr int kTeamWarps = R / 32;                 // warps of a team = of a tile
     static constexpr int kTeams = 2;                          // tiles in flight
@@ -63,6 +81,7 @@ cache_attention_rows_kernel(const __grid_constant__ CUtensorMap tm_k, const __gr
     __shared__ uint32_t s_anc[2][32];                         // per query buffer: ancestors of the tree's nodes
     __shared__ float s_mt[2][2][R];                           // maxima of a team's tiles, for the accumulator
     __shared__ float2 s_ml[2][2][R];                          // per item parity and team: running maximum and sum
+    __shared__ __align__(16) float4 s_tab[L::kSoft][8];       // per softmax warp: scale of K, log2 and inverse of that of V, by 16 tokens
     __shared__ float2 s_hl[R];                                // merge: maximum and sum of the second half
     __shared__ __align__(8) float s_scale[kCaScaleRing][kCaMaxPages][2];
     __shared__ uint32_t s_nan[2][R][D / 32];                  // per item parity: results a NaN of a masked tile of V belongs to
@@ -442,6 +461,13 @@ cache_attention_rows_kernel(const __grid_constant__ CUtensorMap tm_k, const __gr
                             s_nan_any[buf] = 1;
                     }
                 }
+                if (lane < 8) {
+                    const float* z = s_scale[k % kCaScaleRing][(lane * 16) >> p.bt_log2];
+                    const float sv = fmaxf(z[1], 5.421010862e-20f);   // 2^-64
+                    s_tab[warp - 8][lane] = make_float4(z[0], __log2f(sv), __fdividef(1.f, sv), 0.f);
+                }
+                __syncwarp();
+                const float4* tab = s_tab[warp - 8];
                 ok = ca_wait(smem_u32(&b_s[u]), kk & 1);
                 if (!ok) break;
                 tc_fence_after();
@@ -458,33 +484,27 @@ cache_attention_rows_kernel(const __grid_constant__ CUtensorMap tm_k, const __gr
                     }
                     return v;
                 };
-                const float (*sc)[2] = s_scale[k % kCaScaleRing];
                 // pass 1: the row's maximum of t + log2(scale of V).  Tiles without a mask, nearly all of them, have short
                 // loops of their own; their tensor-memory loads run 16 tokens ahead.
                 float mx = -INFINITY;
-                auto scales16 = [&](int c, float& kx, float& sv) {
-                    const float2 z = *reinterpret_cast<const float2*>(sc[c >> p.bt_log2]);
-                    kx = z.x * cr;
-                    sv = fmaxf(z.y, 5.421010862e-20f);        // 2^-64
-                };
-                auto max16 = [&](int c, const float (&x)[16]) {
-                    float kx, sv, a[4];
-                    scales16(c, kx, sv);
-                    const float vx = __log2f(sv);
+                auto max16 = [&](const float4 z, const float (&x)[16]) {
+                    const uint64_t kx2 = pk(z.x * cr, z.x * cr), vx2 = pk(z.y, z.y);
+                    float a[4];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        a[i] = fmaxf(fmaxf(fmaf(x[4 * i], kx, vx), fmaf(x[4 * i + 1], kx, vx)),
-                                     fmaxf(fmaf(x[4 * i + 2], kx, vx), fmaf(x[4 * i + 3], kx, vx)));
+                    for (int i = 0; i < 4; ++i) {
+                        float q0, q1, q2, q3;
+                        upk(fma2(pk(x[4 * i], x[4 * i + 1]), kx2, vx2), q0, q1);
+                        upk(fma2(pk(x[4 * i + 2], x[4 * i + 3]), kx2, vx2), q2, q3);
+                        a[i] = fmaxf(fmaxf(q0, q1), fmaxf(q2, q3));
+                    }
                     mx = fmaxf(mx, fmaxf(fmaxf(a[0], a[1]), fmaxf(a[2], a[3])));
                 };
                 float x[16], y[16];
                 if (masked) {
 #pragma unroll 1
                     for (int c = 0; c < kCaTile; c += 16) {
-                        float kx, sv;
-                        scales16(c, kx, sv);
                         const uint32_t sx = seen16(c);
-                        const float vx = __log2f(sv);
+                        const float kx = tab[c >> 4].x * cr, vx = tab[c >> 4].y;
                         ca_ld16(t_s + c, x);
                         ca_ld16_wait(x);
 #pragma unroll
@@ -495,12 +515,13 @@ cache_attention_rows_kernel(const __grid_constant__ CUtensorMap tm_k, const __gr
                     ca_ld16(t_s, x);
 #pragma unroll 1
                     for (int c = 0; c < kCaTile; c += 32) {
+                        const float4 z0 = tab[c >> 4], z1 = tab[(c >> 4) + 1];
                         ca_ld16_wait(x);
                         ca_ld16(t_s + c + 16, y);
-                        max16(c, x);
+                        max16(z0, x);
                         ca_ld16_wait(y);
                         ca_ld16(t_s + ((c + 32) & (kCaTile - 1)), x);   // in the end: the first tokens, for pass 2
-                        max16(c + 16, y);
+                        max16(z1, y);
                     }
                 }
                 // The product of this team's last tile is done: its P may be overwritten, and the accumulator has taken the
@@ -525,29 +546,29 @@ cache_attention_rows_kernel(const __grid_constant__ CUtensorMap tm_k, const __gr
                     *reinterpret_cast<uint4*>(sp + (c >> 4) * 128) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
                     *reinterpret_cast<uint4*>(sp + (c >> 4) * 128 + L::kPBytes) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
                 };
-                auto prob16 = [&](int c, float (&x)[16]) {
-                    float kx, sv;
-                    scales16(c, kx, sv);
-                    const float vx = __log2f(sv) + m8;
-                    float s0 = 0.f, s1 = 0.f, s2 = 0.f, s3 = 0.f;
+                auto prob16 = [&](int c, const float4 z, float (&x)[16]) {
+                    const uint64_t kx2 = pk(z.x * cr, z.x * cr), vx2 = pk(z.y + m8, z.y + m8);
+                    uint64_t sa = 0ull, sb = 0ull;
 #pragma unroll
                     for (int i = 0; i < 16; i += 4) {
-                        x[i] = ex2(fmaf(x[i], kx, vx));
-                        x[i + 1] = ex2(fmaf(x[i + 1], kx, vx));
-                        x[i + 2] = ex2(fmaf(x[i + 2], kx, vx));
-                        x[i + 3] = ex2(fmaf(x[i + 3], kx, vx));
-                        s0 += x[i]; s1 += x[i + 1]; s2 += x[i + 2]; s3 += x[i + 3];
+                        upk(fma2(pk(x[i], x[i + 1]), kx2, vx2), x[i], x[i + 1]);
+                        upk(fma2(pk(x[i + 2], x[i + 3]), kx2, vx2), x[i + 2], x[i + 3]);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) x[i + e] = ex2(x[i + e]);
+                        sa = add2(sa, pk(x[i], x[i + 1]));
+                        sb = add2(sb, pk(x[i + 2], x[i + 3]));
                     }
-                    sum = fmaf((s0 + s1) + (s2 + s3), __fdividef(1.f, sv), sum);
+                    float s0, s1;
+                    upk(add2(sa, sb), s0, s1);
+                    sum = fmaf(s0 + s1, z.z, sum);
                     split16(c, x);
                 };
                 if (masked) {
 #pragma unroll 1
                     for (int c = 0; c < kCaTile; c += 16) {
-                        float kx, sv, s0 = 0.f;
-                        scales16(c, kx, sv);
+                        float s0 = 0.f;
                         const uint32_t sx = seen16(c);
-                        const float vx = __log2f(sv) + m8;
+                        const float kx = tab[c >> 4].x * cr, vx = tab[c >> 4].y + m8;
                         ca_ld16(t_s + c, x);
                         ca_ld16_wait(x);
 #pragma unroll
@@ -555,18 +576,19 @@ cache_attention_rows_kernel(const __grid_constant__ CUtensorMap tm_k, const __gr
                             x[i] = (sx >> i) & 1u ? ex2(fmaf(x[i], kx, vx)) : 0.f;
                             s0 += x[i];
                         }
-                        if (sx) sum = fmaf(s0, __fdividef(1.f, sv), sum);   // blocks behind the sequence have no scale
+                        if (sx) sum = fmaf(s0, tab[c >> 4].z, sum);   // blocks behind the sequence have no scale
                         split16(c, x);
                     }
                 } else {
 #pragma unroll 1
                     for (int c = 0; c < kCaTile; c += 32) {
+                        const float4 z0 = tab[c >> 4], z1 = tab[(c >> 4) + 1];
                         ca_ld16_wait(x);
                         ca_ld16(t_s + c + 16, y);
-                        prob16(c, x);
+                        prob16(c, z0, x);
                         ca_ld16_wait(y);
                         ca_ld16(t_s + ((c + 32) & (kCaTile - 1)), x);
-                        prob16(c + 16, y);
+                        prob16(c + 16, z1, y);
                     }
                     ca_ld16_wait(x);
                 }

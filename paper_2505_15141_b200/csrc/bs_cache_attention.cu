@@ -202,7 +202,20 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_co
         }
         __syncwarp();
     } else if (warp == 3) {
-        ca_queries<N, D>(p, cur, s_q, s_c, s_anc, b_qfull, b_qempty, &s_abort);
+        // ================================== queries ==================================
+        int item = 0;
+        bool ok = true;
+#pragma unroll 1
+        while (cur.x < cur.end && ok) {
+            const int buf = item & 1;
+            if (item >= 2) ok = ca_wait(smem_u32(&b_qempty[buf]), (uint32_t)(((item >> 1) - 1) & 1)) && !__any_sync(0xffffffffu, s_abort);
+            if (!ok) break;
+            ca_queries<N, D, 32>(p, cur, buf, lane, s_q, s_c, s_anc);
+            if (lane == 0) mbar_arrive(smem_u32(&b_qfull[buf]));
+            ++item;
+            ca_advance(p, cur, ca_tiles_here(cur));
+        }
+        if (!ok && lane == 0) ca_give_up(p, &s_abort);
     } else if (warp < 8) {
         // ================================ accumulator ================================
         // O^T of every tile into fp32 (tensor memory, 16 rows at a time in one short loop: code that does not fit the

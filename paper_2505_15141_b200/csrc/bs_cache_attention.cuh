@@ -426,27 +426,22 @@ __device__ __forceinline__ void ca_init_rings(unsigned long long (*b_full)[RING]
     for (int s = 0; s < kCaScaleRing; ++s) mbar_init(smem_u32(b_scale + s), 32);   // the producer's lanes
 }
 
-// ---- queries: a warp splits them into e4m3, an item ahead ----
-// Buffer i of shared memory: hi, then lo, ROWS x D bytes each, in 8 x 16-byte core matrices.
-template <int ROWS, int D>
-__device__ __forceinline__ void ca_queries(const CacheAttnParams& p, CaCursor cur, unsigned char* s_q, float (*s_c)[ROWS],
-                                           uint32_t (*s_anc)[32], unsigned long long* b_qfull, unsigned long long* b_qempty,
-                                           volatile int* s_abort) {
+// ---- queries, split into e4m3 an item ahead ----
+// Buffer i of shared memory: hi, then lo, ROWS x D bytes each, in 8 x 16-byte core matrices.  qt: 0 to THREADS - 1.
+// THREADS = 32: a warp of its own, for few rows.  128: the accumulator warps, before the item's first tile; for 64 rows a
+// warp of its own took 9 us, which every CTA waited for at its start and at short items.
+template <int ROWS, int D, int THREADS>
+__device__ __forceinline__ void ca_queries(const CacheAttnParams& p, const CaCursor& cur, int buf, int qt, unsigned char* s_q,
+                                           float (*s_c)[ROWS], uint32_t (*s_anc)[32]) {
     constexpr int kLanes = D / 8;                             // lanes of a row
-    constexpr int kRows = 32 / kLanes;                        // rows per pass
-    const int lane = threadIdx.x & 31, sub = lane / kLanes, piece = (lane % kLanes) * 8;
+    constexpr int kRows = THREADS / kLanes;                   // rows per pass
+    const int lane = qt & 31, sub = qt / kLanes, piece = (qt % kLanes) * 8;
     const int inv_g = (65536 + p.G - 1) / p.G;                // exact for r < 128, G <= 64
-    int item = 0;
-    bool ok = true;
-#pragma unroll 1
-    while (cur.x < cur.end && ok) {
-        const int buf = item & 1;
-        if (item >= 2) ok = ca_wait(smem_u32(b_qempty + buf), (uint32_t)(((item >> 1) - 1) & 1)) && !__any_sync(0xffffffffu, *s_abort);
-        if (!ok) break;
+    {
         const int i0 = cur.rt * p.TQ, rows = min(p.TQ, cur.n - i0) * p.G;
         unsigned char* q_hi = s_q + buf * 2 * (ROWS * D);
         // the loads of a batch of rows first: one by one, each would wait for memory (1400 cycles a pass, measured)
-        constexpr int kBatch = ROWS / kRows < 8 ? ROWS / kRows : 8;
+        constexpr int kBatch = ROWS <= kRows ? 1 : ROWS / kRows < 8 ? ROWS / kRows : 8;
 #pragma unroll 1
         for (int rb = 0; rb < ROWS; rb += kBatch * kRows) {
             uint4 raw[kBatch];
@@ -483,7 +478,7 @@ __device__ __forceinline__ void ca_queries(const CacheAttnParams& p, CaCursor cu
                     s_c[buf][r] = r >= rows ? 0.f : fin ? p.scale_log2 * __uint_as_float((uint32_t)(127 - x) << 23) : __int_as_float(0x7fc00000);
             }
         }
-        if (p.node_parent) {                       // ancestors-or-self of node `lane`
+        if (p.node_parent && qt < 32) {            // ancestors-or-self of node `lane`
             int par = 0;
             if (lane >= 1 && lane < cur.n) {
                 par = __ldg(p.node_parent + (size_t)cur.b * p.Nmax + lane - 1);
@@ -504,11 +499,7 @@ __device__ __forceinline__ void ca_queries(const CacheAttnParams& p, CaCursor cu
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
-        if (lane == 0) mbar_arrive(smem_u32(b_qfull + buf));
-        ++item;
-        ca_advance(p, cur, ca_tiles_here(cur));
     }
-    if (!ok && lane == 0) ca_give_up(p, s_abort);
 }
 
 // Many rows (bs_cache_attention_rows.cu); tm: K and V; TQ and G are set.

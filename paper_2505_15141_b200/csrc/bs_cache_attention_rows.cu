@@ -14,7 +14,7 @@
 //
 // Tensor memory: S of two tiles, O of one, the fp32 accumulator (O * 2^(m_tile - m) is added after every tile, as there).
 //
-// Warps: 0, 1 producers, 2 MMA issuer, 3 queries, 4-7 accumulator, then the softmax teams.
+// Warps: 0, 1 producers, 2 MMA issuer, 4-7 queries and accumulator, then the softmax teams.
 #include "bs_cache_attention.cuh"
 
 namespace bs {
@@ -95,7 +95,7 @@ cache_attention_rows_kernel(const __grid_constant__ CUtensorMap tm_k, const __gr
     if (tid == 0) {
         ca_init_rings<RING>(b_full, b_empty, b_scale);
         for (int a = 0; a < 2; ++a) {
-            mbar_init(smem_u32(&b_qfull[a]), 1);
+            mbar_init(smem_u32(&b_qfull[a]), 4);              // the accumulator warps
             mbar_init(smem_u32(&b_qempty[a]), 1 + L::kSoft);  // the MMAs and the softmax warps
             mbar_init(smem_u32(&b_s[a]), 1);
             mbar_init(smem_u32(&b_p[a]), TW);
@@ -128,7 +128,8 @@ cache_attention_rows_kernel(const __grid_constant__ CUtensorMap tm_k, const __gr
     } else if (warp == 2) {
         // ================================= MMA issuer =================================
         // S of tiles 0 and 1, then, whenever the probabilities of a tile are there: S of the tile two further on, whose
-        // place in tensor memory they have left, and O of the tile itself.
+        // place in tensor memory they have left, and O of the tile itself.  O goes first where S begins an item: the
+        // queries of that item are split when the accumulator has finished the item two before it, maybe with this very O.
         constexpr uint32_t id_s = (1u << 4) | ((uint32_t)(kCaTile >> 3) << 17) | (8u << 24);
         constexpr uint32_t id_o = (1u << 4) | (1u << 16) | ((uint32_t)(D >> 3) << 17) | (8u << 24);
         const uint32_t elected = ca_elect();
@@ -140,46 +141,51 @@ cache_attention_rows_kernel(const __grid_constant__ CUtensorMap tm_k, const __gr
         for (uint32_t j = 0; j < total + 2 && ok; ++j) {      // S of tile j, O of tile j - 2
             const uint32_t u = j & 1;
             if (j >= 2) ok = ca_wait(smem_u32(&b_p[u]), ((j >> 1) - 1) & 1);
-            if (ok && j < total) {
-                if (left == 0) {
-                    if (item >= 0) ca_advance(p, cur, ca_tiles_here(cur));
-                    ++item;
-                    left = ca_tiles_here(cur);
-                    ok = ca_wait(smem_u32(&b_qfull[item & 1]), (uint32_t)((item >> 1) & 1));
+            const bool s_first = left > 0;
+#pragma unroll 1
+            for (int turn = 0; turn < 2 && ok; ++turn) {
+                if ((turn == 0) == s_first) {
+                    if (j >= total) continue;
+                    if (left == 0) {
+                        if (item >= 0) ca_advance(p, cur, ca_tiles_here(cur));
+                        ++item;
+                        left = ca_tiles_here(cur);
+                        ok = ca_wait(smem_u32(&b_qfull[item & 1]), (uint32_t)((item >> 1) & 1));
+                    }
+                    ok = ok && ca_wait(smem_u32(&b_full[0][ks]), kph) && !__any_sync(0xffffffffu, s_abort);
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint64_t dk = ca_desc(smem_u32(smem + ks * L::kTileBytes), 16, 8 * D, kSw);
+                    const uint64_t dq = ca_desc(smem_u32(s_q + (item & 1) * 2 * L::kQBytes) - (L::kHalves > 1 && u ? R * D : 0), 128, 8 * D, 0);
+#pragma unroll
+                    for (int term = 0; term < 2; ++term)
+#pragma unroll
+                        for (int s = 0; s < D / 32; ++s)
+                            ca_mma(tmem + u * 128, dq + ((term * L::kQBytes + s * 256) >> 4), dk + ((s * 32) >> 4), id_s, (term | s) ? 1u : 0u, elected);
+                    ca_commit(smem_u32(&b_s[u]), elected);
+                    ca_commit(smem_u32(&b_empty[0][ks]), elected);
+                    if (--left == 0) ca_commit(smem_u32(&b_qempty[item & 1]), elected);
+                    if (++ks == RING) { ks = 0; kph ^= 1u; }
+                } else {
+                    if (j < 2) continue;
+                    const uint32_t k = j - 2;
+                    if (!ca_wait(smem_u32(&b_full[1][vs]), vph) || (k >= 1 && !ca_wait(smem_u32(&b_ofree[u ^ 1]), ((k - 1) >> 1) & 1)) ||
+                        __any_sync(0xffffffffu, s_abort)) {
+                        ok = false;
+                        break;
+                    }
+                    tc_fence_after();
+                    const uint64_t dv = ca_desc(smem_u32(smem + (RING + vs) * L::kTileBytes), 0, 8 * D, kSw);
+                    const uint64_t dp = ca_desc(smem_u32(s_p + (L::kPBufs > 1 ? u * 2 * L::kPBytes : 0)), 128, 1024, 0);
+#pragma unroll
+                    for (int term = 0; term < 2; ++term)
+#pragma unroll
+                        for (int s = 0; s < kCaTile / 32; ++s)
+                            ca_mma(tmem + L::kColO, dp + ((term * L::kPBytes + s * 256) >> 4), dv + ((s * 32 * D) >> 4), id_o, (term | s) ? 1u : 0u, elected);
+                    ca_commit(smem_u32(&b_o[u]), elected);
+                    ca_commit(smem_u32(&b_empty[1][vs]), elected);
+                    if (++vs == RING) { vs = 0; vph ^= 1u; }
                 }
-                ok = ok && ca_wait(smem_u32(&b_full[0][ks]), kph) && !__any_sync(0xffffffffu, s_abort);
-                if (!ok) break;
-                tc_fence_after();
-                const uint64_t dk = ca_desc(smem_u32(smem + ks * L::kTileBytes), 16, 8 * D, kSw);
-                const uint64_t dq = ca_desc(smem_u32(s_q + (item & 1) * 2 * L::kQBytes) - (L::kHalves > 1 && u ? R * D : 0), 128, 8 * D, 0);
-#pragma unroll
-                for (int term = 0; term < 2; ++term)
-#pragma unroll
-                    for (int s = 0; s < D / 32; ++s)
-                        ca_mma(tmem + u * 128, dq + ((term * L::kQBytes + s * 256) >> 4), dk + ((s * 32) >> 4), id_s, (term | s) ? 1u : 0u, elected);
-                ca_commit(smem_u32(&b_s[u]), elected);
-                ca_commit(smem_u32(&b_empty[0][ks]), elected);
-                if (--left == 0) ca_commit(smem_u32(&b_qempty[item & 1]), elected);
-                if (++ks == RING) { ks = 0; kph ^= 1u; }
-            }
-            if (ok && j >= 2) {
-                const uint32_t k = j - 2;
-                if (!ca_wait(smem_u32(&b_full[1][vs]), vph) || (k >= 1 && !ca_wait(smem_u32(&b_ofree[u ^ 1]), ((k - 1) >> 1) & 1)) ||
-                    __any_sync(0xffffffffu, s_abort)) {
-                    ok = false;
-                    break;
-                }
-                tc_fence_after();
-                const uint64_t dv = ca_desc(smem_u32(smem + (RING + vs) * L::kTileBytes), 0, 8 * D, kSw);
-                const uint64_t dp = ca_desc(smem_u32(s_p + (L::kPBufs > 1 ? u * 2 * L::kPBytes : 0)), 128, 1024, 0);
-#pragma unroll
-                for (int term = 0; term < 2; ++term)
-#pragma unroll
-                    for (int s = 0; s < kCaTile / 32; ++s)
-                        ca_mma(tmem + L::kColO, dp + ((term * L::kPBytes + s * 256) >> 4), dv + ((s * 32 * D) >> 4), id_o, (term | s) ? 1u : 0u, elected);
-                ca_commit(smem_u32(&b_o[u]), elected);
-                ca_commit(smem_u32(&b_empty[1][vs]), elected);
-                if (++vs == RING) { vs = 0; vph ^= 1u; }
             }
         }
         if (!ok) {
@@ -190,7 +196,7 @@ cache_attention_rows_kernel(const __grid_constant__ CUtensorMap tm_k, const __gr
         }
         __syncwarp();
     } else if (warp == 3) {
-        ca_queries<R, D>(p, cur, s_q, s_c, s_anc, b_qfull, b_qempty, &s_abort);
+        // nothing: warps 4-7 have to be the four quarters of tensor memory
     } else if (warp < 8) {
         // ================================ accumulator ================================
         const int wq = warp & 3;                              // lane quarter of tensor memory
@@ -200,11 +206,26 @@ cache_attention_rows_kernel(const __grid_constant__ CUtensorMap tm_k, const __gr
         uint32_t k = 0;                                       // running tile number
         int item = 0;
         bool ok = true;
+        CaCursor qc = cur;                                    // the queries are an item ahead
+        int q_item = 0;
+        auto queries = [&]() {
+            if (qc.x >= qc.end || !ok) return;
+            const int qb = q_item & 1;
+            // the products and the constants of the item that had this buffer are done with: its tiles have been joined here
+            if (q_item >= 2) ok = ca_wait(smem_u32(&b_qempty[qb]), (uint32_t)(((q_item >> 1) - 1) & 1)) && !__any_sync(0xffffffffu, s_abort);
+            if (!ok) return;
+            ca_queries<R, D, 128>(p, qc, qb, wq * 32 + lane, s_q, s_c, s_anc);
+            if (lane == 0) mbar_arrive(smem_u32(&b_qfull[qb]));
+            ++q_item;
+            ca_advance(p, qc, ca_tiles_here(qc));
+        };
+        queries();
 #pragma unroll 1
         while (cur.x < cur.end) {
             const int buf = item & 1;
             const int nt = ca_tiles_here(cur);
             const int i0 = cur.rt * p.TQ, rows = min(p.TQ, cur.n - i0) * p.G;
+            queries();
             float m_run = -INFINITY;
             bool have = false;                                // the accumulator holds something
 #pragma unroll 1
@@ -336,7 +357,7 @@ cache_attention_rows_kernel(const __grid_constant__ CUtensorMap tm_k, const __gr
                 }
                 ca_bar_any(1, 128, false);
                 write = joined = s_last != 0;                 // written again only after a further barrier of the group
-                if (joined && leads) {
+                if (joined) {
                     __threadfence();
                     float mm = -INFINITY, ll = 0.f;
 #pragma unroll 4
@@ -351,33 +372,10 @@ cache_attention_rows_kernel(const __grid_constant__ CUtensorMap tm_k, const __gr
                     l_run = ll;
                 }
             }
-            if (write && leads) {
+            if (write && (joined || leads)) {
                 const float inv = l_run == 0.f ? 0.f : 1.f / l_run;   // nothing seen: zeros
                 __nv_bfloat16* o = p.out + (long long)(cur.q0 + i0 + row / p.G) * p.o_st + (long long)(cur.h * p.G + row % p.G) * p.o_sh;
-#pragma unroll 1
-                for (int c = 0; c < D; c += 16) {
-                    float y[16];
-                    if (!joined) {
-                        acc16(c, y);
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) y[i] = 0.f;
-                        if (row < rows)
-#pragma unroll 2
-                            for (int z = c_first; z <= c_last; ++z) {
-                                const float* q = p.partial + ((size_t)z * 2 + (z == c_first ? 1 : 0)) * L::kPiece;
-                                const float mc = __ldcg(q + R * D + row);
-                                const float f = mc == -INFINITY ? 0.f : ex2(mc - m_run);
-#pragma unroll
-                                for (int i = 0; i < 16; i += 4) {
-                                    const float4 v = __ldcg(reinterpret_cast<const float4*>(q + row * D + c + i));
-                                    y[i] = fmaf(v.x, f, y[i]);
-                                    y[i + 1] = fmaf(v.y, f, y[i + 1]);
-                                    y[i + 2] = fmaf(v.z, f, y[i + 2]);
-                                    y[i + 3] = fmaf(v.w, f, y[i + 3]);
-                                }
-                            }
-                    }
+                auto put16 = [&](int c, const float (&y)[16]) {
                     if (row < rows) {
                         uint32_t w[8];
 #pragma unroll
@@ -387,6 +385,40 @@ cache_attention_rows_kernel(const __grid_constant__ CUtensorMap tm_k, const __gr
                         }
                         *reinterpret_cast<uint4*>(o + c) = make_uint4(w[0], w[1], w[2], w[3]);
                         *reinterpret_cast<uint4*>(o + c + 8) = make_uint4(w[4], w[5], w[6], w[7]);
+                    }
+                };
+                if (!joined) {
+#pragma unroll 1
+                    for (int c = 0; c < D; c += 16) {
+                        float y[16];
+                        acc16(c, y);
+                        put16(c, y);
+                    }
+                } else {                                      // each half of the warps takes its half of the elements
+                    constexpr int kPart = D / L::kHalves;
+#pragma unroll 1
+                    for (int c = half * kPart; c < (half + 1) * kPart; c += 16) {
+                        float y[16];
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) y[i] = 0.f;
+                        if (row < rows)
+#pragma unroll 4
+                            for (int z = c_first; z <= c_last; ++z) {
+                                const float* q = p.partial + ((size_t)z * 2 + (z == c_first ? 1 : 0)) * L::kPiece;
+                                const float mc = __ldcg(q + R * D + row);
+                                float4 v[4];
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) v[i] = __ldcg(reinterpret_cast<const float4*>(q + row * D + c) + i);
+                                const float f = mc == -INFINITY ? 0.f : ex2(mc - m_run);
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) {
+                                    y[4 * i] = fmaf(v[i].x, f, y[4 * i]);
+                                    y[4 * i + 1] = fmaf(v[i].y, f, y[4 * i + 1]);
+                                    y[4 * i + 2] = fmaf(v[i].z, f, y[4 * i + 2]);
+                                    y[4 * i + 3] = fmaf(v[i].w, f, y[4 * i + 3]);
+                                }
+                            }
+                        put16(c, y);
                     }
                 }
             }

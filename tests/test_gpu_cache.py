@@ -172,11 +172,30 @@ def test_piece_of_a_prompt(lib, G):
     c.check(c.run(lib))
 
 
-def test_split_over_many_ctas(lib):
+@pytest.mark.parametrize("max_new", [4, 5, 16, 32])
+def test_split_over_many_ctas(lib, max_new):
     c = Case(3, [20000], [5], 4, 1, 128, 64, q_mul=3.0)
-    c.check(c.run(lib))
+    c.check(c.run(lib, max_new=max_new))
     c = Case(4, [9000, 1, 5000], [2, 3, 1], 7, 1, 64, 16, q_mul=3.0)
-    c.check(c.run(lib))
+    c.check(c.run(lib, max_new=max_new))
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("G,new,max_new", [(2, [1, 3, 8], 8), (4, [8, 1, 5], 8), (8, [8, 3, 1], 8), (4, [16, 40, 3], 40)])
+def test_many_short_items(lib, d, G, new, max_new):
+    """Many more sequences than CTAs, a tile or two each: every CTA walks through a row of items, of the four tile widths."""
+    rng = np.random.default_rng(G)
+    B = 500
+    new = [new[b % 3] if b % 11 else 0 for b in range(B)]
+    ctx = rng.integers(0, 150, B).tolist()
+    c = Case(G, ctx, new, 2 * G, 2, d, 16, q_mul=2.0)
+    st = torch.zeros(B, dtype=torch.int32, device=DEV)
+    ws, dev = lib.new_cache_workspace(2 * G, 2, d, DEV), c.device()
+    out = c.run(lib, max_new=max_new, status=st, ws=ws, dev=dev)
+    assert not st.any()
+    c.check(out, seqs=[0, 1, 2, 3, 250, 251, 252, 497, 498, 499])
+    for _ in range(20):
+        assert torch.equal(c.run(lib, max_new=max_new, ws=ws, dev=dev), out)
 
 
 def _random_parents(rng, n, N):
@@ -215,24 +234,27 @@ def test_bad_trees_are_flagged_and_hang_under_the_root(lib):
     assert st.tolist() == [lib.BS_DEV_BAD_LENGTH] * 3
 
 
-def test_rows_that_see_nothing_are_zero(lib):
+@pytest.mark.parametrize("max_new", [4, 8, 16, 40])
+def test_rows_that_see_nothing_are_zero(lib, max_new):
     c = Case(8, [-3, 20, -9], [5, 2, 4], 8, 2, 128, 16)   # fewer cached tokens than new ones; none at all
-    out = c.run(lib)
+    out = c.run(lib, max_new=max_new)
     c.check(out)
     assert (out[:3] == 0).all() and (out[7:11] == 0).all()
 
 
-def test_nan_and_infinity_stay_with_those_who_see_them(lib):
-    c = Case(9, [100, 50], [6, 3], 8, 2, 128, 16)
+@pytest.mark.parametrize("max_new", [4, 8, 16, 40])     # tiles of 16, 32, 64 and 128 rows
+@pytest.mark.parametrize("d", [64, 128])
+def test_nan_and_infinity_stay_with_those_who_see_them(lib, d, max_new):
+    c = Case(9, [100, 50], [6, 3], 8, 2, d, 16)
     blk, off = c.table[0, 103 // 16], 103 % 16
     c.codes[1][blk, 1, off, 5] = 0x7F                     # V of new token 3 of sequence 0, head 1
-    c.codes[1][blk, 1, off, 77] = 0xFF
+    c.codes[1][blk, 1, off, 57] = 0xFF
     c.codes[0][c.table[0, 105 // 16], 0, 105 % 16, 3] = 0x7F   # K of its token 5, head 0
     c.q[c.cu[1] + 1, 2, 9] = float("inf")                 # a query of sequence 1
     c.q[c.cu[1] + 2, 7, 1] = float("nan")
-    out = c.run(lib).float().cpu().numpy()
+    out = c.run(lib, max_new=max_new).float().cpu().numpy()
     bad = np.zeros(out.shape, bool)
-    bad[3:6, 4:8, 5] = bad[3:6, 4:8, 77] = True
+    bad[3:6, 4:8, 5] = bad[3:6, 4:8, 57] = True
     bad[5, 0:4] = True
     bad[c.cu[1] + 1, 2] = bad[c.cu[1] + 2, 7] = True
     assert np.array_equal(np.isnan(out), bad)
@@ -244,8 +266,9 @@ def test_nan_and_infinity_stay_with_those_who_see_them(lib):
         assert (np.abs(out[seq] - want)[ok] <= (tol + 2.0 ** -8 * np.abs(want))[ok]).all()
 
 
+@pytest.mark.parametrize("max_new", [4, 16, 40])        # tokens as lanes, rows as lanes (64, 128)
 @pytest.mark.parametrize("kind", ["v_scales", "k_scales", "sharp", "flat", "tiny_q", "negative_scale"])
-def test_values_far_apart(lib, kind):
+def test_values_far_apart(lib, kind, max_new):
     c = Case(10, [400, 130], [4, 3], 8, 2, 128, 16, q_mul={"sharp": 40.0, "flat": 1e-3, "tiny_q": 1e-30}.get(kind, 2.0))
     rng = np.random.default_rng(0)
     if kind == "v_scales":                                # blocks 2^44 apart inside one tile, and a block of zeros
@@ -256,7 +279,7 @@ def test_values_far_apart(lib, kind):
         c.scales[0] = np.where(np.isnan(c.scales[0]), c.scales[0], 2.0 ** rng.integers(-20, -3, c.scales[0].shape)).astype(np.float32)
     if kind == "negative_scale":
         c.scale = -c.scale
-    c.check(c.run(lib))
+    c.check(c.run(lib, max_new=max_new))
 
 
 def test_strides_and_a_padded_batch(lib):
@@ -290,13 +313,14 @@ def test_bad_lengths_and_blocks_are_flagged(lib):
     assert st[1].item() == lib.BS_DEV_BAD_LENGTH
 
 
-def test_repeats_bit_for_bit_and_leaves_the_workspace_clear(lib):
+@pytest.mark.parametrize("max_new", [4, 8, 16, 32])
+def test_repeats_bit_for_bit_and_leaves_the_workspace_clear(lib, max_new):
     c = Case(13, [3000, 700, 1], [5, 9, 2], 8, 2, 128, 16, q_mul=2.0)
     ws, dev = lib.new_cache_workspace(8, 2, 128, DEV), c.device()
-    first = c.run(lib, ws=ws, dev=dev)
+    first = c.run(lib, ws=ws, dev=dev, max_new=max_new)
     c.check(first)
     for _ in range(200):
-        assert torch.equal(c.run(lib, ws=ws, dev=dev), first)
+        assert torch.equal(c.run(lib, ws=ws, dev=dev, max_new=max_new), first)
     assert not ws[:592].any()                             # arrival counters
 
 
@@ -521,7 +545,7 @@ def test_plan_rounds(lib, B, bt):
         kept = np.where(got > 0, rng.integers(0, 10, B) % np.maximum(got, 1) + 1, 0)
 
 
-def test_plan_prompts_in_a_cluster(lib):
+def test_plan_large_slot_maps(lib):
     rng = np.random.default_rng(5)
     p = Plan(rng, 90, 16, 200, 90 * 100, 0)
     new = rng.integers(0, 1500, 90)

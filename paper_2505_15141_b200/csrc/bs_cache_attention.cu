@@ -26,7 +26,7 @@
 // 4-7 accumulator (a thread is an element of d), 8-11 and 12-15 two softmax groups that take the tiles in turn, each with
 // its own maximum and sum (a thread is a token).
 //
-// Work.  Item = (sequence, key head, N rows).  All tiles of all items, in order, are cut into equal contiguous shares,
+// Work.  Item = (sequence, key head, N rows).  All items, in order, a few places and one for each tile, are cut into equal contiguous shares,
 // one per CTA, from the lengths on the device; an item that spans several CTAs is joined by the one that finishes
 // last, in the order of the shares (the result does not depend on who that is).
 #include "bs_cache_attention.cuh"
@@ -148,7 +148,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_co
         constexpr uint32_t id_s = (1u << 4) | ((uint32_t)(L::kCols >> 3) << 17) | ((uint32_t)(kCaTile >> 4) << 24);
         constexpr uint32_t id_o = (1u << 4) | (1u << 15) | (1u << 16) | ((uint32_t)(L::kCols >> 3) << 17) | ((uint32_t)(D >> 4) << 24);
         const uint32_t elected = ca_elect();
-        const uint32_t total = (uint32_t)(cur.end - cur.x);
+        uint32_t total = cur.x < cur.end ? 0xffff0000u : 0u;  // tiles of this CTA, known when its last item is through
         uint32_t ks = 0, kph = 0, vs = 0, vph = 0;            // places in the rings of K and V
         int item = -1, left = 0;                              // tiles of the item whose S is still to be issued
         bool ok = true;
@@ -159,11 +159,17 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_co
             if (ok && j < total) {
                 if (left == 0) {
                     if (item >= 0) ca_advance(p, cur, ca_tiles_here(cur));
-                    ++item;
-                    left = ca_tiles_here(cur);
-                    ok = ca_wait(smem_u32(&b_qfull[item & 1]), (uint32_t)((item >> 1) & 1));
+                    if (cur.x >= cur.end) {
+                        total = j;
+                    } else {
+                        ++item;
+                        left = ca_tiles_here(cur);
+                        ok = ca_wait(smem_u32(&b_qfull[item & 1]), (uint32_t)((item >> 1) & 1));
+                    }
                 }
-                ok = ok && ca_wait(smem_u32(&b_full[0][ks]), kph) && !__any_sync(0xffffffffu, s_abort);
+            }
+            if (ok && j < total) {
+                ok = ca_wait(smem_u32(&b_full[0][ks]), kph) && !__any_sync(0xffffffffu, s_abort);
                 if (!ok) break;
                 tc_fence_after();
                 const uint64_t dk = ca_desc(smem_u32(smem + ks * L::kTileBytes), 16, 8 * D, kSw);

@@ -15,6 +15,7 @@ constexpr int kCaSmem = 230400;                // of 232448 bytes a CTA may use
 constexpr int kCaScaleRing = 8;                // tiles whose scales are kept; more than the tiles in flight
 constexpr int kCaMaxPages = 8;                 // blocks of 16 tokens in a tile
 constexpr int kCaMaxRows = 128;                // rows of an item, at most
+constexpr int kCaItemCost = 2;                 // what an item costs besides its tiles (queries, joining, results), in tiles
 
 struct CacheAttnParams {
     const __nv_bfloat16* q;
@@ -39,7 +40,8 @@ struct CaCursor {
     int b, h, rt, nrt;                         // item
     int n, base, q0;                           // its sequence: new tokens, position of the first, its row
     int t, ntiles;                             // next tile, tiles of the item
-    long long x, end;                          // the same counted over all work; end of this CTA's share
+    // The work is a line: every item takes kCaItemCost places and then one for each tile.
+    long long x, end;                          // place of the next tile; end of this CTA's share
 };
 
 __device__ __forceinline__ int ca_limit(const CacheAttnParams& p, int base, int n, int rt) {   // tokens an item may see
@@ -60,7 +62,7 @@ __device__ __forceinline__ bool ca_seq(const CacheAttnParams& p, int b, int& n, 
 __device__ __forceinline__ long long ca_head_work(const CacheAttnParams& p, int n, int base) {
     long long w = 0;
 #pragma unroll 1
-    for (int rt = 0; rt * p.TQ < n; ++rt) w += ca_tiles(ca_limit(p, base, n, rt));
+    for (int rt = 0; rt * p.TQ < n; ++rt) w += kCaItemCost + ca_tiles(ca_limit(p, base, n, rt));
     return w;
 }
 __device__ __forceinline__ void ca_item(const CacheAttnParams& p, CaCursor& c) {
@@ -69,6 +71,7 @@ __device__ __forceinline__ void ca_item(const CacheAttnParams& p, CaCursor& c) {
 // To the next item (c.t = 0).
 __device__ __forceinline__ void ca_next(const CacheAttnParams& p, CaCursor& c) {
     c.t = 0;
+    c.x += kCaItemCost;
     if (++c.rt == c.nrt) {
         c.rt = 0;
         if (++c.h == p.Hkv) {
@@ -260,7 +263,7 @@ struct CaShare {                               // shared memory
     int b;
 };
 struct CaPart {
-    long long work, grid;                      // tiles of all items, CTAs that have a share
+    long long work, grid;                      // length of the line of work, CTAs that have a share of it
 };
 // All threads of the CTA, after the grid dependency; ends with a barrier of all of them.
 template <int THREADS>
@@ -291,8 +294,8 @@ __device__ __forceinline__ CaPart ca_share(const CacheAttnParams& p, CaShare& sh
         if (w < warp) before += sh.w[w];
         work += sh.w[w];
     }
-    // two tiles at least for a CTA: they are worked on side by side, and a short item is not cut for nothing
-    const long long grid = min((work + 1) / 2, (long long)gridDim.x);
+    // an item of two tiles at least for a CTA: they are worked on side by side, and a short item is not cut for nothing
+    const long long grid = min((work + kCaItemCost + 1) / (kCaItemCost + 2), (long long)gridDim.x);
     const long long x_lo = grid ? blockIdx.x * work / grid : 0, x_hi = grid && blockIdx.x < grid ? (blockIdx.x + 1) * work / grid : 0;
     const long long from = before + incl - mine;
     if (x_lo < x_hi && x_lo >= from && x_lo < from + mine) {
@@ -322,12 +325,13 @@ __device__ __forceinline__ CaPart ca_share(const CacheAttnParams& p, CaShare& sh
         long long off = sh.off - cur.h * hw;
         cur.rt = 0;
         ca_item(p, cur);
-        while (off >= cur.ntiles) {
-            off -= cur.ntiles;
+        while (off >= kCaItemCost + cur.ntiles) {
+            off -= kCaItemCost + cur.ntiles;
             ++cur.rt;
             ca_item(p, cur);
         }
-        cur.t = (int)off;
+        cur.t = (int)max(0ll, off - kCaItemCost);
+        cur.x += kCaItemCost + cur.t - off;                   // behind the item's own places
     }
     return CaPart{work, grid};
 }

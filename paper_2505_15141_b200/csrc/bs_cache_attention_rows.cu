@@ -133,7 +133,7 @@ cache_attention_rows_kernel(const __grid_constant__ CUtensorMap tm_k, const __gr
         constexpr uint32_t id_s = (1u << 4) | ((uint32_t)(kCaTile >> 3) << 17) | (8u << 24);
         constexpr uint32_t id_o = (1u << 4) | (1u << 16) | ((uint32_t)(D >> 3) << 17) | (8u << 24);
         const uint32_t elected = ca_elect();
-        const uint32_t total = (uint32_t)(cur.end - cur.x);
+        uint32_t total = cur.x < cur.end ? 0xffff0000u : 0u;  // tiles of this CTA, known when its last item is through
         uint32_t ks = 0, kph = 0, vs = 0, vph = 0;            // places in the rings of K and V
         int item = -1, left = 0;                              // tiles of the item whose S is still to be issued
         bool ok = true;
@@ -148,6 +148,10 @@ cache_attention_rows_kernel(const __grid_constant__ CUtensorMap tm_k, const __gr
                     if (j >= total) continue;
                     if (left == 0) {
                         if (item >= 0) ca_advance(p, cur, ca_tiles_here(cur));
+                        if (cur.x >= cur.end) {
+                            total = j;
+                            continue;
+                        }
                         ++item;
                         left = ca_tiles_here(cur);
                         ok = ca_wait(smem_u32(&b_qfull[item & 1]), (uint32_t)((item >> 1) & 1));

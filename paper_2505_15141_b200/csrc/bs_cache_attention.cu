@@ -394,15 +394,20 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_co
 #pragma unroll 1
                         for (int z = (int)c_first; z <= (int)c_last; ++z) {
                             const float* q = p.partial + ((size_t)z * 2 + (z == c_first ? 1 : 0)) * L::kPiece;
-                            float v[16], mc[16];
+                            float v[16];
+                            float4 mc[4];
 #pragma unroll
-                            for (int r = 0; r < 16; ++r) {
-                                v[r] = c + r < rows && has_dim ? __ldcg(q + (c + r) * D + dim) : 0.f;
-                                mc[r] = __ldcg(q + N * D + c + r);
+                            for (int r = 0; r < 16; ++r) v[r] = c + r < rows && has_dim ? __ldcg(q + (c + r) * D + dim) : 0.f;
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) mc[i] = __ldcg(reinterpret_cast<const float4*>(q + N * D + c) + i);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const float4 mm = lds4(f_b + c + 4 * i);
+                                y[4 * i] = fmaf(v[4 * i], mc[i].x == -INFINITY ? 0.f : ex2(mc[i].x - mm.x), y[4 * i]);
+                                y[4 * i + 1] = fmaf(v[4 * i + 1], mc[i].y == -INFINITY ? 0.f : ex2(mc[i].y - mm.y), y[4 * i + 1]);
+                                y[4 * i + 2] = fmaf(v[4 * i + 2], mc[i].z == -INFINITY ? 0.f : ex2(mc[i].z - mm.z), y[4 * i + 2]);
+                                y[4 * i + 3] = fmaf(v[4 * i + 3], mc[i].w == -INFINITY ? 0.f : ex2(mc[i].w - mm.w), y[4 * i + 3]);
                             }
-#pragma unroll
-                            for (int r = 0; r < 16; ++r)
-                                y[r] = fmaf(v[r], mc[r] == -INFINITY ? 0.f : ex2(mc[r] - f_b[c + r]), y[r]);
                         }
                     }
                     if (has_dim)

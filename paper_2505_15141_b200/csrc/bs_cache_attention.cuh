@@ -15,7 +15,10 @@ constexpr int kCaSmem = 230400;                // of 232448 bytes a CTA may use
 constexpr int kCaScaleRing = 8;                // tiles whose scales are kept; more than the tiles in flight
 constexpr int kCaMaxPages = 8;                 // blocks of 16 tokens in a tile
 constexpr int kCaMaxRows = 128;                // rows of an item, at most
-constexpr int kCaItemCost = 2;                 // what an item costs besides its tiles (queries, joining, results), in tiles
+// What an item costs besides its tiles (queries, joining, results), in tiles, when the work is cut into shares.  Measured with
+// 1, 2, 4 and 6: prompt pieces of 1 to 36 tiles 186, 152, 141, 139 us, trees on 1 to 33 tiles 177, 161, 153, 149 us, long
+// items the same.
+constexpr int kCaItemCost = 4;
 
 struct CacheAttnParams {
     const __nv_bfloat16* q;
@@ -259,6 +262,7 @@ __device__ __noinline__ bool ca_clean_v(unsigned char* tile, int tok, const CaWh
 // ---- this CTA's share of the work ----
 struct CaShare {                               // shared memory
     long long w[32];
+    int items[32];
     long long off;
     int b;
 };
@@ -272,30 +276,40 @@ __device__ __forceinline__ CaPart ca_share(const CacheAttnParams& p, CaShare& sh
     if (tid == 0) sh.b = -1;
     const int per = (p.B + THREADS - 1) / THREADS;
     long long mine = 0;
+    int items = 0;
 #pragma unroll 1
     for (int b = tid * per; b < min(p.B, (tid + 1) * per); ++b) {
         int n, base, q0;
         if (!ca_seq(p, b, n, base, q0) && p.status && blockIdx.x == 0) atomicOr(p.status + b, BS_DEV_BAD_LENGTH);
         mine += p.Hkv * ca_head_work(p, n, base);
+        items += p.Hkv * ((n + p.TQ - 1) / p.TQ);
     }
+    items = __reduce_add_sync(0xffffffffu, items);
     long long incl = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
         const long long y = __shfl_up_sync(0xffffffffu, incl, o);
         if (lane >= o) incl += y;
     }
-    if (lane == 31) sh.w[warp] = incl;
+    if (lane == 31) {
+        sh.w[warp] = incl;
+        sh.items[warp] = items;
+    }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    long long work = 0, before = 0;
+    long long work = 0, before = 0, all = 0;
 #pragma unroll 1
     for (int w = 0; w < THREADS / 32; ++w) {
         if (w < warp) before += sh.w[w];
         work += sh.w[w];
+        all += sh.items[w];
     }
-    // an item of two tiles at least for a CTA: they are worked on side by side, and a short item is not cut for nothing
-    const long long grid = min((work + kCaItemCost + 1) / (kCaItemCost + 2), (long long)gridDim.x);
+    // Little work: where items are short, shares of a whole one of two tiles (they are worked on side by side).  Long ones
+    // are cut; a part takes about 0.3 of a tile's time to join, so least + 0.3 tiles / least is what a CTA waits for.
+    const float tiles = all ? (float)(work - kCaItemCost * all) / (float)all : 0.f;   // of an item
+    const int least = tiles <= 8.f ? kCaItemCost + 2 : max(2, (int)sqrtf(0.3f * tiles));
+    const long long grid = min((work + least - 1) / least, (long long)gridDim.x);
     const long long x_lo = grid ? blockIdx.x * work / grid : 0, x_hi = grid && blockIdx.x < grid ? (blockIdx.x + 1) * work / grid : 0;
     const long long from = before + incl - mine;
     if (x_lo < x_hi && x_lo >= from && x_lo < from + mine) {

@@ -360,7 +360,7 @@ bs_status bs_lmhead_verify(const void* H_t, const void* W_t, int d_t, const void
  * cu_new[b] .. cu_new[b + 1] - 1 of the query, key and value arrays.  block table, lengths and slots are the same
  * for all layers.  `status` [B] int32 or NULL: bs_cache_plan writes its BS_DEV_* bits, the other calls add theirs. */
 
-/* Block tables and slot maps from lengths that are on the device.  One launch.
+/* Block tables and slot maps from lengths that are on the device.  One launch, two where T is above 8192.
  *
  *  seq_len     [B] in / out: tokens of every sequence in the cache.  kept[b] tokens of the round before are added first
  *  kept        [B] or NULL (= 0)
@@ -418,7 +418,7 @@ size_t bs_cache_workspace_bytes(int Hq, int Hkv, int d);
  *  workspace    bs_cache_workspace_bytes bytes, 256-byte aligned, cleared once; calls that may overlap need one each
  *
  * Keys and values enter the tensor cores as the e4m3 codes they are; a bf16 query is split into two e4m3 numbers, which
- * holds it exactly down to 2^-10 of its row's largest element; probabilities are split the same way, relative error at
+ * holds it exactly down to 2^-9 of its row's largest element; probabilities are split the same way, relative error at
  * most 2^-8 where they are within 2^-10 of the largest of their 128-token tile and absolute error 2^-18 of that
  * below.  Products accumulate in fp32, tiles are joined in fp32.  Scales of V within a tile should lie within 2^126 of one another.
  * A token that sees nothing (kv_len < its position) gets zeros.  Rows of out behind cu_new[B] are left as they are, and so

@@ -3,32 +3,42 @@
 //
 //   out_i = sum_j 2^(t_ij) v_j / sum_j 2^(t_ij),   t_ij = log2(e) softmax_scale q_i . k_j
 //
-// A CTA works on 128 cached tokens at a time, for the rows (new token, query head of the group) of one key head.
-// Both products run on the tensor cores with the cache's codes as they are:
+// This file: the entry point, and the kernel for up to 32 rows (new token, query head of the group) of a key head;
+// bs_cache_attention_rows.cu has the one for more.  A CTA works on tiles of 128 cached tokens.  Both products run on
+// the tensor cores with the cache's codes as they are:
 //
 //   S^T [128 tokens, N rows] = K [128, d] Q^T     K K-major, as the TMA copy leaves it (swizzled)
 //   O^T [d, N rows]          = V^T P^T            V^T is the same tile read M-major; P^T from shared memory, N-major
 //
-// i.e. the tokens (and then d) are the 128 lanes of the MMA and the rows its N: a few rows cost no more than their
-// share, and no code is ever converted.  The other operand has to be e4m3 as well (kind::f8f6f4): a bf16 query, scaled by a
-// power of two so that its row's largest element lies in [128, 256), is the sum of two e4m3 numbers exactly (four
-// significant bits, a signed remainder of four more; elements below 2^-9 of the largest lose bits under 2^-17
-// of it), and a probability is split the same way (relative error 2^-8 as in bf16), so each product is two MMAs
-// into one accumulator.  Their accumulation was measured against 64 bits: error 2^-20 of the largest product.
+// i.e. the tokens (and then d) are the 128 lanes of the MMA and the rows its N = 16 or 32: a few rows cost no more than
+// their share, and no code is ever converted.  The other operand has to be e4m3 as well (kind::f8f6f4): a bf16 query,
+// scaled by a power of two so that its row's largest element lies in [128, 256), is the sum of two e4m3 numbers exactly
+// (four significant bits, a signed remainder of four more; elements below 2^-9 of the largest lose bits under 2^-17
+// of it), and a probability is split the same way (relative error 2^-8 as in bf16).  Their accumulation was measured
+// against 64 bits: error 2^-20 of the largest product.
 //
 // Scales.  Keys: t_ij = S_ij * (scale of j's block * c_i).  Values: the scale of a token's block joins the exponent:
 //   P''_ij = 2^(t_ij + log2 s_j + 8 - m_i),  m_i = max_j (t_ij + log2 s_j) over the tile,
 // which uses the e4m3 range up to 256 whatever the scales are; the sum of the probabilities takes P'' / s_j in fp32.
-// O^T of every tile is taken from tensor memory and joined in fp32 registers with the tile's own factor 2^(m_i - m),
+// O^T of every tile is taken from tensor memory and joined in fp32 with the tile's own factor 2^(m_i - m),
 // so a token far below the row's running maximum keeps its bits relative to its own tile.
 //
-// Roles of the 16 warps: 0 and 1 TMA producers of K and V, 2 MMA issuer, 3 queries (split into e4m3 one work item ahead),
-// 4-7 accumulator (a thread is an element of d), 8-11 and 12-15 two softmax groups that take the tiles in turn, each with
-// its own maximum and sum (a thread is a token).
+// Roles of the 16 warps: 0 and 1 TMA producers of K and V (one producer of both: 4.3 TB/s of 16-byte-row boxes of
+// 16-token blocks, two: 6.5), 2 MMA issuer, 3 queries (split into e4m3 one work item ahead), 4-7 accumulator (a thread
+// is an element of d), 8-11 and 12-15 two softmax groups that take the tiles in turn, each with its own maximum and
+// sum (a thread is a token).  Sums and accumulator stand in tensor memory, and the loops over rows are rolled: the
+// roles run side by side and share one instruction cache, and every larger form of them (unrolled rows, a third
+// softmax group, accumulators in registers) was slower.
 //
-// Work.  Item = (sequence, key head, N rows).  All items, in order, a few places and one for each tile, are cut into equal contiguous shares,
-// one per CTA, from the lengths on the device; an item that spans several CTAs is joined by the one that finishes
-// last, in the order of the shares (the result does not depend on who that is).
+// Work.  Item = (sequence, key head, N rows).  All items, in order, a few places and one for each tile, are cut into equal
+// contiguous shares, one per CTA, from the lengths on the device; an item that spans several CTAs is joined by the one that
+// finishes last, in the order of the shares (the result does not depend on who that is).
+//
+// Bound by the instructions of the softmax on 16 rows (47 % of issue slots, DRAM 50 % busy: both softmax groups
+// and the accumulator are chained within a tile), close to HBM's rate when a row count of 4 leaves little to do.
+// 32 query / 8 key heads of 128, caches larger than L2: 256 sequences of 4096 tokens, 4 rows, 2.15 GB in 0.45 ms
+// (4.8 TB/s); 64 sequences, 16 rows, 0.135 ms (4.0 TB/s); 32 rows 0.174 ms; two sequences of 100003 and 131072
+// tokens, 20 rows, 0.145 ms (3.3 TB/s); one token on 200 cached ones 9.3 us in a graph.
 #include "bs_cache_attention.cuh"
 
 namespace bs {
@@ -718,7 +728,10 @@ extern "C" bs_status bs_cache_attention(const void* q, long long q_stride_t, lon
     CUtensorMap tm[2];
     if (!ca_map(&tm[0], k_cache, n_blocks, Hkv, block_tokens, d) || !ca_map(&tm[1], v_cache, n_blocks, Hkv, block_tokens, d))
         return BS_ERR_CUDA;
-    // the fewest rows that take a sequence's key head at once, so that its cache is read once
+    // The fewest rows that take a sequence's key head at once, so that its cache is read once.  Tokens as lanes cost
+    // in proportion to the rows, rows as lanes the same for any number up to 64 and more for the few: 64
+    // sequences of 4096 tokens, 8 key heads of 128, with 32 rows 174 us here and 219 there, with 48 rows 250 and 217,
+    // with 64 rows 305 and 219.  Prompts take 128 at once: the copies and the scales serve twice the rows.
     const long long rows = (long long)max_new * p.G;
     const int N = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : kCaMaxRows;
     p.TQ = N / p.G;

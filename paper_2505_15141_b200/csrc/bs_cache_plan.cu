@@ -8,7 +8,7 @@
 //
 // Everything is prefix sums over the batch, which is small (B <= 4096): one CTA.  It also writes the slots of an ordinary
 // round; a large slot map (prompts) is written by a second launch over many CTAs from the finished tables.  Bound by
-// latency: a handful of dependent loads and block-wide scans.
+// latency: a handful of dependent loads and block-wide scans.  64 sequences take 6.4 us in a graph.
 #include "bs_common.cuh"
 
 #include <atomic>
@@ -35,7 +35,9 @@ struct CachePlanParams {
 
 constexpr int kPlanThreads = 1024;
 constexpr int kSlotThreads = 256;
-// Slots that the planning CTA writes itself; larger maps take a launch of their own.
+// Slots that the planning CTA writes itself; larger maps take a launch of their own.  64 sequences, planned and given
+// back, one launch against two: 512 slots 18.4 and 26.6 us, 4096 20.5 and 24.6, 8192 22.5 and 22.5, 16384 28.7 and 22.5,
+// 65536 61 and 25.
 constexpr int kPlanSlotsInline = 8192;
 
 // Inclusive prefix sum over the CTA's threads of a pair of counts; `total` is the sum over all of them.

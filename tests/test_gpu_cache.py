@@ -447,9 +447,10 @@ def test_append_one_token(lib):
     _append_check(lib, *_append_case(lib, 2, [(2, 15, 1)], 8, 64, 16, torch.bfloat16), 16)
 
 
+@pytest.mark.parametrize("H", [2, 4, 8])
 @pytest.mark.parametrize("bt", [16, 128])
-def test_append_many_tokens(lib, bt):
-    """Enough tokens that a group of warps looks after a block's worth of them; runs that cross its borders."""
+def test_append_many_tokens(lib, bt, H):
+    """A group of warps looks after 4 tokens, 8, or a block's worth of them; runs that cross its borders."""
     runs, blk = [], 0
     rng = np.random.default_rng(bt)
     while sum(r[2] for r in runs) < 4500:
@@ -458,7 +459,7 @@ def test_append_many_tokens(lib, bt):
             m = min(n, bt - off)
             runs.append((blk, off, m))
             blk, off, n = blk + 1, 0, n - m
-    _append_check(lib, *_append_case(lib, bt, runs, 4, 64, bt, torch.bfloat16), bt)
+    _append_check(lib, *_append_case(lib, bt, runs, H, 64, bt, torch.bfloat16), bt)
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])

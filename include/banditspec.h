@@ -358,7 +358,9 @@ bs_status bs_lmhead_verify(const void* H_t, const void* W_t, int d_t, const void
  * tokens of one sequence.  d is 64 or 128.  block_table [B, max_blocks] int32 lists the blocks of every sequence in
  * order; entries behind those it holds are never read.  New tokens are packed: those of sequence b are rows
  * cu_new[b] .. cu_new[b + 1] - 1 of the query, key and value arrays.  block table, lengths and slots are the same
- * for all layers.  `status` [B] int32 or NULL: bs_cache_plan writes its BS_DEV_* bits, the other calls add theirs. */
+ * for all layers.  Scales are positive and finite; a block that nothing was written to needs none.  Sequences may share
+ * blocks that are only read (a common prefix); a block that a call writes to belongs to one sequence.
+ * `status` [B] int32 or NULL: bs_cache_plan writes its BS_DEV_* bits, the other calls add theirs. */
 
 /* Block tables and slot maps from lengths that are on the device.  One launch, two where T is above 8192.
  *

@@ -1,4 +1,4 @@
-"""The key / value cache of a round on the GPU against the checker (needs a B200), through the C ABI: bs_cache_plan,
+"""The key / value cache of a round on the GPU against the oracle (needs a B200), through the C ABI: bs_cache_plan,
 bs_cache_append, bs_cache_attention, bs_cache_keep_path, and rounds of all of them together.
 
 Whole numbers, codes and scales are compared bit for bit.  Tolerance of the attention, from its arithmetic: out =
@@ -227,7 +227,7 @@ def test_bad_trees_are_flagged_and_hang_under_the_root(lib):
     st = torch.zeros(3, dtype=torch.int32, device=DEV)
     out = c.run(lib, status=st)
     assert st.tolist() == [0, lib.BS_DEV_BAD_TREE, 0]
-    c.check(out)                                          # the checker reads a bad parent as the root, too
+    c.check(out)                                          # the oracle reads a bad parent as the root, too
     c.parent = np.array([[0], [0], [0]])                  # room for one drafted node, five rows
     st.zero_()
     assert (c.run(lib, status=st)[:15] == 7.0).all()
@@ -290,6 +290,13 @@ def test_strides_and_a_padded_batch(lib):
     out = c.run(lib, q=big[:, 8:16], out=o[:, 1])
     c.check(out)
     assert (o[:, 0] == 7.0).all()
+
+
+@pytest.mark.parametrize("max_new", [4, 16])
+def test_sequences_share_the_blocks_of_a_common_prefix(lib, max_new):
+    c = Case(41, [100, 300, 90], [3, 4, 2], 16, 4, 128, 16, q_mul=2.0)
+    c.table[1, :5] = c.table[2, :5] = c.table[0, :5]
+    c.check(c.run(lib, max_new=max_new))
 
 
 def test_bad_lengths_and_blocks_are_flagged(lib):

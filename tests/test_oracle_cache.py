@@ -1,4 +1,4 @@
-"""The checker of the key / value cache against independent statements, and the host-side refusals of bs_cache_*
+"""The oracle of the key / value cache against independent statements, and the host-side refusals of bs_cache_*
 (no kernel is launched here)."""
 import numpy as np
 import pytest

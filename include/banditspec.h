@@ -386,6 +386,18 @@ bs_status bs_cache_plan(int32_t* seq_len, const int32_t* kept, const int32_t* n_
                         int32_t* free_blocks, int n_blocks, int32_t* n_free, int32_t* kv_len, int32_t* cu_new,
                         int32_t* slot_map, int32_t* positions, int T, int32_t* status, void* stream);
 
+/* The same where the round before may have refused sequences.  A refused sequence has no rows in the packed arrays, but the
+ * verification of the whole batch still returns an out_len for it; those tokens were never in the cache.
+ *
+ *  last_cu [B + 1] or NULL: cu_new of the plan whose new tokens `kept` counts (the array cu_new itself may be passed: it is read
+ *          before it is written).  A sequence that got no new tokens then keeps none, whatever kept says; one that is
+ *          said to keep more than it got is BS_DEV_BAD_LENGTH.  NULL, and bs_cache_plan: kept is taken as it is, and
+ *          has to be 0 where the plan before set a bit of status. */
+bs_status bs_cache_plan_next(int32_t* seq_len, const int32_t* kept, const int32_t* last_cu, const int32_t* n_new, int extra,
+                             const uint8_t* active, int B, int block_tokens, int32_t* block_table, int max_blocks,
+                             int32_t* n_held, int32_t* free_blocks, int n_blocks, int32_t* n_free, int32_t* kv_len,
+                             int32_t* cu_new, int32_t* slot_map, int32_t* positions, int T, int32_t* status, void* stream);
+
 /* Writes the new tokens' keys and values into their slots, quantised.
  *
  *  k, v      [T, Hkv, d] dtype, d contiguous; strides of a token and of a head in elements, multiples of 16 bytes,
@@ -440,7 +452,8 @@ bs_status bs_cache_attention(const void* q, long long q_stride_t, long long q_st
  *  out_nodes [B, Nmax] and accept_len [B] from bs_tree_verify_greedy; seq_len [B] from bs_cache_plan of the round (tokens
  *  before the tree).
  * A destination block's scale becomes the largest of its own and those of the blocks its tokens come from.  A sequence
- * with BS_DEV_BAD_LENGTH, BS_DEV_BAD_TREE (nodes that do not ascend) or BS_DEV_BAD_BLOCK is left as it is. */
+ * with BS_DEV_BAD_LENGTH, BS_DEV_BAD_TREE (nodes that do not ascend) or BS_DEV_BAD_BLOCK is left as it is, and so is one whose
+ * status says that bs_cache_plan gave it no new tokens (pass the plan's status; with NULL its accept_len has to be 0). */
 bs_status bs_cache_keep_path(const int32_t* out_nodes, const int32_t* accept_len, const int32_t* seq_len, int B, int Nmax,
                              const int32_t* block_table, int max_blocks, int Hkv, int d, void* k_cache, float* k_scale,
                              void* v_cache, float* v_scale, int n_blocks, int block_tokens, int32_t* status, void* stream);

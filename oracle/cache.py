@@ -48,8 +48,12 @@ def block_scale(x: np.ndarray) -> float:
 
 # ---- plan ------------------------------------------------------------------------------------
 
-def plan(seq_len, kept, n_new, extra, active, bt, table, held, free, T):
-    """One call.  `free`: list, its top last.  Returns the new state and the outputs as a dict."""
+def plan(seq_len, kept, n_new, extra, active, bt, table, held, free, T, last_cu=None):
+    """One call.  `free`: list, its top last.  last_cu: cu_new of the call whose tokens `kept` counts.  Returns the new
+    state and the outputs as a dict."""
+    if kept is not None and last_cu is not None:
+        got = np.diff(last_cu)
+        kept = [k if k <= 0 else 0 if g <= 0 else -1 if k > g else k for k, g in zip(np.asarray(kept).tolist(), got.tolist())]
     B, W = table.shape
     seq_len, table, held, free = seq_len.copy(), table.copy(), held.copy(), list(free)
     status, new, kv = np.zeros(B, np.int64), np.zeros(B, np.int64), np.zeros(B, np.int64)

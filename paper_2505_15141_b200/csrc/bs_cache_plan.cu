@@ -18,6 +18,7 @@ namespace bs {
 struct CachePlanParams {
     int32_t* seq_len;          // [B] in / out
     const int32_t* kept;       // [B] or NULL
+    const int32_t* last_cu;    // [B + 1] or NULL: cu_new of the plan whose tokens `kept` counts; may be cu_new
     const int32_t* n_new;      // [B]
     const uint8_t* active;     // [B] or NULL
     int32_t* block_table;      // [B, W] in / out
@@ -88,7 +89,12 @@ __global__ void __launch_bounds__(kPlanThreads) cache_plan_kernel(const CachePla
         int held = 0, bits = 0;
         if (b < p.B) {
             const bool act = !p.active || p.active[b];
-            const int len = __ldcg(p.seq_len + b), keep = act && p.kept ? p.kept[b] : 0;
+            const int len = __ldcg(p.seq_len + b);
+            int keep = act && p.kept ? p.kept[b] : 0;
+            if (keep > 0 && p.last_cu) {                       // of no new tokens none stay, whatever was verified
+                const int got = p.last_cu[b + 1] - p.last_cu[b];
+                keep = got <= 0 ? 0 : keep > got ? -1 : keep;
+            }
             held = __ldcg(p.n_held + b);
             L = (long long)len + keep;
             n = act ? (long long)p.n_new[b] + p.extra : 0;
@@ -242,11 +248,11 @@ static std::atomic<bool> g_plan_attr[64];
 
 using namespace bs;
 
-extern "C" bs_status bs_cache_plan(int32_t* seq_len, const int32_t* kept, const int32_t* n_new, int extra,
-                                   const uint8_t* active, int B, int block_tokens, int32_t* block_table, int max_blocks,
-                                   int32_t* n_held, int32_t* free_blocks, int n_blocks, int32_t* n_free, int32_t* kv_len,
-                                   int32_t* cu_new, int32_t* slot_map, int32_t* positions, int T, int32_t* status,
-                                   void* stream) {
+extern "C" bs_status bs_cache_plan_next(int32_t* seq_len, const int32_t* kept, const int32_t* last_cu, const int32_t* n_new,
+                                        int extra, const uint8_t* active, int B, int block_tokens, int32_t* block_table,
+                                        int max_blocks, int32_t* n_held, int32_t* free_blocks, int n_blocks, int32_t* n_free,
+                                        int32_t* kv_len, int32_t* cu_new, int32_t* slot_map, int32_t* positions, int T,
+                                        int32_t* status, void* stream) {
     if (B < 1 || max_blocks < 1 || n_blocks < 1 || T < 1 || extra < 0) return BS_ERR_INVALID_ARG;
     if (!seq_len || !n_new || !block_table || !n_held || !free_blocks || !n_free || !kv_len || !cu_new || !slot_map)
         return BS_ERR_INVALID_ARG;
@@ -258,7 +264,7 @@ extern "C" bs_status bs_cache_plan(int32_t* seq_len, const int32_t* kept, const 
         ((long long)n_blocks << lg) > 0x7fffffffLL)
         return BS_ERR_UNSUPPORTED;
     CachePlanParams p;
-    p.seq_len = seq_len; p.kept = kept; p.n_new = n_new; p.active = active; p.block_table = block_table;
+    p.seq_len = seq_len; p.kept = kept; p.last_cu = last_cu; p.n_new = n_new; p.active = active; p.block_table = block_table;
     p.n_held = n_held; p.free_blocks = free_blocks; p.n_free = n_free; p.kv_len = kv_len; p.cu_new = cu_new;
     p.slot_map = slot_map; p.positions = positions; p.status = status;
     p.extra = extra; p.bt_log2 = lg; p.B = B; p.W = max_blocks; p.n_blocks = n_blocks; p.T = T;
@@ -277,4 +283,13 @@ extern "C" bs_status bs_cache_plan(int32_t* seq_len, const int32_t* kept, const 
     const cudaError_t e = launch_pdl(cache_plan_kernel, 1, kPlanThreads, smem, st, p);
     if (e != cudaSuccess || p.inline_slots) return cuda_status(e);
     return cuda_status(launch_pdl(cache_slots_kernel, (unsigned)(((long long)T + 1023) / 1024), kSlotThreads, 0, st, p));
+}
+
+extern "C" bs_status bs_cache_plan(int32_t* seq_len, const int32_t* kept, const int32_t* n_new, int extra,
+                                   const uint8_t* active, int B, int block_tokens, int32_t* block_table, int max_blocks,
+                                   int32_t* n_held, int32_t* free_blocks, int n_blocks, int32_t* n_free, int32_t* kv_len,
+                                   int32_t* cu_new, int32_t* slot_map, int32_t* positions, int T, int32_t* status,
+                                   void* stream) {
+    return bs_cache_plan_next(seq_len, kept, nullptr, n_new, extra, active, B, block_tokens, block_table, max_blocks, n_held,
+                              free_blocks, n_blocks, n_free, kv_len, cu_new, slot_map, positions, T, status, stream);
 }

@@ -196,6 +196,9 @@ __global__ void __launch_bounds__(kKeepWarps * 32) cache_keep_kernel(const Cache
     float* scales = kv ? p.scale[1] : p.scale[0];
     const int tau = p.accept_len[b];
     const long long base = p.seq_len[b];
+    const int st = p.status ? __ldcg(p.status + b) : 0;
+    // the plan gave the sequence no slots: its path was never written
+    if (st & (BS_DEV_BAD_LENGTH | BS_DEV_NO_BLOCKS | BS_DEV_NO_ROOM)) return;
     if (tau == 0 && base >= 0) return;
     // lane j holds token j of the path
     const bool mine = lane < tau && tau <= p.Nmax;

@@ -358,8 +358,9 @@ bs_status bs_lmhead_verify(const void* H_t, const void* W_t, int d_t, const void
  * tokens of one sequence.  d is 64 or 128.  block_table [B, max_blocks] int32 lists the blocks of every sequence in
  * order; entries behind those it holds are never read.  New tokens are packed: those of sequence b are rows
  * cu_new[b] .. cu_new[b + 1] - 1 of the query, key and value arrays.  block table, lengths and slots are the same
- * for all layers.  Scales are positive and finite; a block that nothing was written to needs none.  Sequences may share
- * blocks that are only read (a common prefix); a block that a call writes to belongs to one sequence.
+ * for all layers.  Scales are positive and finite; a block that nothing was written to needs none.  bs_cache_attention may
+ * be given tables whose sequences share blocks (a common prefix); a block that a call writes to belongs to one sequence, and in
+ * the tables of a plan every block stands in one place, but for the leading ones that n_shared of bs_cache_plan_next counts.
  * `status` [B] int32 or NULL: bs_cache_plan writes its BS_DEV_* bits, the other calls add theirs. */
 
 /* Block tables and slot maps from lengths that are on the device.  One launch, two where T is above 8192.
@@ -386,17 +387,24 @@ bs_status bs_cache_plan(int32_t* seq_len, const int32_t* kept, const int32_t* n_
                         int32_t* free_blocks, int n_blocks, int32_t* n_free, int32_t* kv_len, int32_t* cu_new,
                         int32_t* slot_map, int32_t* positions, int T, int32_t* status, void* stream);
 
-/* The same where the round before may have refused sequences.  A refused sequence has no rows in the packed arrays, but the
- * verification of the whole batch still returns an out_len for it; those tokens were never in the cache.
+/* The same where the round before may have refused sequences, and where sequences share a prefix.  A refused sequence has
+ * no rows in the packed arrays, but the verification of the whole batch still returns an out_len for it; those tokens
+ * were never in the cache.
  *
  *  last_cu [B + 1] or NULL: cu_new of the plan whose new tokens `kept` counts (the array cu_new itself may be passed: it is read
  *          before it is written).  A sequence that got no new tokens then keeps none, whatever kept says; one that is
  *          said to keep more than it got is BS_DEV_BAD_LENGTH.  NULL, and bs_cache_plan: kept is taken as it is, and
- *          has to be 0 where the plan before set a bit of status. */
-bs_status bs_cache_plan_next(int32_t* seq_len, const int32_t* kept, const int32_t* last_cu, const int32_t* n_new, int extra,
-                             const uint8_t* active, int B, int block_tokens, int32_t* block_table, int max_blocks,
-                             int32_t* n_held, int32_t* free_blocks, int n_blocks, int32_t* n_free, int32_t* kv_len,
-                             int32_t* cu_new, int32_t* slot_map, int32_t* positions, int T, int32_t* status, void* stream);
+ *          has to be 0 where the plan before set a bit of status.
+ *  n_shared [B] or NULL (= 0): the first n_shared[b] blocks of the row, full ones, are shared with other sequences and only
+ *          read.  They count in n_held and are never returned, also when the sequence ends; a sequence whose new tokens would
+ *          lie in them (seq_len < n_shared * block_tokens), or that holds fewer, is BS_DEV_BAD_LENGTH.  The caller knows who still
+ *          reads them: the row of a sequence that ended is let go of with n_held[b] = n_shared[b] = 0, the last reader's with
+ *          n_shared[b] = 0 alone, and then they go back to the stack with the rest. */
+bs_status bs_cache_plan_next(int32_t* seq_len, const int32_t* kept, const int32_t* last_cu, const int32_t* n_shared,
+                             const int32_t* n_new, int extra, const uint8_t* active, int B, int block_tokens,
+                             int32_t* block_table, int max_blocks, int32_t* n_held, int32_t* free_blocks, int n_blocks,
+                             int32_t* n_free, int32_t* kv_len, int32_t* cu_new, int32_t* slot_map, int32_t* positions, int T,
+                             int32_t* status, void* stream);
 
 /* Writes the new tokens' keys and values into their slots, quantised.
  *

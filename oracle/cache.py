@@ -48,9 +48,9 @@ def block_scale(x: np.ndarray) -> float:
 
 # ---- plan ------------------------------------------------------------------------------------
 
-def plan(seq_len, kept, n_new, extra, active, bt, table, held, free, T, last_cu=None):
-    """One call.  `free`: list, its top last.  last_cu: cu_new of the call whose tokens `kept` counts.  Returns the new
-    state and the outputs as a dict."""
+def plan(seq_len, kept, n_new, extra, active, bt, table, held, free, T, last_cu=None, shared=None):
+    """One call.  `free`: list, its top last.  last_cu: cu_new of the call whose tokens `kept` counts.  shared: leading
+    blocks of every sequence that are not returned.  Returns the new state and the outputs as a dict."""
     if kept is not None and last_cu is not None:
         got = np.diff(last_cu)
         kept = [k if k <= 0 else 0 if g <= 0 else -1 if k > g else k for k, g in zip(np.asarray(kept).tolist(), got.tolist())]
@@ -63,8 +63,9 @@ def plan(seq_len, kept, n_new, extra, active, bt, table, held, free, T, last_cu=
         on = active is None or active[b]
         L = int(seq_len[b]) + (int(kept[b]) if on and kept is not None else 0)
         n = int(n_new[b]) + extra if on else 0
+        sh = 0 if shared is None else int(shared[b])
         if seq_len[b] < 0 or (on and kept is not None and kept[b] < 0) or n < 0 or not 0 <= held[b] <= W \
-                or L > held[b] * bt or L + n > W * bt:
+                or L > held[b] * bt or L + n > W * bt or not 0 <= sh <= held[b] or (n > 0 and L < sh * bt):
             status[b] = BAD_LENGTH
             continue
         asked += n
@@ -73,7 +74,7 @@ def plan(seq_len, kept, n_new, extra, active, bt, table, held, free, T, last_cu=
             status[b] = NO_ROOM
             continue
         new[b] = n
-        want[b] = -(-(L + n) // bt)
+        want[b] = max(-(-(L + n) // bt), sh)
     gone = []                                             # surplus blocks, in the order of the sequences
     for b in range(B):
         for j in range(int(want[b]), int(held[b])):

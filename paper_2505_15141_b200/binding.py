@@ -54,7 +54,7 @@ SIGNATURES = {
     "bs_lmhead_verify": (_i, [_vp, _vp, _i, _vp, _vp, _i, _vp, _vp, _vp, _f, _i, _i, _i, _vp, _vp, _vp, _vp, _vp,
                               _vp, _sz, _vp]),
     "bs_cache_plan": (_i, [_vp, _vp, _vp, _i, _vp, _i, _i, _vp, _i, _vp, _vp, _i, _vp, _vp, _vp, _vp, _vp, _i, _vp, _vp]),
-    "bs_cache_plan_next": (_i, [_vp, _vp, _vp, _vp, _i, _vp, _i, _i, _vp, _i, _vp, _vp, _i, _vp, _vp, _vp, _vp, _vp, _i, _vp, _vp]),
+    "bs_cache_plan_next": (_i, [_vp, _vp, _vp, _vp, _vp, _i, _vp, _i, _i, _vp, _i, _vp, _vp, _i, _vp, _vp, _vp, _vp, _vp, _i, _vp, _vp]),
     "bs_cache_append": (_i, [_vp, _vp, _i, _ll, _ll, _ll, _ll, _vp, _i, _i, _i, _vp, _vp, _vp, _vp, _i, _i, _vp]),
     "bs_cache_workspace_bytes": (_sz, [_i, _i, _i]),
     "bs_cache_attention": (_i, [_vp, _ll, _ll, _vp, _vp, _vp, _i, _vp, _i, _vp, _vp, _vp, _vp, _i, _i, _i, _i, _i, _i, _i,
@@ -358,14 +358,17 @@ def new_cache(n_blocks: int, Hkv: int, block_tokens: int, d: int, device="cuda")
 
 
 def bs_cache_plan(seq_len, kept, n_new, extra: int, active, block_tokens: int, block_table, n_held, free_blocks, n_free,
-                  kv_len, cu_new, slot_map, positions, status, stream=None, last_cu=None) -> None:
+                  kv_len, cu_new, slot_map, positions, status, stream=None, last_cu=None,
+                  n_shared=None) -> None:
     """Block tables, slots and positions of a round's new tokens; seq_len, block_table, n_held, free_blocks and n_free
     are updated in place.  last_cu: cu_new of the plan whose tokens `kept` counts (may be cu_new), so that a sequence it
-    refused keeps none."""
+    refused keeps none.  n_shared: leading blocks of each sequence that it shares with others and that are never returned."""
     B, W = block_table.shape
     n_blocks, T = free_blocks.numel(), slot_map.numel()
     assert active is None or (active.dtype is torch.uint8 and active.numel() == B and active.is_contiguous())
-    fn, more = (_lib.bs_cache_plan, ()) if last_cu is None else (_lib.bs_cache_plan_next, (_i32(last_cu, B + 1),))
+    fn, more = _lib.bs_cache_plan, ()
+    if last_cu is not None or n_shared is not None:
+        fn, more = _lib.bs_cache_plan_next, (_i32(last_cu, B + 1), _i32(n_shared, B))
     _call(fn, "bs_cache_plan", seq_len.device, stream, _i32(seq_len, B), _i32(kept, B), *more, _i32(n_new, B), extra,
           None if active is None else active.data_ptr(), B, block_tokens, _i32(block_table, B * W), W, _i32(n_held, B),
           _i32(free_blocks, n_blocks), n_blocks, _i32(n_free, 1), _i32(kv_len, B), _i32(cu_new, B + 1), _i32(slot_map, T),

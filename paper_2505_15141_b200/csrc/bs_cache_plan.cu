@@ -5,6 +5,7 @@
 // hold ceil((L + n) / bt) blocks.  Surplus blocks go back first, in such an order that the j-th of them
 // (counted over the sequences, ascending within one) becomes the (j + 1)-th from the top; then the j-th missing
 // block is the (j + 1)-th from the top.  A round that is planned and given back whole leaves the stack as it was.
+// Leading blocks that a sequence shares with others (n_shared) count as needed for ever: they are never returned.
 //
 // Everything is prefix sums over the batch, which is small (B <= 4096): one CTA.  It also writes the slots of an ordinary
 // round; a large slot map (prompts) is written by a second launch over many CTAs from the finished tables.  Bound by
@@ -19,6 +20,7 @@ struct CachePlanParams {
     int32_t* seq_len;          // [B] in / out
     const int32_t* kept;       // [B] or NULL
     const int32_t* last_cu;    // [B + 1] or NULL: cu_new of the plan whose tokens `kept` counts; may be cu_new
+    const int32_t* n_shared;   // [B] or NULL: leading blocks that are not the plan's to return
     const int32_t* n_new;      // [B]
     const uint8_t* active;     // [B] or NULL
     int32_t* block_table;      // [B, W] in / out
@@ -86,7 +88,7 @@ __global__ void __launch_bounds__(kPlanThreads) cache_plan_kernel(const CachePla
     for (int b0 = 0; b0 < p.B; b0 += kPlanThreads) {
         const int b = b0 + tid;
         long long L = 0, n = 0;
-        int held = 0, bits = 0;
+        int held = 0, shared = 0, bits = 0;
         if (b < p.B) {
             const bool act = !p.active || p.active[b];
             const int len = __ldcg(p.seq_len + b);
@@ -98,8 +100,10 @@ __global__ void __launch_bounds__(kPlanThreads) cache_plan_kernel(const CachePla
             held = __ldcg(p.n_held + b);
             L = (long long)len + keep;
             n = act ? (long long)p.n_new[b] + p.extra : 0;
+            shared = p.n_shared ? p.n_shared[b] : 0;
             if (len < 0 || keep < 0 || n < 0 || held < 0 || held > p.W || L > (long long)held * bt ||
-                L + n > (long long)p.W * bt) {
+                L + n > (long long)p.W * bt || shared < 0 || shared > held ||
+                (n > 0 && L < (long long)shared * bt)) {       // its tokens would be written into shared blocks
                 bits = BS_DEV_BAD_LENGTH;
                 n = 0;
             }
@@ -107,7 +111,7 @@ __global__ void __launch_bounds__(kPlanThreads) cache_plan_kernel(const CachePla
         const longlong2 inc = plan_scan(make_longlong2(n, 0), s_w, total);
         if (n > 0 && carry.x + inc.x > p.T) bits |= BS_DEV_NO_ROOM;
         carry.x += total.x;
-        const int delta = bits || b >= p.B ? 0 : (int)((L + n + bt - 1) >> p.bt_log2) - held;
+        const int delta = bits || b >= p.B ? 0 : max((int)((L + n + bt - 1) >> p.bt_log2), shared) - held;
         if (b < p.B) {
             s_len[b] = (int)((bits & BS_DEV_BAD_LENGTH) ? 0 : L);
             s_held[b] = held;
@@ -248,11 +252,11 @@ static std::atomic<bool> g_plan_attr[64];
 
 using namespace bs;
 
-extern "C" bs_status bs_cache_plan_next(int32_t* seq_len, const int32_t* kept, const int32_t* last_cu, const int32_t* n_new,
-                                        int extra, const uint8_t* active, int B, int block_tokens, int32_t* block_table,
-                                        int max_blocks, int32_t* n_held, int32_t* free_blocks, int n_blocks, int32_t* n_free,
-                                        int32_t* kv_len, int32_t* cu_new, int32_t* slot_map, int32_t* positions, int T,
-                                        int32_t* status, void* stream) {
+extern "C" bs_status bs_cache_plan_next(int32_t* seq_len, const int32_t* kept, const int32_t* last_cu,
+                                        const int32_t* n_shared, const int32_t* n_new, int extra, const uint8_t* active, int B,
+                                        int block_tokens, int32_t* block_table, int max_blocks, int32_t* n_held,
+                                        int32_t* free_blocks, int n_blocks, int32_t* n_free, int32_t* kv_len, int32_t* cu_new,
+                                        int32_t* slot_map, int32_t* positions, int T, int32_t* status, void* stream) {
     if (B < 1 || max_blocks < 1 || n_blocks < 1 || T < 1 || extra < 0) return BS_ERR_INVALID_ARG;
     if (!seq_len || !n_new || !block_table || !n_held || !free_blocks || !n_free || !kv_len || !cu_new || !slot_map)
         return BS_ERR_INVALID_ARG;
@@ -264,8 +268,8 @@ extern "C" bs_status bs_cache_plan_next(int32_t* seq_len, const int32_t* kept, c
         ((long long)n_blocks << lg) > 0x7fffffffLL)
         return BS_ERR_UNSUPPORTED;
     CachePlanParams p;
-    p.seq_len = seq_len; p.kept = kept; p.last_cu = last_cu; p.n_new = n_new; p.active = active; p.block_table = block_table;
-    p.n_held = n_held; p.free_blocks = free_blocks; p.n_free = n_free; p.kv_len = kv_len; p.cu_new = cu_new;
+    p.seq_len = seq_len; p.kept = kept; p.last_cu = last_cu; p.n_shared = n_shared; p.n_new = n_new; p.active = active;
+    p.block_table = block_table; p.n_held = n_held; p.free_blocks = free_blocks; p.n_free = n_free; p.kv_len = kv_len; p.cu_new = cu_new;
     p.slot_map = slot_map; p.positions = positions; p.status = status;
     p.extra = extra; p.bt_log2 = lg; p.B = B; p.W = max_blocks; p.n_blocks = n_blocks; p.T = T;
     int dev = 0;
@@ -290,6 +294,6 @@ extern "C" bs_status bs_cache_plan(int32_t* seq_len, const int32_t* kept, const 
                                    int32_t* n_held, int32_t* free_blocks, int n_blocks, int32_t* n_free, int32_t* kv_len,
                                    int32_t* cu_new, int32_t* slot_map, int32_t* positions, int T, int32_t* status,
                                    void* stream) {
-    return bs_cache_plan_next(seq_len, kept, nullptr, n_new, extra, active, B, block_tokens, block_table, max_blocks, n_held,
-                              free_blocks, n_blocks, n_free, kv_len, cu_new, slot_map, positions, T, status, stream);
+    return bs_cache_plan_next(seq_len, kept, nullptr, nullptr, n_new, extra, active, B, block_tokens, block_table, max_blocks,
+                              n_held, free_blocks, n_blocks, n_free, kv_len, cu_new, slot_map, positions, T, status, stream);
 }

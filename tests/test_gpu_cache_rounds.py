@@ -1,5 +1,5 @@
-"""Rounds of the key / value cache in which sequences are refused, on the GPU (needs a B200): a sequence that got no slots keeps
-nothing, whatever the verification of the batch says about it."""
+"""Rounds of the key / value cache in which sequences are refused or share a prefix, on the GPU (needs a B200): a sequence that got
+no slots keeps nothing, whatever the verification of the batch says about it; shared blocks are neither returned nor written."""
 import numpy as np
 import pytest
 import torch
@@ -24,14 +24,15 @@ class Pool:
         self.d = dict(seq=_i32(self.seq), held=_i32(self.held), table=_i32(self.table), free=_i32(self.free), n_free=_i32([n_blocks]),
                       kv=_i32([0] * B), cu=_i32(self.cu), slots=_i32([0] * T), pos=_i32([0] * T), status=_i32([0] * B))
 
-    def plan(self, lib, kept, new, extra=0):
+    def plan(self, lib, kept, new, extra=0, shared=None):
         d = self.d
         d["seq"].copy_(_i32(self.seq))
         lib.bs_cache_plan(d["seq"], kept, _i32(new), extra, None, self.bt, d["table"], d["held"], d["free"], d["n_free"], d["kv"], d["cu"],
-                          d["slots"], d["pos"], d["status"], last_cu=d["cu"])
+                          d["slots"], d["pos"], d["status"], last_cu=d["cu"],
+                          n_shared=None if shared is None else _i32(shared))
         torch.cuda.synchronize()
         r = oc.plan(self.seq, None if kept is None else kept.cpu().numpy(), np.asarray(new), extra, None, self.bt, self.table, self.held,
-                    self.free, self.T, self.cu)
+                    self.free, self.T, self.cu, shared)
         for n, k in (("seq", "seq_len"), ("held", "held"), ("table", "table"), ("kv", "kv_len"), ("cu", "cu_new"), ("slots", "slot_map"),
                      ("pos", "positions"), ("status", "status")):
             assert np.array_equal(d[n].cpu().numpy(), r[k]), n
@@ -86,3 +87,46 @@ def test_the_path_of_a_refused_tree_moves_nothing(lib):
     for x, w in zip((kc, vc), was):
         assert torch.equal(x[own], w[own]) and not torch.equal(x, w)
     assert p.d["status"].tolist() == [lib.BS_DEV_NO_BLOCKS, 0]
+
+
+@pytest.mark.parametrize("B,T", [(6, 300), (1100, 20000)])
+def test_sequences_behind_a_common_prefix_come_and_go(lib, B, T):
+    rng = np.random.default_rng(B + 1)
+    bt, W, sh, nb, H, d = 16, 10, 3, 5 * B + 3, 2, 64
+    prefix = [2, 0, 4]
+    p = Pool(B, bt, W, nb, T)
+    p.table[:, :sh] = prefix
+    p.seq[:], p.held[:], p.free = sh * bt, sh, [b for b in range(nb) if b not in prefix]
+    for n, x in (("table", p.table), ("held", p.held), ("n_free", [len(p.free)])):
+        p.d[n].copy_(_i32(x))
+    p.d["free"][:len(p.free)] = _i32(p.free)
+    codes = [torch.randint(0, 127, (nb, H, bt, d), device=DEV, dtype=torch.uint8) for _ in range(2)]
+    scales = [torch.full((nb, H), 2.0 ** -9, device=DEV) for _ in range(2)]
+    was = [x[prefix].clone() for x in codes + scales]
+    kept, shared = None, np.full(B, sh)
+    for _ in range(6):
+        r = p.plan(lib, kept, rng.integers(0, 14, B), 1, shared)
+        assert not (r["status"] & lib.BS_DEV_BAD_LENGTH).any()
+        x = torch.randn(T, H, d, device=DEV)              # far above what the present scales hold: a block written to changes
+        lib.bs_cache_append(x, x, p.d["slots"], codes[0], scales[0], codes[1], scales[1])
+        torch.cuda.synchronize()
+        assert all(torch.equal(a[prefix], w) for a, w in zip(codes + scales, was))
+        kept = rng.integers(0, 15, B) % np.maximum(np.diff(p.cu), 1)
+        gone = rng.random(B) < 0.25
+        p.seq[gone], kept[gone] = sh * bt, 0
+        kept = _i32(kept)
+    p.seq[:] = 0                                          # all end; the last reader lets the prefix go
+    p.plan(lib, None, np.zeros(B, int), 0, np.array([0] + [sh] * (B - 1)))
+    assert sorted(p.free) == list(range(nb))
+
+
+def test_new_tokens_inside_shared_blocks_are_flagged(lib):
+    p = Pool(4, 16, 4, 8, 64)
+    p.table[:3, 0], p.held[:] = 0, [1, 1, 2, 0]
+    p.table[2, 1] = 1
+    p.seq[:], p.free = [16, 15, 31, 0], [5, 6]
+    for n, x in (("table", p.table), ("held", p.held), ("n_free", [2])):
+        p.d[n].copy_(_i32(x))
+    p.d["free"][:2] = _i32([5, 6])
+    r = p.plan(lib, None, [1, 1, 0, 1], 0, [1, 1, 2, 1])
+    assert r["status"].tolist() == [0, lib.BS_DEV_BAD_LENGTH, 0, lib.BS_DEV_BAD_LENGTH]

@@ -41,11 +41,42 @@ def test_more_kept_than_granted_is_a_bad_length():
     assert r["status"].tolist() == [oc.BAD_LENGTH, 0] and r["seq_len"].tolist() == [3, 7]
 
 
+@pytest.mark.parametrize("seed", range(10))
+def test_shared_blocks_are_nobodys_to_return(seed):
+    """Sequences behind a common prefix come and go: its blocks never reach the stack, every other block has one place."""
+    rng = np.random.default_rng(seed)
+    B, bt, W, nb, sh = 5, 16, 32, 30, 2
+    prefix = [7, 3]
+    table = np.full((B, W), -1)
+    table[:, :sh] = prefix
+    seq, held, free, cu, kept = np.full(B, sh * bt), np.full(B, sh), [b for b in range(nb) if b not in prefix], None, None
+    for _ in range(15):
+        shared = np.full(B, sh)
+        r = oc.plan(seq, kept, rng.integers(0, 30, B), 0, None, bt, table, held, free, 500, cu, shared)
+        seq, held, table, free, cu = r["seq_len"], r["held"], r["table"], r["free"], r["cu_new"]
+        assert not (r["status"] & oc.BAD_LENGTH).any() and (table[:, :sh] == prefix).all()
+        used = [int(x) for b in range(B) for x in table[b, sh:held[b]]] + [int(x) for x in free]
+        assert sorted(used + prefix) == list(range(nb))
+        kept = np.minimum(np.diff(cu), rng.integers(0, 30, B))
+        for b in np.nonzero(rng.random(B) < 0.3)[0]:      # it ends; the next one begins behind the same prefix
+            seq[b], kept[b] = sh * bt, 0
+    # all end, the last reader lets go: every block is back
+    r = oc.plan(np.zeros(B, int), None, np.zeros(B, int), 0, None, bt, table, held, free, 1, None, np.array([0] + [sh] * (B - 1)))
+    assert sorted(int(x) for x in r["free"]) == list(range(nb)) and r["held"].tolist() == [0] + [sh] * (B - 1)
+
+
+def test_new_tokens_inside_shared_blocks_are_a_bad_length():
+    table = np.array([[0, 1], [0, 1], [0, 2], [0, -1]])
+    r = oc.plan(np.array([16, 15, 31, 0]), None, np.array([1, 1, 0, 1]), 0, None, 16, table, np.array([1, 1, 2, 0]), [5, 6], 8, None,
+                np.array([1, 1, 2, 1]))
+    assert r["status"].tolist() == [0, oc.BAD_LENGTH, 0, oc.BAD_LENGTH]
+
+
 def test_plan_next_refuses(lib):
     f = lib._lib.bs_cache_plan_next
 
-    def call(seq=P, last=P, new=P, extra=1, B=4, bt=16, table=P, W=8, held=P, free=P, nb=64, nfree=P, kv=P, cu=P, slots=P, T=16):
-        return f(seq, None, last, new, extra, None, B, bt, table, W, held, free, nb, nfree, kv, cu, slots, None, T, None, None)
+    def call(seq=P, last=P, shared=P, new=P, extra=1, B=4, bt=16, table=P, W=8, held=P, free=P, nb=64, nfree=P, kv=P, cu=P, slots=P, T=16):
+        return f(seq, None, last, shared, new, extra, None, B, bt, table, W, held, free, nb, nfree, kv, cu, slots, None, T, None, None)
 
     for kw in ({"seq": None}, {"new": None}, {"table": None}, {"held": None}, {"free": None}, {"nfree": None}, {"kv": None},
                {"cu": None}, {"slots": None}, {"B": 0}, {"W": 0}, {"nb": 0}, {"T": 0}, {"extra": -1}):

@@ -303,6 +303,9 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_co
             }
             // ---- end of the item, or of this CTA's part of it: the sums of the groups ----
             if (ok) ok = ca_wait(smem_u32(&b_l[buf]), (uint32_t)((item >> 1) & 1)) && !__any_sync(0xffffffffu, s_abort);
+            // A wait that gave up leaves `ok` false in its warp only; the four leave together, here.  Behind it all of them have
+            // seen b_l, so what they read below is the same for each and they meet at the barriers that depend on it.
+            if (ca_bar_any(1 + NG, 128, !ok)) { ok = false; break; }
 #pragma unroll
             for (int i = 0; i < (N + 31) / 32; ++i) {
                 const int r = i * 32 + lane;
@@ -325,7 +328,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_co
 #pragma unroll
                             for (int i = 0; i < 16; ++i) y[i] = i == r ? __int_as_float(0x7fc00000) : y[i];
             };
-            bool write = ok, joined = false;
+            bool write = true, joined = false;
             long long c_first = 0, c_last = 0;
             if (nt < cur.ntiles) {
                 // part of an item: leave it in the workspace; the CTA that completes the item joins the parts
@@ -350,7 +353,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_co
                             part[N * D + N + i * 32 + lane] = l_run[i];
                         }
                 __threadfence();
-                if (ca_bar_any(1 + NG, 128, !ok)) { ok = false; break; }
+                ca_bar_any(1 + NG, 128, false);
                 if (wq == 0 && lane == 0) {
                     const uint32_t old = atomicAdd(p.ticket + c_first, 1u);
                     const bool last = old == (uint32_t)(c_last - c_first);

@@ -279,6 +279,10 @@ cache_attention_rows_kernel(const __grid_constant__ CUtensorMap tm_k, const __gr
             }
             // ---- end of the item, or of this CTA's part of it: the sums of the teams ----
             if (ok) ok = ca_wait(smem_u32(&b_l[buf]), (uint32_t)((item >> 1) & 1)) && !__any_sync(0xffffffffu, s_abort);
+            // A wait that gave up leaves `ok` false in its warp only; the four leave together, here.  Behind it all of them have
+            // seen b_l, so what they read below is the same for each and they meet at the barriers that depend on it; and the
+            // item before has been read out of the merge buffer.
+            if (ca_bar_any(1, 128, !ok)) { ok = false; break; }
             float l_run = 0.f;
 #pragma unroll
             for (int u = 0; u < 2; ++u)
@@ -300,7 +304,6 @@ cache_attention_rows_kernel(const __grid_constant__ CUtensorMap tm_k, const __gr
             };
             float f0 = 1.f, f1 = 0.f;                         // factors of the halves
             if (L::kHalves > 1) {
-                if (ca_bar_any(1, 128, !ok)) { ok = false; break; }   // the item before has been read out of the merge buffer
                 if (half) {
 #pragma unroll 1
                     for (int c = 0; c < D; c += 16) {
@@ -334,7 +337,7 @@ cache_attention_rows_kernel(const __grid_constant__ CUtensorMap tm_k, const __gr
                 }
             };
             const bool leads = half == 0;                     // these warps write the result
-            bool write = ok, joined = false;
+            bool write = true, joined = false;
             int c_first = 0, c_last = 0;
             if (nt < cur.ntiles) {
                 // part of an item: leave it in the workspace; the CTA that completes the item joins the parts
@@ -356,7 +359,7 @@ cache_attention_rows_kernel(const __grid_constant__ CUtensorMap tm_k, const __gr
                     part[R * D + R + row] = l_run;
                 }
                 __threadfence();
-                if (ca_bar_any(1, 128, !ok)) { ok = false; break; }
+                ca_bar_any(1, 128, false);
                 if (wq == 0 && lane == 0) {
                     const uint32_t old = atomicAdd(p.ticket + c_first, 1u);
                     const bool last = old == (uint32_t)(c_last - c_first);

@@ -368,7 +368,7 @@ __device__ __forceinline__ void ca_give_up(const CacheAttnParams& p, volatile in
 template <int D, uint32_t RING>
 __device__ __forceinline__ void ca_produce(const CacheAttnParams& p, CaCursor cur, int kv, const CUtensorMap* tm, unsigned char* ring,
                                            unsigned long long* b_full, unsigned long long* b_empty, unsigned long long* b_scale,
-                                           float (*s_scale)[kCaMaxPages][2], volatile int* s_abort) {
+                                           float (*s_scale)[kCaMaxPages][2], uint32_t* s_tiles, volatile int* s_abort) {
     const int lane = threadIdx.x & 31;
     const uint32_t elected = ca_elect();
     uint32_t slot = 0, ph = 0, tile = 0;
@@ -424,14 +424,26 @@ __device__ __forceinline__ void ca_produce(const CacheAttnParams& p, CaCursor cu
         n_tiles = next_tiles;
         ids = next_ids;
     }
-    if (!ok) {                                                // leave no copy in flight behind
-        if (lane == 0) {
-            ca_give_up(p, s_abort);
-#pragma unroll 1
-            for (uint32_t f = tile > RING ? tile - RING : 0u; f < tile; ++f) mbar_wait(smem_u32(b_full + f % RING), (f / RING) & 1);
-        }
-        __syncwarp();
+    if (lane == 0) {
+        s_tiles[kv] = tile;
+        if (!ok) ca_give_up(p, s_abort);
     }
+    __syncwarp();
+}
+// After a wait that gave up, behind the barrier at which all roles meet: nothing is issued any more, and nothing may be left
+// in flight that writes this CTA's shared or tensor memory, whichever role it was that gave up.  Every wait is bounded.
+template <uint32_t RING>
+__device__ __noinline__ void ca_drain(int warp, unsigned long long (*b_full)[RING], const uint32_t* s_tiles, unsigned long long* b_drain) {
+    if (warp < 2) {
+        const uint32_t tiles = s_tiles[warp];
+#pragma unroll 1
+        for (uint32_t f = tiles > RING ? tiles - RING : 0u; f < tiles; ++f) ca_wait(smem_u32(&b_full[warp][f % RING]), (f / RING) & 1);
+        asm volatile("cp.async.wait_all;" ::: "memory");      // scales
+    } else if (warp == 2) {
+        ca_commit(smem_u32(b_drain), ca_elect());
+        ca_wait(smem_u32(b_drain), 0);
+    }
+    __syncwarp();
 }
 template <uint32_t RING>
 __device__ __forceinline__ void ca_init_rings(unsigned long long (*b_full)[RING], unsigned long long (*b_empty)[RING],

@@ -94,6 +94,7 @@ cache_attention_rows_kernel(const __grid_constant__ CUtensorMap tm_k, const __gr
     __shared__ uint32_t s_tmem;
     __shared__ volatile int s_abort;
     __shared__ int s_last;
+    __shared__ uint32_t s_tiles[2];                           // tiles whose copies the producers have issued
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     if (tid == 0) {
@@ -128,7 +129,7 @@ cache_attention_rows_kernel(const __grid_constant__ CUtensorMap tm_k, const __gr
 
     if (warp < 2) {
         // K: warp 0, V: warp 1
-        ca_produce<D, RING>(p, cur, warp, warp ? &tm_v : &tm_k, smem + warp * RING * L::kTileBytes, b_full[warp], b_empty[warp], b_scale, s_scale, &s_abort);
+        ca_produce<D, RING>(p, cur, warp, warp ? &tm_v : &tm_k, smem + warp * RING * L::kTileBytes, b_full[warp], b_empty[warp], b_scale, s_scale, s_tiles, &s_abort);
     } else if (warp == 2) {
         // ================================= MMA issuer =================================
         // S of tiles 0 and 1, then, whenever the probabilities of a tile are there: S of the tile two further on, whose
@@ -196,12 +197,7 @@ cache_attention_rows_kernel(const __grid_constant__ CUtensorMap tm_k, const __gr
                 }
             }
         }
-        if (!ok) {
-            if (lane == 0) ca_give_up(p, &s_abort);
-            __syncwarp();
-            ca_commit(smem_u32(&b_drain), elected);           // leave no MMA in flight behind
-            ca_wait(smem_u32(&b_drain), 0);
-        }
+        if (!ok && lane == 0) ca_give_up(p, &s_abort);
         __syncwarp();
     } else if (warp == 3) {
         // nothing: warps 4-7 have to be the four quarters of tensor memory
@@ -659,6 +655,7 @@ cache_attention_rows_kernel(const __grid_constant__ CUtensorMap tm_k, const __gr
     __syncwarp();
     tc_fence_before();
     __syncthreads();
+    if (s_abort) ca_drain<RING>(warp, b_full, s_tiles, &b_drain);
     if (warp == 2) {
         tc_fence_after();
         tc_free(tmem, L::kTmemCols);

@@ -32,3 +32,18 @@ def test_accumulator_warps_leave_together_before_they_branch_on_the_marks(name):
     rest = src[at.end():]
     assert "ok" not in re.findall(r"\bok\b", rest[:rest.index("mbar_arrive(smem_u32(&b_lfree")])
     assert not vote.search(rest)
+
+
+@pytest.mark.parametrize("name", KERNELS)
+def test_nothing_is_in_flight_when_a_cta_that_gave_up_ends(name):
+    """A producer that had issued its last copy, or an issuer its last product, before another role gave up has left its own loop:
+    the drain has to come behind the barrier at which all roles meet, and before tensor memory goes back."""
+    src = re.sub(r"//[^\n]*", "", open(os.path.join(CSRC, name)).read())
+    end = src[:src.index("tc_free(")].rindex("__syncthreads();")
+    assert re.search(r"if \(s_abort\) ca_drain<RING>\(warp, b_full, s_tiles, &b_drain\);", src[end:src.index("tc_free(")])
+    head = re.sub(r"//[^\n]*", "", open(os.path.join(CSRC, "bs_cache_attention.cuh")).read())
+    body = head[head.index("void ca_drain("):]
+    body = body[:body.index("\n}\n")]
+    assert body.index("warp < 2") < body.index("b_full[warp]") < body.index("cp.async.wait_all") < body.index("warp == 2") < body.index("ca_commit")
+    produce = head[head.index("void ca_produce("):head.index("void ca_drain(")]
+    assert "s_tiles[kv] = tile;" in produce and "mbar_wait" not in produce

@@ -53,7 +53,7 @@ typedef enum {
     BS_ERR_CUDA = 2,          /* a CUDA runtime call or launch failed */
     BS_ERR_UNSUPPORTED = 3,   /* valid request outside the implemented limits */
     BS_ERR_WORKSPACE = 4,     /* workspace too small or misaligned */
-    BS_ERR_TIMEOUT = 5,       /* bs_get_device_status: a bounded wait inside a kernel gave up */
+    BS_ERR_TIMEOUT = 5,       /* bs_get_device_status, bs_cache_get_device_status: a bounded wait inside a kernel gave up */
     BS_ERR_DEVICE_DATA = 6    /* bs_get_device_status: some sequence carries a data error */
 } bs_status;
 
@@ -76,7 +76,8 @@ typedef enum { BS_UCB = 0, BS_EXP3 = 1, BS_UCB_REWARD = 2 } bs_alg;
 #define BS_DEV_NO_ROOM       256   /* bs_cache_plan: its tokens do not fit slot_map; the sequence got no new tokens */
 #define BS_DEV_BAD_BLOCK     512   /* bs_cache_attention / bs_cache_keep_path: a block id outside [0, n_blocks) */
 #define BS_DEV_TIMEOUT       1024  /* bs_cache_attention: a bounded wait gave up; every output of the call is undefined and
-                                      its workspace has to be cleared with bs_workspace_init */
+                                      its workspace has to be cleared with bs_workspace_init.  Set in status[0]; without
+                                      a status array bs_cache_get_device_status still tells */
 
 /* Limits of this implementation. */
 #define BS_MAX_GAMMA   31      /* Gmax <= 31 (one warp scans the accept flags) */
@@ -426,6 +427,10 @@ bs_status bs_cache_append(const void* k, const void* v, bs_dtype dtype, long lon
 /* Bytes of scratch bs_cache_attention needs on the current device for these heads (any batch and length);
  * 0 for unsupported ones.  Clear it once with bs_workspace_init. */
 size_t bs_cache_workspace_bytes(int Hq, int Hkv, int d);
+
+/* Whether a bounded wait gave up in any bs_cache_attention on this workspace since it was cleared: BS_ERR_TIMEOUT, else
+ * BS_OK.  Synchronises `stream`.  Clear the workspace with bs_workspace_init before it is used again. */
+bs_status bs_cache_get_device_status(const void* workspace, size_t workspace_bytes, void* stream);
 
 /* Attention of the new tokens over the cache: out_i = sum_j softmax_j(softmax_scale * q_i . k_j) v_j.
  *

@@ -57,6 +57,7 @@ SIGNATURES = {
     "bs_cache_plan_next": (_i, [_vp, _vp, _vp, _vp, _vp, _i, _vp, _i, _i, _vp, _i, _vp, _vp, _i, _vp, _vp, _vp, _vp, _vp, _i, _vp, _vp]),
     "bs_cache_append": (_i, [_vp, _vp, _i, _ll, _ll, _ll, _ll, _vp, _i, _i, _i, _vp, _vp, _vp, _vp, _i, _i, _vp]),
     "bs_cache_workspace_bytes": (_sz, [_i, _i, _i]),
+    "bs_cache_get_device_status": (_i, [_vp, _sz, _vp]),
     "bs_cache_attention": (_i, [_vp, _ll, _ll, _vp, _vp, _vp, _i, _vp, _i, _vp, _vp, _vp, _vp, _i, _i, _i, _i, _i, _i, _i,
                                 _i, _f, _vp, _ll, _ll, _vp, _vp, _sz, _vp]),
     "bs_cache_keep_path": (_i, [_vp, _vp, _vp, _i, _i, _vp, _i, _i, _i, _vp, _vp, _vp, _vp, _i, _i, _vp, _vp]),
@@ -396,6 +397,13 @@ def new_cache_workspace(Hq: int, Hkv: int, d: int, device="cuda") -> torch.Tenso
         ws = torch.empty(n, dtype=torch.uint8, device=device)
         bs_workspace_init(ws)
     return ws
+
+
+def bs_cache_get_device_status(workspace, stream=None) -> None:
+    """Raises BanditSpecError (BS_ERR_TIMEOUT) if a bounded wait gave up in an attention on this workspace since it was cleared
+    (synchronises)."""
+    _call(_lib.bs_cache_get_device_status, "bs_cache_get_device_status", workspace.device, stream,
+          workspace.data_ptr(), workspace.numel())
 
 
 def bs_cache_attention(q, cu_new, kv_len, block_table, node_parent, k_cache, k_scale, v_cache, v_scale, max_new: int,

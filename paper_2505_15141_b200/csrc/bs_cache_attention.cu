@@ -680,7 +680,8 @@ static bs_status launch_ca(const CUtensorMap* tm, const CacheAttnParams& p, cuda
     return cuda_status(launch_pdl(kern, sm_count(), L::kThreads, L::kDynamic, st, tm[0], tm[1], p));
 }
 
-static size_t ca_ticket_bytes() { return align_up(sizeof(uint32_t) * (size_t)sm_count(), 256); }
+// Workspace: an arrival counter per CTA and behind them the abort word, then the parts of items.
+static size_t ca_ticket_bytes() { return align_up(sizeof(uint32_t) * ((size_t)sm_count() + 1), 256); }
 
 }  // namespace bs
 
@@ -689,6 +690,18 @@ using namespace bs;
 extern "C" size_t bs_cache_workspace_bytes(int Hq, int Hkv, int d) {
     if (Hkv < 1 || Hq < Hkv || Hq % Hkv || Hq / Hkv > 64 || (d != 64 && d != 128)) return 0;
     return ca_ticket_bytes() + align_up(sizeof(float) * 2 * (size_t)sm_count() * kCaMaxRows * (d + 2), 256);
+}
+
+extern "C" bs_status bs_cache_get_device_status(const void* workspace, size_t workspace_bytes, void* stream) {
+    if (!workspace) return BS_ERR_INVALID_ARG;
+    if ((reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < ca_ticket_bytes()) return BS_ERR_WORKSPACE;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    uint32_t aborted = 0;
+    cudaError_t e = cudaMemcpyAsync(&aborted, static_cast<const uint32_t*>(workspace) + sm_count(), sizeof(aborted),
+                                    cudaMemcpyDeviceToHost, st);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(st);
+    if (e != cudaSuccess) return cuda_status(e);
+    return aborted ? BS_ERR_TIMEOUT : BS_OK;
 }
 
 extern "C" bs_status bs_cache_attention(const void* q, long long q_stride_t, long long q_stride_h, const int32_t* cu_new,
@@ -719,6 +732,7 @@ extern "C" bs_status bs_cache_attention(const void* q, long long q_stride_t, lon
     p.cu_new = cu_new; p.kv_len = kv_len; p.block_table = block_table; p.node_parent = node_parent;
     p.k_scale = k_scale; p.v_scale = v_scale; p.status = status;
     p.ticket = static_cast<uint32_t*>(workspace);
+    p.abort = p.ticket + sm_count();
     p.partial = reinterpret_cast<float*>(static_cast<char*>(workspace) + ca_ticket_bytes());
     p.scale_log2 = softmax_scale * kLog2e;
     p.B = B; p.T = T; p.W = max_blocks; p.Nmax = Nmax; p.Hq = Hq; p.Hkv = Hkv; p.G = Hq / Hkv;

@@ -33,6 +33,7 @@ struct CacheAttnParams {
     int32_t* status;
     float* partial;                            // [grid, 2] pieces
     uint32_t* ticket;                          // [grid] arrivals at an item, kept by its first CTA; zero between calls
+    volatile uint32_t* abort;                  // [1] set when a wait gave up, cleared with the workspace
     float scale_log2;                          // softmax_scale * log2(e)
     int B, T, W, Nmax, Hq, Hkv, G, TQ;         // TQ: new tokens of an item, N / G
     int bt_log2, n_blocks;
@@ -358,6 +359,7 @@ __device__ __forceinline__ void ca_advance(const CacheAttnParams& p, CaCursor& c
 }
 __device__ __forceinline__ void ca_give_up(const CacheAttnParams& p, volatile int* s_abort) {   // one thread
     *s_abort = 1;
+    *p.abort = 1u;
     if (p.status) atomicOr(p.status, BS_DEV_TIMEOUT);
 }
 

@@ -47,3 +47,13 @@ def test_nothing_is_in_flight_when_a_cta_that_gave_up_ends(name):
     assert body.index("warp < 2") < body.index("b_full[warp]") < body.index("cp.async.wait_all") < body.index("warp == 2") < body.index("ca_commit")
     produce = head[head.index("void ca_produce("):head.index("void ca_drain(")]
     assert "s_tiles[kv] = tile;" in produce and "mbar_wait" not in produce
+
+
+def test_a_time_out_is_kept_where_the_host_can_read_it(lib):
+    head = open(os.path.join(CSRC, "bs_cache_attention.cuh")).read()
+    give_up = head[head.index("void ca_give_up("):]
+    assert "*p.abort = 1u;" in give_up[:give_up.index("\n}\n")]
+    f = lib._lib.bs_cache_get_device_status
+    assert f(None, 1 << 20, None) == lib.BS_ERR_INVALID_ARG
+    assert f(4096 + 16, 1 << 20, None) == lib.BS_ERR_WORKSPACE
+    assert f(4096, 64, None) == lib.BS_ERR_WORKSPACE

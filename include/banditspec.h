@@ -447,7 +447,10 @@ bs_status bs_cache_get_device_status(const void* workspace, size_t workspace_byt
  * Keys and values enter the tensor cores as the e4m3 codes they are; a bf16 query is split into two e4m3 numbers, which
  * holds it exactly down to 2^-9 of its row's largest element; probabilities are split the same way, relative error at
  * most 2^-8 where they are within 2^-10 of the largest of their 128-token tile and absolute error 2^-18 of that
- * below.  Products accumulate in fp32, tiles are joined in fp32.  Scales of V within a tile should lie within 2^126 of one another.
+ * below.  Products accumulate in fp32, tiles are joined in fp32.
+ * Range of the scales, which need not be powers of two: those of K at most 2^100, and softmax_scale x largest |q| of a row x scale of
+ * K below 2^120; those of V from 2^-64 to 2^100, and the ones that a sequence reads within 2^96 of one another.  Outside it results
+ * are undefined.  (bs_cache_append writes 2^-64 and more, and more than 2^100 only for values above 5e32.)
  * A token that sees nothing (kv_len < its position) gets zeros.  Rows of out behind cu_new[B] are left as they are, and so
  * are the rows of a sequence with BS_DEV_BAD_LENGTH (lengths outside the block table, cu_new not ascending or
  * above T; trees: more than Nmax + 1 new tokens).  BS_DEV_BAD_BLOCK: the rows of that sequence are undefined.

@@ -501,7 +501,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_co
                     }
                     if (vis) {
                         const float* sc = s_scale[k % kCaScaleRing][tok >> p.bt_log2];
-                        const float sv = fmaxf(sc[1], 5.421010862e-20f);    // 2^-64
+                        const float sv = fmaxf(sc[1], kCaMinScaleV);
                         ks = sc[0];
                         lsv = __log2f(sv);
                         isv = __fdividef(1.f, sv);

@@ -15,6 +15,7 @@ constexpr int kCaSmem = 230400;                // of 232448 bytes a CTA may use
 constexpr int kCaScaleRing = 8;                // tiles whose scales are kept; more than the tiles in flight
 constexpr int kCaMaxPages = 8;                 // blocks of 16 tokens in a tile
 constexpr int kCaMaxRows = 128;                // rows of an item, at most
+constexpr float kCaMinScaleV = 5.421010862e-20f;   // 2^-64, the smallest scale of V that the header allows
 // What an item costs besides its tiles (queries, joining, results), in tiles, when the work is cut into shares.  Measured with
 // 1, 2, 4 and 6: prompt pieces of 1 to 36 tiles 186, 152, 141, 139 us, trees on 1 to 33 tiles 177, 161, 153, 149 us, long
 // items the same.

@@ -502,7 +502,7 @@ cache_attention_rows_kernel(const __grid_constant__ CUtensorMap tm_k, const __gr
                 }
                 if (lane < 8) {
                     const float* z = s_scale[k % kCaScaleRing][(lane * 16) >> p.bt_log2];
-                    const float sv = fmaxf(z[1], 5.421010862e-20f);   // 2^-64
+                    const float sv = fmaxf(z[1], kCaMinScaleV);
                     s_tab[warp - 8][lane] = make_float4(z[0], __log2f(sv), __fdividef(1.f, sv), 0.f);
                 }
                 __syncwarp();

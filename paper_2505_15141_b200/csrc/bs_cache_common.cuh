@@ -13,8 +13,9 @@
 
 namespace bs {
 
-constexpr int kCacheMinExp = -64;      // smallest block scale 2^-64; kept within 2^126 of any scale a finite bf16
-                                       // or fp32 value of ordinary size needs (the attention divides by V scales)
+// Smallest block scale 2^-64.  The attention puts the scale of V into the exponent of a probability, where fp32 has room for
+// 2^96 between the scales of a sequence beside 2^30 between its probabilities: with this floor up to 2^32.
+constexpr int kCacheMinExp = -64;
 
 // The smallest power of two s >= 2^-64 with amax / s <= 448 (amax finite, >= 0).
 __device__ __forceinline__ float pow2_scale(float amax) {

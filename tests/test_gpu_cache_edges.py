@@ -25,3 +25,55 @@ def test_a_time_out_is_reported_without_a_status_array(lib):
     lib.bs_cache_get_device_status(ws, torch.cuda.current_stream())
     assert torch.equal(c.run(lib, ws=ws), want)
     lib.bs_cache_get_device_status(ws)
+
+
+LANES = [4, 8, 16, 40]                                    # with four query heads a key head: tiles of 16, 32, 64, 128 rows
+
+
+def _scales(c, i, f):
+    """Sets the scales of K (i = 0) or V (1): f(position of the block's first token, block) where a block is in use."""
+    for b, kv in enumerate(c.kv):
+        for j in range(-(-kv // c.bt)):
+            c.scales[i][c.table[b, j]] = f(j * c.bt, c.table[b, j])
+
+
+@pytest.mark.parametrize("max_new", LANES)
+@pytest.mark.parametrize("rising", [False, True])
+def test_scales_of_v_far_apart_in_different_tiles(lib, rising, max_new):
+    """2^96 between the tiles of a sequence: a tile whose values vanish beside another's still has its share of the softmax sum."""
+    c = Case(21, [400, 130, 3000], [4, 3, 2], 8, 2, 128, 16, q_mul=0.5)
+    _scales(c, 1, lambda pos, blk: 2.0 ** (-64 if (pos // 128 % 2 == 0) == rising else 32))
+    c.check(c.run(lib, max_new=max_new))
+
+
+@pytest.mark.parametrize("max_new", LANES)
+def test_scales_of_v_far_apart_in_one_tile(lib, max_new):
+    c = Case(22, [400, 130], [4, 3], 8, 2, 128, 16, q_mul=0.5)
+    _scales(c, 1, lambda pos, blk: 2.0 ** (-64 if pos // 16 % 2 else 32))
+    c.check(c.run(lib, max_new=max_new))
+
+
+@pytest.mark.parametrize("max_new", LANES)
+@pytest.mark.parametrize("e", [-64, 100])
+def test_scales_of_v_at_the_ends_of_their_range(lib, e, max_new):
+    c = Case(23, [400, 130, 3000], [4, 3, 2], 8, 2, 128, 16, q_mul=2.0)
+    _scales(c, 1, lambda pos, blk: 2.0 ** e)
+    c.check(c.run(lib, max_new=max_new))
+
+
+@pytest.mark.parametrize("max_new", LANES)
+@pytest.mark.parametrize("e", [-100, 100])
+def test_scales_of_k_and_queries_far_from_one(lib, e, max_new):
+    c = Case(24, [400, 130], [4, 3], 8, 2, 128, 16, q_mul=2.0 ** (-6 - e))
+    _scales(c, 0, lambda pos, blk: 2.0 ** e)
+    c.check(c.run(lib, max_new=max_new))
+
+
+@pytest.mark.parametrize("max_new", LANES)
+@pytest.mark.parametrize("d", [64, 128])
+def test_scales_that_are_no_powers_of_two(lib, d, max_new):
+    c = Case(25, [400, 130, 77], [4, 3, 5], 8, 2, d, 16, q_mul=2.0, spread=2.0)
+    rng = np.random.default_rng(25)
+    for s in c.scales:
+        s *= rng.uniform(1.0, 2.0, s.shape).astype(np.float32)
+    c.check(c.run(lib, max_new=max_new))

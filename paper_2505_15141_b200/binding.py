@@ -344,9 +344,13 @@ def _call(fn, where: str, device: torch.device, stream, *args) -> None:
         raise BanditSpecError(code, where)
 
 
+_CODES = (torch.float8_e4m3fn, torch.uint8)
+
+
 def _cache_args(k_cache, k_scale, v_cache, v_scale):
     shape = k_cache.shape
-    assert k_cache.element_size() == 1 and v_cache.element_size() == 1 and v_cache.shape == shape
+    assert k_cache.dtype in _CODES and v_cache.dtype in _CODES, f"codes must be float8_e4m3fn, or uint8 that holds them, got {k_cache.dtype}, {v_cache.dtype}"
+    assert v_cache.shape == shape
     assert k_scale.dtype is torch.float32 and v_scale.dtype is torch.float32 and k_scale.shape == v_scale.shape == shape[:2]
     assert k_cache.is_contiguous() and v_cache.is_contiguous() and k_scale.is_contiguous() and v_scale.is_contiguous()
     return shape

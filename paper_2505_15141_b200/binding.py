@@ -321,7 +321,8 @@ def bs_lmhead_verify(H_t, W_t, H_d, W_d, draft_tokens, gamma, u_accept, temperat
 
 # These calls are made once or more per layer: their checks are kept to a few attribute look-ups each.
 
-_raw_stream = torch._C._cuda_getCurrentRawStream
+# The current stream's handle without building a Stream object; where torch lacks this name (a build without CUDA), the long way.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
 def _i32(t, n: int) -> Optional[int]:

@@ -325,36 +325,47 @@ def bs_lmhead_verify(H_t, W_t, H_d, W_d, draft_tokens, gamma, u_accept, temperat
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
-def _i32(t, n: int) -> Optional[int]:
-    """Pointer of a contiguous int32 tensor of n elements (None stays NULL)."""
+def _i32(t, n: int, index: Optional[int] = None) -> Optional[int]:
+    """Pointer of a contiguous int32 tensor of n elements, on GPU `index` if that is given (None stays NULL)."""
     if t is None:
         return None
-    assert t.dtype is torch.int32 and t.numel() == n and t.is_contiguous(), f"contiguous int32 of {n} elements expected, got {t.dtype} {tuple(t.shape)}"
+    assert t.dtype is _int32 and t.numel() == n and t.is_contiguous(), f"contiguous int32 of {n} elements expected, got {t.dtype} {tuple(t.shape)}"
+    assert index is None or t.get_device() == index, f"every tensor of a call has to be on its GPU {index}, got {t.device}"
     return t.data_ptr()
 
 
-def _call(fn, where: str, device: torch.device, stream, *args) -> None:
-    """fn(*args, stream) with the tensors' device current, on `stream` or that device's current stream."""
-    index = device.index
+def _gpu(index: int, *tensors) -> int:
+    """`index` if it is a GPU's and all tensors are there: a pointer into other memory would fault in the kernel."""
+    assert index >= 0, "the tensors have to be on a GPU"
+    for t in tensors:
+        assert t.get_device() == index, f"every tensor of a call has to be on its GPU {index}, got {t.device}"
+    return index
+
+
+def _call(fn, where: str, index: int, stream, *args) -> None:
+    """fn(*args, stream) with GPU `index` current, on `stream` or that GPU's current stream."""
     if index == torch.cuda.current_device():
         code = fn(*args, _raw_stream(index) if stream is None else stream.cuda_stream)
     else:
-        with torch.cuda.device(device):
+        with torch.cuda.device(index):
             code = fn(*args, _raw_stream(index) if stream is None else stream.cuda_stream)
     if code != BS_OK:
         raise BanditSpecError(code, where)
 
 
-_CODES = (torch.float8_e4m3fn, torch.uint8)
+_CODES, _f32, _int32 = (torch.float8_e4m3fn, torch.uint8), torch.float32, torch.int32
 
 
 def _cache_args(k_cache, k_scale, v_cache, v_scale):
-    shape = k_cache.shape
+    """The caches' GPU and shape: index, n_blocks, Hkv, block_tokens, d."""
     assert k_cache.dtype in _CODES and v_cache.dtype in _CODES, f"codes must be float8_e4m3fn, or uint8 that holds them, got {k_cache.dtype}, {v_cache.dtype}"
-    assert v_cache.shape == shape
-    assert k_scale.dtype is torch.float32 and v_scale.dtype is torch.float32 and k_scale.shape == v_scale.shape == shape[:2]
+    shape = k_cache.shape
+    n, H, bt, d = shape
+    blocks = (n, H)
+    assert v_cache.shape == shape and k_scale.shape == blocks and v_scale.shape == blocks
+    assert k_scale.dtype is _f32 and v_scale.dtype is _f32
     assert k_cache.is_contiguous() and v_cache.is_contiguous() and k_scale.is_contiguous() and v_scale.is_contiguous()
-    return shape
+    return _gpu(k_cache.get_device(), k_scale, v_cache, v_scale), n, H, bt, d
 
 
 def new_cache(n_blocks: int, Hkv: int, block_tokens: int, d: int, device="cuda"):
@@ -371,26 +382,28 @@ def bs_cache_plan(seq_len, kept, n_new, extra: int, active, block_tokens: int, b
     refused keeps none.  n_shared: leading blocks of each sequence that it shares with others and that are never returned."""
     B, W = block_table.shape
     n_blocks, T = free_blocks.numel(), slot_map.numel()
+    index = _gpu(seq_len.get_device(), *(() if active is None else (active,)))
     assert active is None or (active.dtype is torch.uint8 and active.numel() == B and active.is_contiguous())
     fn, more = _lib.bs_cache_plan, ()
     if last_cu is not None or n_shared is not None:
-        fn, more = _lib.bs_cache_plan_next, (_i32(last_cu, B + 1), _i32(n_shared, B))
-    _call(fn, "bs_cache_plan", seq_len.device, stream, _i32(seq_len, B), _i32(kept, B), *more, _i32(n_new, B), extra,
-          None if active is None else active.data_ptr(), B, block_tokens, _i32(block_table, B * W), W, _i32(n_held, B),
-          _i32(free_blocks, n_blocks), n_blocks, _i32(n_free, 1), _i32(kv_len, B), _i32(cu_new, B + 1), _i32(slot_map, T),
-          _i32(positions, T), T, _i32(status, B))
+        fn, more = _lib.bs_cache_plan_next, (_i32(last_cu, B + 1, index), _i32(n_shared, B, index))
+    _call(fn, "bs_cache_plan", index, stream, _i32(seq_len, B, index), _i32(kept, B, index), *more, _i32(n_new, B, index), extra,
+          None if active is None else active.data_ptr(), B, block_tokens, _i32(block_table, B * W, index), W, _i32(n_held, B, index),
+          _i32(free_blocks, n_blocks, index), n_blocks, _i32(n_free, 1, index), _i32(kv_len, B, index), _i32(cu_new, B + 1, index), _i32(slot_map, T, index),
+          _i32(positions, T, index), T, _i32(status, B, index))
 
 
 def bs_cache_append(k, v, slot_map, k_cache, k_scale, v_cache, v_scale, stream=None) -> None:
     """k, v [T, Hkv, d] (bf16 or fp32, last dimension contiguous) into their slots."""
-    n_blocks, Hkv, bt, d = _cache_args(k_cache, k_scale, v_cache, v_scale)
+    index, n_blocks, Hkv, bt, d = _cache_args(k_cache, k_scale, v_cache, v_scale)
     T = slot_map.numel()
+    _gpu(index, k, v)
     assert k.shape == v.shape == (T, Hkv, d) and k.dtype is v.dtype
     kt, kh, k1 = k.stride()
     vt, vh, v1 = v.stride()
     assert k1 == 1 and v1 == 1, "the last dimension must be contiguous"
-    _call(_lib.bs_cache_append, "bs_cache_append", k_cache.device, stream, k.data_ptr(), v.data_ptr(), _dtype_code(k), kt, kh, vt, vh,
-          _i32(slot_map, T), T, Hkv, d, k_cache.data_ptr(), k_scale.data_ptr(), v_cache.data_ptr(), v_scale.data_ptr(), n_blocks, bt)
+    _call(_lib.bs_cache_append, "bs_cache_append", index, stream, k.data_ptr(), v.data_ptr(), _dtype_code(k), kt, kh, vt, vh,
+          _i32(slot_map, T, index), T, Hkv, d, k_cache.data_ptr(), k_scale.data_ptr(), v_cache.data_ptr(), v_scale.data_ptr(), n_blocks, bt)
 
 
 def new_cache_workspace(Hq: int, Hkv: int, d: int, device="cuda") -> torch.Tensor:
@@ -407,7 +420,7 @@ def new_cache_workspace(Hq: int, Hkv: int, d: int, device="cuda") -> torch.Tenso
 def bs_cache_get_device_status(workspace, stream=None) -> None:
     """Raises BanditSpecError (BS_ERR_TIMEOUT) if a bounded wait gave up in an attention on this workspace since it was cleared
     (synchronises)."""
-    _call(_lib.bs_cache_get_device_status, "bs_cache_get_device_status", workspace.device, stream,
+    _call(_lib.bs_cache_get_device_status, "bs_cache_get_device_status", _gpu(workspace.get_device()), stream,
           workspace.data_ptr(), workspace.numel())
 
 
@@ -415,29 +428,30 @@ def bs_cache_attention(q, cu_new, kv_len, block_table, node_parent, k_cache, k_s
                        softmax_scale: float, out, status, workspace, stream=None) -> None:
     """q, out [T, Hq, d] bf16 (last dimension contiguous): attention of the new tokens over the cache.  node_parent
     None: chains; [B, Nmax] int32: trees of drafts."""
-    n_blocks, Hkv, bt, d = _cache_args(k_cache, k_scale, v_cache, v_scale)
+    index, n_blocks, Hkv, bt, d = _cache_args(k_cache, k_scale, v_cache, v_scale)
     B, W = block_table.shape
     T, Hq, dq = q.shape
+    _gpu(index, q, out, workspace)
     assert q.dtype is torch.bfloat16 and out.dtype is torch.bfloat16 and dq == d and out.shape == q.shape
     qt, qh, q1 = q.stride()
     ot, oh, o1 = out.stride()
     assert q1 == 1 and o1 == 1, "the last dimension must be contiguous"
     Nmax = 0 if node_parent is None else node_parent.shape[1]
-    _call(_lib.bs_cache_attention, "bs_cache_attention", k_cache.device, stream, q.data_ptr(), qt, qh, _i32(cu_new, B + 1),
-          _i32(kv_len, B), _i32(block_table, B * W), W, _i32(node_parent, B * Nmax), Nmax, k_cache.data_ptr(), k_scale.data_ptr(),
+    _call(_lib.bs_cache_attention, "bs_cache_attention", index, stream, q.data_ptr(), qt, qh, _i32(cu_new, B + 1, index),
+          _i32(kv_len, B, index), _i32(block_table, B * W, index), W, _i32(node_parent, B * Nmax, index), Nmax, k_cache.data_ptr(), k_scale.data_ptr(),
           v_cache.data_ptr(), v_scale.data_ptr(), n_blocks, bt, B, T, Hq, Hkv, d, max_new, softmax_scale, out.data_ptr(), ot, oh,
-          _i32(status, B), workspace.data_ptr(), workspace.numel())
+          _i32(status, B, index), workspace.data_ptr(), workspace.numel())
 
 
 def bs_cache_keep_path(out_nodes, accept_len, seq_len, block_table, k_cache, k_scale, v_cache, v_scale, status,
                        stream=None) -> None:
     """The accepted path of bs_tree_verify_greedy to the front of its tree."""
-    n_blocks, Hkv, bt, d = _cache_args(k_cache, k_scale, v_cache, v_scale)
+    index, n_blocks, Hkv, bt, d = _cache_args(k_cache, k_scale, v_cache, v_scale)
     B, W = block_table.shape
     Nmax = out_nodes.shape[1]
-    _call(_lib.bs_cache_keep_path, "bs_cache_keep_path", k_cache.device, stream, _i32(out_nodes, B * Nmax), _i32(accept_len, B),
-          _i32(seq_len, B), B, Nmax, _i32(block_table, B * W), W, Hkv, d, k_cache.data_ptr(), k_scale.data_ptr(), v_cache.data_ptr(),
-          v_scale.data_ptr(), n_blocks, bt, _i32(status, B))
+    _call(_lib.bs_cache_keep_path, "bs_cache_keep_path", index, stream, _i32(out_nodes, B * Nmax, index), _i32(accept_len, B, index),
+          _i32(seq_len, B, index), B, Nmax, _i32(block_table, B * W, index), W, Hkv, d, k_cache.data_ptr(), k_scale.data_ptr(), v_cache.data_ptr(),
+          v_scale.data_ptr(), n_blocks, bt, _i32(status, B, index))
 
 
 # ---- bandits ---------------------------------------------------------------------------

@@ -437,8 +437,11 @@ def bs_cache_attention(q, cu_new, kv_len, block_table, node_parent, k_cache, k_s
     ot, oh, o1 = out.stride()
     assert q1 == 1 and o1 == 1, "the last dimension must be contiguous"
     Nmax = 0 if node_parent is None else node_parent.shape[1]
+    parent = _i32(node_parent, B * Nmax, index)
+    if node_parent is not None and Nmax == 0:             # trees of a root alone: nothing to read, but NULL would mean chains
+        parent = kv_len.data_ptr()
     _call(_lib.bs_cache_attention, "bs_cache_attention", index, stream, q.data_ptr(), qt, qh, _i32(cu_new, B + 1, index),
-          _i32(kv_len, B, index), _i32(block_table, B * W, index), W, _i32(node_parent, B * Nmax, index), Nmax, k_cache.data_ptr(), k_scale.data_ptr(),
+          _i32(kv_len, B, index), _i32(block_table, B * W, index), W, parent, Nmax, k_cache.data_ptr(), k_scale.data_ptr(),
           v_cache.data_ptr(), v_scale.data_ptr(), n_blocks, bt, B, T, Hq, Hkv, d, max_new, softmax_scale, out.data_ptr(), ot, oh,
           _i32(status, B, index), workspace.data_ptr(), workspace.numel())
 

@@ -94,3 +94,15 @@ def test_every_tensor_has_to_be_on_the_calls_gpu(lib, monkeypatch, name):
     with pytest.raises(AssertionError, match="GPU"):         # all of them in host memory
         fn(*[place(x, -1) for x in args], **{k: place(x, -1) for k, x in kw.items()})
     assert len(made) == 1
+
+
+def test_trees_without_drafts_are_not_chains(lib, monkeypatch):
+    """An empty tensor has no address, and NULL means chains."""
+    seen = []
+    monkeypatch.setattr(lib, "_call", lambda fn, where, index, stream, *a: seen.append(a))
+    args, _ = _calls(lib)["bs_cache_attention"]
+    args[4] = torch.zeros(3, 0, dtype=torch.int32)
+    lib.bs_cache_attention(*[Placed(x) if isinstance(x, torch.Tensor) else x for x in args])
+    args[4] = None
+    lib.bs_cache_attention(*[Placed(x) if isinstance(x, torch.Tensor) else x for x in args])
+    assert seen[0][7] and seen[0][8] == 0 and seen[1][7] is None and seen[1][8] == 0

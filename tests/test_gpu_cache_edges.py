@@ -77,3 +77,13 @@ def test_scales_that_are_no_powers_of_two(lib, d, max_new):
     for s in c.scales:
         s *= rng.uniform(1.0, 2.0, s.shape).astype(np.float32)
     c.check(c.run(lib, max_new=max_new))
+
+
+@pytest.mark.parametrize("max_new", LANES)
+def test_trees_of_a_root_alone(lib, max_new):
+    c = Case(26, [100, 33, 4], [1, 2, 1], 8, 2, 128, 16)
+    c.parent = np.zeros((3, 0), int)
+    st = torch.zeros(3, dtype=torch.int32, device=DEV)
+    out = c.run(lib, max_new=max_new, status=st)
+    assert st.tolist() == [0, lib.BS_DEV_BAD_LENGTH, 0] and (out[1:3] == 7.0).all()
+    c.check(out, seqs=[0, 2])

@@ -87,3 +87,43 @@ def test_trees_of_a_root_alone(lib, max_new):
     out = c.run(lib, max_new=max_new, status=st)
     assert st.tolist() == [0, lib.BS_DEV_BAD_LENGTH, 0] and (out[1:3] == 7.0).all()
     c.check(out, seqs=[0, 2])
+
+
+@pytest.mark.parametrize("max_new", [1, 4, 8, 16, 40])
+@pytest.mark.parametrize("d", [64, 128])
+def test_trees_larger_than_max_new(lib, d, max_new):
+    """max_new chooses the tile: a tree's rows may fall into several of them."""
+    rng = np.random.default_rng(d)
+    new = [32, 7, 20, 1]
+    c = Case(27, [200, 90, 5, 128], new, 16, 4, d, 16, q_mul=2.0)
+    c.parent = np.array([[int(rng.integers(0, k)) for k in range(1, n)] + [0] * (32 - n) for n in new])
+    st = torch.zeros(4, dtype=torch.int32, device=DEV)
+    c.check(c.run(lib, max_new=max_new, status=st))
+    assert not st.any()
+
+
+@pytest.mark.parametrize("max_new", LANES)
+def test_bad_data_without_a_status_array(lib, max_new):
+    c = Case(28, [60, 200, 30, 40, 50], [3, 2, 4, 2, 4], 8, 2, 128, 16)
+    c.parent = np.array([[0, 1, 2]] * 4 + [[0, 9, -1]])
+    good = c.run(lib, max_new=max_new)                    # its last tree has bad parents
+    st = torch.zeros(5, dtype=torch.int32, device=DEV)
+    assert torch.equal(c.run(lib, max_new=max_new, status=st), good) and st.tolist() == [0, 0, 0, 0, lib.BS_DEV_BAD_TREE]
+    c.kv[1] = c.table.shape[1] * 16 + 1
+    c.table[2, 1] = -7
+    out = c.run(lib, max_new=max_new)
+    assert torch.equal(out[:3], good[:3]) and (out[3:5] == 7.0).all() and torch.equal(out[9:], good[9:])
+
+
+@pytest.mark.parametrize("B", [600, 1500, 4096])
+@pytest.mark.parametrize("max_new", LANES)
+def test_more_sequences_than_threads(lib, B, max_new):
+    """A thread looks after several sequences when the work is cut into shares; 4096 is the largest batch."""
+    rng = np.random.default_rng(B)
+    new = [int(n) for n in rng.integers(0, 4, B)]
+    c = Case(B, rng.integers(0, 70, B).tolist(), new, 4, 1, 64, 64, q_mul=2.0)
+    st, ws, dev = torch.zeros(B, dtype=torch.int32, device=DEV), lib.new_cache_workspace(4, 1, 64, DEV), c.device()
+    out = c.run(lib, max_new=max_new, status=st, ws=ws, dev=dev)
+    assert not st.any()
+    c.check(out, seqs=[0, 1, B - 2, B - 1] + sorted(int(b) for b in rng.integers(0, B, 60)))
+    assert torch.equal(c.run(lib, max_new=max_new, ws=ws, dev=dev), out)

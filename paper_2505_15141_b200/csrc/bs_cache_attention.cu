@@ -43,9 +43,8 @@
 
 namespace bs {
 
-// Sums of 16 per-lane values over the lanes of a warp: lanes 2j and 2j + 1 end with that of row ca_sum_row(lane).  Every
-// step halves the values and the lanes that hold them: 16 shuffles rather than 80.
-__device__ __forceinline__ int ca_sum_row(int lane) { return (lane >> 1 & 8) | (lane >> 1 & 4) | (lane >> 1 & 2) | (lane >> 1 & 1); }
+// Sums of 16 per-lane values over the lanes of a warp: lanes 2j and 2j + 1 end with that of row j.  Every step halves the
+// values and the lanes that hold them: 16 shuffles rather than 80.
 __device__ __forceinline__ float ca_row_sums16(float (&x)[16], int lane) {
 #pragma unroll
     for (int h = 8; h > 0; h >>= 1) {
@@ -73,12 +72,16 @@ template <int N, int D> struct CaLayout {
     static constexpr int kQBytes = N * D;                     // one term of the queries
     static constexpr int kPBytes = N * kCaTile;               // one term of the probabilities
     static constexpr int kFixed = 4 * kQBytes + 2 * kGroups * kPBytes;
-    // shared memory besides the rings: the static arrays of the kernel take up to 20 KB
-    static constexpr int kSlotsFit = (kCaSmem - 20480 - 1024 - kFixed) / kTileBytes;
+    // shared memory besides the rings: the kernel's static arrays, in the order of their declaration; then barriers and words
+    static constexpr int kStatic = 4 * N * (4 * kGroups + 4 * kGroups + 4 * kGroups + 2 * (4 * kGroups + 4) + 2 * kGroups) +
+                                   8 * 2 * kGroups * N + 4 * 2 * N + 4 * 2 * 32 + 8 * kCaScaleRing * kCaMaxPages +
+                                   4 * 2 * N * (D / 32) + (int)sizeof(CaShare) + 512;
+    static constexpr int kSlotsFit = (kCaSmem - 20480 - 1024 - kFixed) / kTileBytes;   // 20480: rings of 5 or 6 tiles
     static constexpr int kRing = kSlotsFit / 2 > 6 ? 6 : kSlotsFit / 2;   // tiles in the ring of K, and in that of V
     static constexpr int kDynamic = 2 * kRing * kTileBytes + kFixed + 1024;
     static constexpr int kPiece = N * D + 2 * N;              // floats of a partial result
     static_assert(kRing >= 3 && kRing + 2 <= kCaScaleRing, "ring");
+    static_assert(kStatic + kDynamic <= kCaSmem, "shared memory");
     static_assert(kColsUsed <= 512, "tensor memory");
     static_assert(N % 16 == 0 && N <= 32, "rows");
 };
@@ -247,23 +250,17 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_co
             const int buf = item & 1;
             const int nt = ca_tiles_here(cur);
             const int i0 = cur.rt * p.TQ, rows = min(p.TQ, cur.n - i0) * p.G;
-            float m_run[(N + 31) / 32], l_run[(N + 31) / 32]; // rows lane, lane + 32
-#pragma unroll
-            for (int i = 0; i < (N + 31) / 32; ++i) { m_run[i] = -INFINITY; l_run[i] = 0.f; }
+            float m_run = -INFINITY, l_run = 0.f;             // row `lane`
 #pragma unroll 1
             for (int t = 0; t < nt; ++t, ++k) {
                 const uint32_t g = k % NG, kk = k / NG;
                 if (ok) ok = ca_wait(smem_u32(&b_mt[g][kk & 1]), (kk >> 1) & 1) && !__any_sync(0xffffffffu, s_abort);
                 if (!ok) continue;
-#pragma unroll
-                for (int i = 0; i < (N + 31) / 32; ++i) {
-                    const int r = i * 32 + lane;
-                    if (r < N) {
-                        const float mt = s_mt[g][kk & 1][r], mn = fmaxf(m_run[i], mt);
-                        f_a[r] = mn == -INFINITY ? 1.f : ex2(m_run[i] - mn);
-                        f_b[r] = mn == -INFINITY ? 0.f : ex2(mt - mn) * 0.00390625f;
-                        m_run[i] = mn;
-                    }
+                if (lane < N) {
+                    const float mt = s_mt[g][kk & 1][lane], mn = fmaxf(m_run, mt);
+                    f_a[lane] = mn == -INFINITY ? 1.f : ex2(m_run - mn);
+                    f_b[lane] = mn == -INFINITY ? 0.f : ex2(mt - mn) * 0.00390625f;
+                    m_run = mn;
                 }
                 __syncwarp();
                 ok = ca_wait(smem_u32(&b_o[g]), kk & 1);
@@ -273,7 +270,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_co
                 for (int c = 0; c < N; c += 16) {
                     float x[16], old[16];
                     if (t) ca_ld16(t_acc + c, old);
-                    ca_result16<true>(t_lane + L::kColO + g * L::kCols + c, N, x);
+                    ca_result16(t_lane + L::kColO + g * L::kCols + c, N, x);
                     if (t) ca_ld16_wait(old);
 #pragma unroll
                     for (int i = 0; i < 16; i += 4) {
@@ -302,16 +299,12 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_co
             // A wait that gave up leaves `ok` false in its warp only; the four leave together, here.  Behind it all of them have
             // seen b_l, so what they read below is the same for each and they meet at the barriers that depend on it.
             if (ca_bar_any(1 + NG, 128, !ok)) { ok = false; break; }
+            if (lane < N)
 #pragma unroll
-            for (int i = 0; i < (N + 31) / 32; ++i) {
-                const int r = i * 32 + lane;
-                if (r < N)
-#pragma unroll
-                    for (int g = 0; g < NG; ++g) {
-                        const float2 x = s_ml[buf][g][r];
-                        l_run[i] += x.y * (x.x == -INFINITY ? 0.f : ex2(x.x - m_run[i]));
-                    }
-            }
+                for (int g = 0; g < NG; ++g) {
+                    const float2 x = s_ml[buf][g][lane];
+                    l_run += x.y * (x.x == -INFINITY ? 0.f : ex2(x.x - m_run));
+                }
             // 16 rows of the accumulator; results that a NaN of a masked tile belongs to
             const bool nans = s_nan_any[buf] != 0;
             auto acc16 = [&](int c, float (&y)[16]) {
@@ -341,13 +334,10 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_co
                         for (int r = 0; r < 16; ++r)
                             if (c + r < rows) part[(c + r) * D + dim] = y[r];
                 }
-                if (wq == 0)
-#pragma unroll
-                    for (int i = 0; i < (N + 31) / 32; ++i)
-                        if (i * 32 + lane < N) {
-                            part[N * D + i * 32 + lane] = m_run[i];
-                            part[N * D + N + i * 32 + lane] = l_run[i];
-                        }
+                if (wq == 0 && lane < N) {
+                    part[N * D + lane] = m_run;
+                    part[N * D + N + lane] = l_run;
+                }
                 __threadfence();
                 ca_bar_any(1 + NG, 128, false);
                 if (wq == 0 && lane == 0) {
@@ -360,34 +350,26 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_co
                 write = joined = s_last != 0;                 // written again only after a further barrier of the group
                 if (joined) {
                     __threadfence();
-                    // maxima and sums over the parts, for rows lane, lane + 32
-#pragma unroll
-                    for (int i = 0; i < (N + 31) / 32; ++i) {
-                        const int r = i * 32 + lane;
-                        float mm = -INFINITY, ll = 0.f;
-                        if (r < N)
+                    // maximum and sum of the row over the parts
+                    float mm = -INFINITY, ll = 0.f;
+                    if (lane < N)
 #pragma unroll 4
-                            for (int c = (int)c_first; c <= (int)c_last; ++c) {
-                                const float* q = p.partial + ((size_t)c * 2 + (c == c_first ? 1 : 0)) * L::kPiece + N * D;
-                                const float mc = __ldcg(q + r), lc = __ldcg(q + N + r);
-                                const float mn = fmaxf(mm, mc);
-                                ll = (mm == -INFINITY ? ll * 0.f : ll * ex2(mm - mn)) + (mc == -INFINITY ? lc * 0.f : lc * ex2(mc - mn));
-                                mm = mn;
-                            }
-                        m_run[i] = mm;
-                        l_run[i] = ll;
-                    }
+                        for (int c = (int)c_first; c <= (int)c_last; ++c) {
+                            const float* q = p.partial + ((size_t)c * 2 + (c == c_first ? 1 : 0)) * L::kPiece + N * D;
+                            const float mc = __ldcg(q + lane), lc = __ldcg(q + N + lane);
+                            const float mn = fmaxf(mm, mc);
+                            ll = (mm == -INFINITY ? ll * 0.f : ll * ex2(mm - mn)) + (mc == -INFINITY ? lc * 0.f : lc * ex2(mc - mn));
+                            mm = mn;
+                        }
+                    m_run = mm;
+                    l_run = ll;
                 }
             }
             if (write) {
                 __syncwarp();
-#pragma unroll
-                for (int i = 0; i < (N + 31) / 32; ++i) {
-                    const int r = i * 32 + lane;
-                    if (r < N) {
-                        f_a[r] = l_run[i] == 0.f ? 0.f : 1.f / l_run[i];   // nothing seen: zeros
-                        f_b[r] = m_run[i];
-                    }
+                if (lane < N) {
+                    f_a[lane] = l_run == 0.f ? 0.f : 1.f / l_run;   // nothing seen: zeros
+                    f_b[lane] = m_run;
                 }
                 __syncwarp();
                 __nv_bfloat16* o = p.out + (long long)(cur.q0 + i0) * p.o_st + (long long)cur.h * p.G * p.o_sh + dim;
@@ -462,9 +444,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_co
             const int seen = p.node_parent ? cur.base : cur.base + i0 + 1;
             // the accumulator is through with the item two before this one, which used the same sums and marks
             if (ok && item >= 2) ok = ca_wait(smem_u32(&b_lfree[buf]), (uint32_t)(((item >> 1) - 1) & 1));
-            float m_run[(N + 31) / 32];                       // running maxima of rows lane, lane + 32
-#pragma unroll
-            for (int i = 0; i < (N + 31) / 32; ++i) m_run[i] = -INFINITY;
+            float m_run = -INFINITY;                          // running maximum of row `lane`
             const int t_first = cur.t + (int)((g + NG - g0 % NG) % NG);
 
 #pragma unroll 1
@@ -510,7 +490,7 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_co
                 }
                 // Exponents t = S * ks * c + lsv (+ m) of this thread's token, 16 rows at a time.
                 auto exponents = [&](int c, float (&x)[16], const float* m) {
-                    ca_result16<true>(t_s + c, N, x);
+                    ca_result16(t_s + c, N, x);
 #pragma unroll
                     for (int i = 0; i < 16; i += 4) {
                         const float4 cc = lds4(&s_c[buf][c + i]);
@@ -550,18 +530,14 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_co
                 if (ok && k >= NG) ok = ca_wait(smem_u32(&b_o[g]), (kk - 1) & 1);
                 if (ca_bar_any(1 + g, 128, !ok)) { ok = false; break; }
                 // the tile's maxima over the four warps; factors of the sums, for this warp's own use
-#pragma unroll
-                for (int i = 0; i < (N + 31) / 32; ++i) {
-                    const int r = i * 32 + lane;
-                    if (r < N) {
-                        const float mt = fmaxf(fmaxf(s_red[g][0][r], s_red[g][1][r]), fmaxf(s_red[g][2][r], s_red[g][3][r]));
-                        const float mn = fmaxf(m_run[i], mt);
-                        s_m[w8][r] = mt == -INFINITY ? 0.f : 8.f - mt;
-                        s_a[w8][r] = mn == -INFINITY ? 1.f : ex2(m_run[i] - mn);
-                        s_b[w8][r] = mn == -INFINITY ? 0.f : ex2(mt - mn) * 0.00390625f;
-                        if (wq == 0) s_mt[g][kk & 1][r] = mt;
-                        m_run[i] = mn;
-                    }
+                if (lane < N) {
+                    const float mt = fmaxf(fmaxf(s_red[g][0][lane], s_red[g][1][lane]), fmaxf(s_red[g][2][lane], s_red[g][3][lane]));
+                    const float mn = fmaxf(m_run, mt);
+                    s_m[w8][lane] = mt == -INFINITY ? 0.f : 8.f - mt;
+                    s_a[w8][lane] = mn == -INFINITY ? 1.f : ex2(m_run - mn);
+                    s_b[w8][lane] = mn == -INFINITY ? 0.f : ex2(mt - mn) * 0.00390625f;
+                    if (wq == 0) s_mt[g][kk & 1][lane] = mt;
+                    m_run = mn;
                 }
                 __syncwarp();
                 if (wq == 0 && lane == 0) mbar_arrive(smem_u32(&b_mt[g][kk & 1]));
@@ -607,28 +583,19 @@ cache_attention_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_co
             // ---- end of the item: this group's running maxima and sums ----
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&b_qempty[buf]));   // its constants have been read
-            float l_run[(N + 31) / 32];
-#pragma unroll
-            for (int i = 0; i < (N + 31) / 32; ++i) l_run[i] = 0.f;
+            float l_run = 0.f;
             if (t_first < te) {                               // over the lanes, then over the warps
 #pragma unroll 1
                 for (int c = 0; c < N; c += 16) {
                     float y[16];
                     ca_ld16(t_l + c, y);
                     ca_ld16_wait(y);
-                    s_lred[g][wq][c + ca_sum_row(lane)] = ca_row_sums16(y, lane);
+                    s_lred[g][wq][c + (lane >> 1)] = ca_row_sums16(y, lane);
                 }
                 if (ca_bar_any(1 + g, 128, !ok)) { ok = false; break; }
-#pragma unroll
-                for (int i = 0; i < (N + 31) / 32; ++i) {
-                    const int r = i * 32 + lane;
-                    if (r < N) l_run[i] = (s_lred[g][0][r] + s_lred[g][1][r]) + (s_lred[g][2][r] + s_lred[g][3][r]);
-                }
+                if (lane < N) l_run = (s_lred[g][0][lane] + s_lred[g][1][lane]) + (s_lred[g][2][lane] + s_lred[g][3][lane]);
             }
-            if (wq == 0)
-#pragma unroll
-                for (int i = 0; i < (N + 31) / 32; ++i)
-                    if (i * 32 + lane < N) s_ml[buf][g][i * 32 + lane] = make_float2(m_run[i], l_run[i]);
+            if (wq == 0 && lane < N) s_ml[buf][g][lane] = make_float2(m_run, l_run);
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&b_l[buf]));
             ++item;
@@ -735,7 +702,7 @@ extern "C" bs_status bs_cache_attention(const void* q, long long q_stride_t, lon
     p.abort = p.ticket + sm_count();
     p.partial = reinterpret_cast<float*>(static_cast<char*>(workspace) + ca_ticket_bytes());
     p.scale_log2 = softmax_scale * kLog2e;
-    p.B = B; p.T = T; p.W = max_blocks; p.Nmax = Nmax; p.Hq = Hq; p.Hkv = Hkv; p.G = Hq / Hkv;
+    p.B = B; p.T = T; p.W = max_blocks; p.Nmax = Nmax; p.Hkv = Hkv; p.G = Hq / Hkv;
     p.n_blocks = n_blocks;
     p.bt_log2 = 4;
     while ((1 << p.bt_log2) < block_tokens) ++p.bt_log2;

@@ -36,7 +36,7 @@ struct CacheAttnParams {
     uint32_t* ticket;                          // [grid] arrivals at an item, kept by its first CTA; zero between calls
     volatile uint32_t* abort;                  // [1] set when a wait gave up, cleared with the workspace
     float scale_log2;                          // softmax_scale * log2(e)
-    int B, T, W, Nmax, Hq, Hkv, G, TQ;         // TQ: new tokens of an item, N / G
+    int B, T, W, Nmax, Hkv, G, TQ;             // TQ: new tokens of an item, N / G
     int bt_log2, n_blocks;
 };
 
@@ -185,20 +185,15 @@ __device__ __forceinline__ void ca_st16(uint32_t taddr, const float (&v)[16]) {
           "f"(v[10]), "f"(v[11]), "f"(v[12]), "f"(v[13]), "f"(v[14]), "f"(v[15]), "r"(taddr));
 }
 __device__ __forceinline__ void ca_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-// 16 columns of an MMA result; WIDE: the two terms stand `n` columns apart and are added.
-template <bool WIDE>
+// 16 columns of an MMA result whose two terms stand `n` columns apart.
 __device__ __forceinline__ void ca_result16(uint32_t taddr, int n, float (&x)[16]) {
+    float w[16];
     ca_ld16(taddr, x);
-    if (WIDE) {
-        float w[16];
-        ca_ld16(taddr + n, w);
-        ca_ld16_wait(x);
-        ca_ld16_wait(w);
+    ca_ld16(taddr + n, w);
+    ca_ld16_wait(x);
+    ca_ld16_wait(w);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) x[i] += w[i];
-    } else {
-        ca_ld16_wait(x);
-    }
+    for (int i = 0; i < 16; ++i) x[i] += w[i];
 }
 // Bounded wait of a converged warp.  The loop is out of line: the kernel waits in many places, and its instructions have to
 // stay in the instruction cache.

@@ -56,12 +56,15 @@ template <int R, int D> struct CrLayout {
     static constexpr int kPBufs = kHalves == 1 ? 2 : 1;       // the halves share one
     static constexpr int kMerge = kHalves == 1 ? 0 : R * D * 4;
     static constexpr int kFixed = 4 * kQBytes + 2 * kPBufs * kPBytes + kMerge;
-    // shared memory besides the rings: the static arrays of the kernel take up to 13 KB
-    static constexpr int kSlotsFit = (kCaSmem - 13312 - 1024 - kFixed) / kTileBytes;
+    // shared memory besides the rings: the kernel's static arrays, in the order of their declaration; then barriers and words
+    static constexpr int kStatic = 4 * 2 * R + 4 * 2 * 32 + 4 * 4 * R + 8 * 4 * R + 16 * 8 * kSoft + 8 * (kHalves > 1 ? R : 1) +
+                                   8 * kCaScaleRing * kCaMaxPages + 4 * 2 * R * (D / 32) + (int)sizeof(CaShare) + 512;
+    static constexpr int kSlotsFit = (kCaSmem - kStatic - 1024 - kFixed) / kTileBytes;
     static constexpr int kRing = kSlotsFit / 2 > 6 ? 6 : kSlotsFit / 2;
     static constexpr int kDynamic = 2 * kRing * kTileBytes + kFixed + 1024;
     static constexpr int kPiece = R * D + 2 * R;              // floats of a partial result
     static_assert(kRing >= 2 && kRing + 2 <= kCaScaleRing, "ring");
+    static_assert(kStatic + kDynamic <= kCaSmem, "shared memory");
     // Q is read from R rows before its buffer and up to R rows behind it: rings in front, P behind
     static_assert(2 * kRing * kTileBytes >= R * D && 2 * kPBufs * kPBytes >= R * D, "rows next to Q");
 };
@@ -86,7 +89,7 @@ cache_attention_rows_kernel(const __grid_constant__ CUtensorMap tm_k, const __gr
     __shared__ float s_mt[2][2][R];                           // maxima of a team's tiles, for the accumulator
     __shared__ float2 s_ml[2][2][R];                          // per item parity and team: running maximum and sum
     __shared__ __align__(16) float4 s_tab[L::kSoft][8];       // per softmax warp: scale of K, log2 and inverse of that of V, by 16 tokens
-    __shared__ float2 s_hl[R];                                // merge: maximum and sum of the second half
+    __shared__ float2 s_hl[L::kHalves > 1 ? R : 1];           // merge: maximum and sum of the second half
     __shared__ __align__(8) float s_scale[kCaScaleRing][kCaMaxPages][2];
     __shared__ uint32_t s_nan[2][R][D / 32];                  // per item parity: results a NaN of a masked tile of V belongs to
     __shared__ volatile int s_nan_any[2];

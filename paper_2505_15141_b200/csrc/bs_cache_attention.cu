@@ -15,7 +15,8 @@
 // scaled by a power of two so that its row's largest element lies in [128, 256), is the sum of two e4m3 numbers exactly
 // (four significant bits, a signed remainder of four more; elements below 2^-9 of the largest lose bits under 2^-17
 // of it), and a probability is split the same way (relative error 2^-8 as in bf16).  Their accumulation was measured
-// against 64 bits: error 2^-20 of the largest product.
+// against 64 bits: error 2^-20 of the largest product.  On 200 to 4096 tokens of normal data the splits add 1.0e-4 to 1.6e-4 to a
+// result (norm, relative to 64 bits) whose rounding to bf16 adds 1.6e-3.
 //
 // Scales.  Keys: t_ij = S_ij * (scale of j's block * c_i).  Values: the scale of a token's block joins the exponent:
 //   P''_ij = 2^(t_ij + log2 s_j + 8 - m_i),  m_i = max_j (t_ij + log2 s_j) over the tile,
@@ -36,9 +37,9 @@
 //
 // Bound by the instructions of the softmax on 16 rows (47 % of issue slots, DRAM 50 % busy: both softmax groups
 // and the accumulator are chained within a tile), close to HBM's rate when a row count of 4 leaves little to do.
-// 32 query / 8 key heads of 128, caches larger than L2: 256 sequences of 4096 tokens, 4 rows, 2.15 GB in 0.45 ms
-// (4.8 TB/s); 64 sequences, 16 rows, 0.135 ms (4.0 TB/s); 32 rows 0.174 ms; two sequences of 100003 and 131072
-// tokens, 20 rows, 0.145 ms (3.3 TB/s); one token on 200 cached ones 9.3 us in a graph.
+// 32 query / 8 key heads of 128, caches larger than L2, a call alone on the GPU: 256 sequences of 4096 tokens, 4 rows, 2.15 GB
+// in 0.45 ms (4.8 TB/s); 64 sequences, 16 rows, 0.138 ms (3.9 TB/s); 32 rows 0.178 ms; two sequences of 100003 and 131072
+// tokens, 20 rows, 0.147 ms (3.2 TB/s); one token on 200 cached ones 9.3 us in a graph.
 #include "bs_cache_attention.cuh"
 
 namespace bs {
@@ -710,9 +711,10 @@ extern "C" bs_status bs_cache_attention(const void* q, long long q_stride_t, lon
     if (!ca_map(&tm[0], k_cache, n_blocks, Hkv, block_tokens, d) || !ca_map(&tm[1], v_cache, n_blocks, Hkv, block_tokens, d))
         return BS_ERR_CUDA;
     // The fewest rows that take a sequence's key head at once, so that its cache is read once.  Tokens as lanes cost
-    // in proportion to the rows, rows as lanes the same for any number up to 64 and more for the few: 64
-    // sequences of 4096 tokens, 8 key heads of 128, with 32 rows 174 us here and 219 there, with 48 rows 250 and 217,
-    // with 64 rows 305 and 219.  Prompts take 128 at once: the copies and the scales serve twice the rows.
+    // in proportion to the rows, rows as lanes the same for any number up to 64 and more for the few: 64 sequences of 4096
+    // tokens, 8 key heads of 128, with 8 rows 137 us for tiles of 16, 172 for 32, 215 for 64, 262 for 128; with 32 rows 178 for
+    // 32, 217 for 64; with 48 rows 315 (two items) and 220, with 64 rows 319 and 223, and 268 for 128.  Prompts take 128 at
+    // once: the copies and the scales serve twice the rows.
     const long long rows = (long long)max_new * p.G;
     const int N = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : kCaMaxRows;
     p.TQ = N / p.G;

@@ -303,7 +303,9 @@ __device__ __forceinline__ CaPart ca_share(const CacheAttnParams& p, CaShare& sh
         all += sh.items[w];
     }
     // Little work: where items are short, shares of a whole one of two tiles (they are worked on side by side).  Long ones
-    // are cut; a part takes about 0.3 of a tile's time to join, so least + 0.3 tiles / least is what a CTA waits for.
+    // are cut; a part takes about 0.3 of a tile's time to join, so least + 0.3 tiles / least is what a CTA waits for.  (One
+    // figure for all tiles, from two long contexts with 20 rows and from one key head over 20000 tokens; parts of 128 rows are four
+    // times as large.)
     const float tiles = all ? (float)(work - kCaItemCost * all) / (float)all : 0.f;   // of an item
     const int least = tiles <= 8.f ? kCaItemCost + 2 : max(2, (int)sqrtf(0.3f * tiles));
     const long long grid = min((work + least - 1) / least, (long long)gridDim.x);

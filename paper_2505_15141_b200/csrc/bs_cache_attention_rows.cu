@@ -14,9 +14,11 @@
 //
 // Tensor memory: S of two tiles, O of one, the fp32 accumulator (O * 2^(m_tile - m) is added after every tile, as there).
 //
-// Bound by the four dependent stages of a tile (S, softmax, O, join) with two tiles in flight: issue slots 33 %, tensor
+// Bound by the four dependent stages of a tile (S, softmax, O, join) with two tiles in flight and, with 64 rows, one softmax warp
+// for each sub-partition of the SM: issue slots 33 %, tensor
 // pipe 29 %, DRAM 27 % of their peaks at 63 rows.  32 query / 8 key heads of 128, 64 sequences of 4096 tokens, 64 rows:
-// 0.22 ms for 0.54 GB; pieces of 512 and 333 new tokens behind up to 4096 (47 GFLOP): 0.134 ms with 128 rows at a time.
+// 0.22 ms for 0.54 GB; pieces of 512 and 333 new tokens behind up to 4096 (47 GFLOP): 0.142 ms with 128 rows at a time (calls
+// alone on the GPU; 0.135 among others).
 //
 // Warps: 0, 1 producers, 2 MMA issuer, 4-7 queries and accumulator, then the softmax teams.
 #include "bs_cache_attention.cuh"

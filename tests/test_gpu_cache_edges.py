@@ -127,3 +127,12 @@ def test_more_sequences_than_threads(lib, B, max_new):
     assert not st.any()
     c.check(out, seqs=[0, 1, B - 2, B - 1] + sorted(int(b) for b in rng.integers(0, B, 60)))
     assert torch.equal(c.run(lib, max_new=max_new, ws=ws, dev=dev), out)
+
+
+@pytest.mark.parametrize("max_new", LANES)
+@pytest.mark.parametrize("tree", [False, True])
+def test_a_round_without_new_tokens_writes_nothing(lib, tree, max_new):
+    c = Case(29, [100, 0, 33], [0, 0, 0], 8, 2, 128, 16)
+    c.parent = np.zeros((3, 4), int) if tree else None
+    st = torch.zeros(3, dtype=torch.int32, device=DEV)
+    assert (c.run(lib, max_new=max_new, status=st) == 7.0).all() and not st.any()

@@ -130,3 +130,45 @@ def test_new_tokens_inside_shared_blocks_are_flagged(lib):
     p.d["free"][:2] = _i32([5, 6])
     r = p.plan(lib, None, [1, 1, 0, 1], 0, [1, 1, 2, 1])
     assert r["status"].tolist() == [0, lib.BS_DEV_BAD_LENGTH, 0, lib.BS_DEV_BAD_LENGTH]
+
+
+@pytest.mark.parametrize("T", [64, 9000])
+def test_captured_plans_follow_refusals_on_the_device(lib, T):
+    """One captured plan, replayed: kept, the new tokens and the shared blocks change between replays, cu_new is read and written."""
+    rng = np.random.default_rng(3)
+    B, sh = 6, 1
+    p = Pool(B, 16, 8, 10, T)
+    p.table[:, 0], p.seq[:], p.held[:], p.free = 9, 16, 1, [b for b in range(10) if b != 9]
+    kept, new, shared = _i32([0] * B), _i32([0] * B), _i32([sh] * B)
+    d = p.d
+
+    def load():
+        for n, x in (("seq", p.seq), ("table", p.table), ("held", p.held), ("n_free", [len(p.free)]), ("cu", p.cu)):
+            d[n].copy_(_i32(x))
+        d["free"][:len(p.free)] = _i32(p.free)
+
+    def step():
+        lib.bs_cache_plan(d["seq"], kept, new, 1, None, 16, d["table"], d["held"], d["free"], d["n_free"], d["kv"], d["cu"], d["slots"],
+                          d["pos"], d["status"], last_cu=d["cu"], n_shared=shared)
+
+    load()
+    step()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        step()
+    load()
+    refused = 0
+    for _ in range(12):
+        n, k = rng.integers(3, 12, B), rng.integers(0, 5, B)
+        new.copy_(_i32(n))
+        kept.copy_(_i32(k))
+        g.replay()
+        torch.cuda.synchronize()
+        r = oc.plan(p.seq, k, n, 1, None, 16, p.table, p.held, p.free, T, p.cu, [sh] * B)
+        for name, key in (("seq", "seq_len"), ("held", "held"), ("table", "table"), ("kv", "kv_len"), ("cu", "cu_new"), ("slots", "slot_map"),
+                          ("pos", "positions"), ("status", "status")):
+            assert np.array_equal(d[name].cpu().numpy(), r[key]), name
+        p.seq, p.held, p.table, p.free, p.cu = r["seq_len"], r["held"], r["table"], r["free"], r["cu_new"]
+        refused += int((r["status"] & lib.BS_DEV_NO_BLOCKS != 0).sum())
+    assert refused > 0

@@ -321,8 +321,12 @@ def bs_lmhead_verify(H_t, W_t, H_d, W_d, draft_tokens, gamma, u_accept, temperat
 
 # These calls are made once or more per layer: their checks are kept to a few attribute look-ups each.
 
-# The current stream's handle without building a Stream object; where torch lacks this name (a build without CUDA), the long way.
+# The current stream's handle without building a Stream object, and the current GPU without torch's check that CUDA is up (tensors
+# are there already); where torch lacks these names (a build without CUDA), the long way.
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+_current_gpu = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+_CODES, _f32, _bf16, _int32 = (torch.float8_e4m3fn, torch.uint8), torch.float32, torch.bfloat16, torch.int32
+_ELSEWHERE = "every tensor of a call has to be on the same GPU"
 
 
 def _i32(t, n: int, index: Optional[int] = None) -> Optional[int]:
@@ -330,30 +334,26 @@ def _i32(t, n: int, index: Optional[int] = None) -> Optional[int]:
     if t is None:
         return None
     assert t.dtype is _int32 and t.numel() == n and t.is_contiguous(), f"contiguous int32 of {n} elements expected, got {t.dtype} {tuple(t.shape)}"
-    assert index is None or t.get_device() == index, f"every tensor of a call has to be on its GPU {index}, got {t.device}"
+    assert index is None or t.get_device() == index, _ELSEWHERE
     return t.data_ptr()
 
 
-def _gpu(index: int, *tensors) -> int:
-    """`index` if it is a GPU's and all tensors are there: a pointer into other memory would fault in the kernel."""
+def _gpu(t) -> int:
+    """Index of the tensor's GPU.  All others of the call have to be there, too: a pointer into other memory would fault."""
+    index = t.get_device()
     assert index >= 0, "the tensors have to be on a GPU"
-    for t in tensors:
-        assert t.get_device() == index, f"every tensor of a call has to be on its GPU {index}, got {t.device}"
     return index
 
 
 def _call(fn, where: str, index: int, stream, *args) -> None:
     """fn(*args, stream) with GPU `index` current, on `stream` or that GPU's current stream."""
-    if index == torch.cuda.current_device():
+    if index == _current_gpu():
         code = fn(*args, _raw_stream(index) if stream is None else stream.cuda_stream)
     else:
         with torch.cuda.device(index):
             code = fn(*args, _raw_stream(index) if stream is None else stream.cuda_stream)
     if code != BS_OK:
         raise BanditSpecError(code, where)
-
-
-_CODES, _f32, _int32 = (torch.float8_e4m3fn, torch.uint8), torch.float32, torch.int32
 
 
 def _cache_args(k_cache, k_scale, v_cache, v_scale):
@@ -365,7 +365,9 @@ def _cache_args(k_cache, k_scale, v_cache, v_scale):
     assert v_cache.shape == shape and k_scale.shape == blocks and v_scale.shape == blocks
     assert k_scale.dtype is _f32 and v_scale.dtype is _f32
     assert k_cache.is_contiguous() and v_cache.is_contiguous() and k_scale.is_contiguous() and v_scale.is_contiguous()
-    return _gpu(k_cache.get_device(), k_scale, v_cache, v_scale), n, H, bt, d
+    index = _gpu(k_cache)
+    assert k_scale.get_device() == v_cache.get_device() == v_scale.get_device() == index, _ELSEWHERE
+    return index, n, H, bt, d
 
 
 def new_cache(n_blocks: int, Hkv: int, block_tokens: int, d: int, device="cuda"):
@@ -382,8 +384,10 @@ def bs_cache_plan(seq_len, kept, n_new, extra: int, active, block_tokens: int, b
     refused keeps none.  n_shared: leading blocks of each sequence that it shares with others and that are never returned."""
     B, W = block_table.shape
     n_blocks, T = free_blocks.numel(), slot_map.numel()
-    index = _gpu(seq_len.get_device(), *(() if active is None else (active,)))
-    assert active is None or (active.dtype is torch.uint8 and active.numel() == B and active.is_contiguous())
+    index = _gpu(seq_len)
+    if active is not None:
+        assert active.dtype is torch.uint8 and active.numel() == B and active.is_contiguous()
+        assert active.get_device() == index, _ELSEWHERE
     fn, more = _lib.bs_cache_plan, ()
     if last_cu is not None or n_shared is not None:
         fn, more = _lib.bs_cache_plan_next, (_i32(last_cu, B + 1, index), _i32(n_shared, B, index))
@@ -397,7 +401,7 @@ def bs_cache_append(k, v, slot_map, k_cache, k_scale, v_cache, v_scale, stream=N
     """k, v [T, Hkv, d] (bf16 or fp32, last dimension contiguous) into their slots."""
     index, n_blocks, Hkv, bt, d = _cache_args(k_cache, k_scale, v_cache, v_scale)
     T = slot_map.numel()
-    _gpu(index, k, v)
+    assert k.get_device() == v.get_device() == index, _ELSEWHERE
     assert k.shape == v.shape == (T, Hkv, d) and k.dtype is v.dtype
     kt, kh, k1 = k.stride()
     vt, vh, v1 = v.stride()
@@ -420,7 +424,7 @@ def new_cache_workspace(Hq: int, Hkv: int, d: int, device="cuda") -> torch.Tenso
 def bs_cache_get_device_status(workspace, stream=None) -> None:
     """Raises BanditSpecError (BS_ERR_TIMEOUT) if a bounded wait gave up in an attention on this workspace since it was cleared
     (synchronises)."""
-    _call(_lib.bs_cache_get_device_status, "bs_cache_get_device_status", _gpu(workspace.get_device()), stream,
+    _call(_lib.bs_cache_get_device_status, "bs_cache_get_device_status", _gpu(workspace), stream,
           workspace.data_ptr(), workspace.numel())
 
 
@@ -431,8 +435,8 @@ def bs_cache_attention(q, cu_new, kv_len, block_table, node_parent, k_cache, k_s
     index, n_blocks, Hkv, bt, d = _cache_args(k_cache, k_scale, v_cache, v_scale)
     B, W = block_table.shape
     T, Hq, dq = q.shape
-    _gpu(index, q, out, workspace)
-    assert q.dtype is torch.bfloat16 and out.dtype is torch.bfloat16 and dq == d and out.shape == q.shape
+    assert q.get_device() == out.get_device() == workspace.get_device() == index, _ELSEWHERE
+    assert q.dtype is _bf16 and out.dtype is _bf16 and dq == d and out.shape == q.shape
     qt, qh, q1 = q.stride()
     ot, oh, o1 = out.stride()
     assert q1 == 1 and o1 == 1, "the last dimension must be contiguous"

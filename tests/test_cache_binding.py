@@ -19,14 +19,15 @@ def test_codes_of_another_type_are_refused(lib, dtype, which):
         lib._cache_args(*args)
 
 
-def test_the_binding_imports_without_torchs_private_stream_call(lib):
-    """A torch without CUDA has no torch._C._cuda_getCurrentRawStream."""
+def test_the_binding_imports_without_torchs_private_calls(lib):
+    """A torch without CUDA has neither torch._C._cuda_getCurrentRawStream nor torch._C._cuda_getDevice."""
     code = """
 import torch
-if hasattr(torch._C, "_cuda_getCurrentRawStream"):
-    del torch._C._cuda_getCurrentRawStream
+for name in ("_cuda_getCurrentRawStream", "_cuda_getDevice"):
+    if hasattr(torch._C, name):
+        delattr(torch._C, name)
 from paper_2505_15141_b200 import binding
-assert callable(binding._raw_stream)
+assert callable(binding._raw_stream) and callable(binding._current_gpu)
 """
     r = subprocess.run([sys.executable, "-c", code], cwd=ROOT, capture_output=True, text=True)
     assert r.returncode == 0, r.stderr

@@ -79,6 +79,8 @@ typedef enum { BS_UCB = 0, BS_EXP3 = 1, BS_UCB_REWARD = 2 } bs_alg;
                                       its workspace has to be cleared with bs_workspace_init.  Set in status[0]; without
                                       a status array bs_cache_get_device_status still tells */
 
+#define BS_DEV_BAD_MASK      2048  /* bs_logits_adjust: a mask number outside [-1, n_masks); the row got no mask */
+
 /* Limits of this implementation. */
 #define BS_MAX_GAMMA   31      /* Gmax <= 31 (one warp scans the accept flags) */
 #define BS_MAX_ARMS    32      /* K <= 32 (one lane per arm) */
@@ -473,6 +475,114 @@ bs_status bs_cache_attention(const void* q, long long q_stride_t, long long q_st
 bs_status bs_cache_keep_path(const int32_t* out_nodes, const int32_t* accept_len, const int32_t* seq_len, int B, int Nmax,
                              const int32_t* block_table, int max_blocks, int Hkv, int d, void* k_cache, float* k_scale,
                              void* v_cache, float* v_scale, int n_blocks, int block_tokens, int32_t* status, void* stream);
+
+/* ---- prompts and rotary positions ------------------------------------------------------------
+ *
+ * A prompt enters in the order bs_cache_plan, then in each layer bs_rotary, bs_prompt_attention, bs_cache_append; a round in the
+ * order bs_cache_plan, then in each layer bs_rotary, bs_cache_append, bs_cache_attention.  (A prompt that comes in pieces
+ * attends through bs_cache_attention, too.) */
+
+/* Scaling of the frequencies base^(-2 i / rot) of pair i for contexts longer than `original`, the length that a model was
+ * trained at. */
+typedef enum {
+    BS_ROTARY_PLAIN = 0,
+    BS_ROTARY_LINEAR = 1,     /* all divided by factor */
+    BS_ROTARY_BANDS = 2,      /* pairs that turn `high` times or more within the original length keep their frequency, those
+                                 that turn `low` times or less are divided by factor, between the two it goes over linearly in the turns */
+    BS_ROTARY_YARN = 3        /* pairs below the one that turns `high` times keep theirs, those above the one that turns `low`
+                                 times are divided, between the two (rounded outwards) it goes over linearly in the pair's number; the
+                                 amplitude is 0.1 ln(factor) + 1 */
+} bs_rotary_scaling;
+
+/* Frequencies for bs_rotary, computed on the HOST in fp64: freq_host [rot / 2] turns a position x 2^64, and the amplitude.  rot
+ * even, 2 to 256; base > 1; factor >= 1, 0 < low < high and original >= 1 where the scaling uses them. */
+bs_status bs_rotary_frequencies(bs_rotary_scaling scaling, int rot, double base, double factor, double low, double high,
+                                double original, uint64_t* freq_host, float* amplitude_host);
+
+/* Rotates queries and keys to their positions: (a, b) -> amplitude (a cos w - b sin w, b cos w + a sin w) for every pair,
+ * w = position x frequency.
+ *
+ *  q, q_out  [T, Hq, d], k, k_out [T, Hkv, d] dtype, d contiguous; strides of a token and a head in elements.  q_out may be q and
+ *            k_out may be k (same strides); other overlaps are not supported.  Hq or Hkv may be 0 (pointers NULL)
+ *  positions [T] as bs_cache_plan gives them; rows with a negative one are left as they are (in q_out and k_out, too)
+ *  freq      [rot / 2] DEVICE copy of what bs_rotary_frequencies made; rot <= d, elements from rot on are copied
+ *  interleaved 0: pair i is elements i and i + rot / 2;  else: elements 2 i and 2 i + 1
+ *  node_parent NULL: chains.  [B, Nmax]: trees as in bs_cache_attention, cu_new [B + 1] the plan's: row n of a sequence is rotated
+ *            to position(row 0) + depth of node n, where bs_cache_keep_path will leave it if it is accepted.  A
+ *            parent that is not an earlier node counts as the root; rows behind Nmax + 1 are left as they are
+ * Angles are exact to 2^-32 turns at every position; sines, cosines and products are fp32, results are rounded once.
+ * Any strides work; those that are multiples of 16 bytes (and pointers) take the widest accesses. */
+bs_status bs_rotary(const void* q, long long q_stride_t, long long q_stride_h, const void* k, long long k_stride_t,
+                    long long k_stride_h, bs_dtype dtype, const int32_t* positions, const uint64_t* freq, float amplitude, int rot,
+                    int interleaved, const int32_t* cu_new, const int32_t* node_parent, int B, int Nmax, int T, int Hq, int Hkv, int d,
+                    void* q_out, long long qo_stride_t, long long qo_stride_h, void* k_out, long long ko_stride_t,
+                    long long ko_stride_h, void* stream);
+
+/* Causal attention of whole prompts to themselves: out_i = sum_{j <= i} softmax_j(softmax_scale * q_i . k_j) v_j within each
+ * sequence.
+ *
+ *  q, out  [T, Hq, d], k, v [T, Hkv, d] bf16, d (64 or 128) contiguous; strides of a token and a head in elements, multiples of 8 and
+ *          not negative, 16-byte aligned.  Query head i reads key head i / (Hq / Hkv); Hq / Hkv <= 64.  out overlaps no input
+ *  cu_seqlens [B + 1]: sequence b is rows cu_seqlens[b] .. cu_seqlens[b + 1] - 1 (bs_cache_plan's cu_new, if all begin here).  Empty sequences
+ *          are fine.  Rows of out behind cu_seqlens[B] are left as they are, what the other arrays hold there does not matter
+ *  softmax_scale > 0
+ *  status  [B] or NULL: bits are added.  BS_DEV_BAD_LENGTH: cu_seqlens not ascending, outside [0, T] or with more tokens than T, the
+ *          sequence's rows are left as they are; BS_DEV_TIMEOUT in status[0]: a bounded wait gave up, every output is undefined
+ *          (without a status array nothing tells)
+ * Products accumulate in fp32, probabilities enter the second product as bf16.  Keys and values of later tokens may be NaN or
+ * infinite without a trace; an element of v that is not finite makes that element of the rows that see it NaN or infinite.
+ * Results do not depend on the order in which CTAs run. */
+bs_status bs_prompt_attention(const void* q, long long q_stride_t, long long q_stride_h, const void* k, long long k_stride_t,
+                              long long k_stride_h, const void* v, long long v_stride_t, long long v_stride_h,
+                              const int32_t* cu_seqlens, int B, int T, int Hq, int Hkv, int d, float softmax_scale, void* out,
+                              long long out_stride_t, long long out_stride_h, int32_t* status, void* stream);
+
+/* ---- what is done to logits before they are verified ---------------------------------------------
+ *
+ * History of a sequence's tokens: [B, V] int16, an entry is 2 x (times the token was emitted, up to 16383) + (1 if it is in the
+ * prompt).  bs_history_update enters prompts when a sequence is admitted and the verification's out_tokens after every
+ * round; bs_logits_adjust reads it before the next one. */
+
+/* Enters tokens in the histories.
+ *  history    [B, V] int16 in / out
+ *  fresh      [B] uint8 or NULL (= 0): histories that begin anew, with no entry before this call's
+ *  cu_prompt  [B + 1] or NULL: prompt tokens of sequence b are prompt_tokens[cu_prompt[b] .. cu_prompt[b + 1] - 1], of Tp
+ *  out_tokens [B, W], out_len [B] or NULL: the first out_len[b] tokens were emitted (W <= BS_MAX_GAMMA + 1)
+ *  status     [B] or NULL: bits are added.  BS_DEV_BAD_TOKEN: a token outside [0, V) was left out; BS_DEV_BAD_LENGTH: lengths outside
+ *             the arrays, nothing of the sequence was entered
+ * Two calls on the same history must not overlap. */
+bs_status bs_history_update(int16_t* history, int B, int V, const uint8_t* fresh, const int32_t* cu_prompt,
+                            const int32_t* prompt_tokens, int Tp, const int32_t* out_tokens, const int32_t* out_len, int W,
+                            int32_t* status, void* stream);
+
+/* Penalties, biases and grammar masks on the rows of a batch of logits, in this order:
+ *   seen (in the prompt, emitted, or drafted on the way to this row):  x = x > 0 ? x / r : x r
+ *   emitted or drafted c > 0 times:  x = x - f c - p
+ *   listed:  x = x + its biases
+ *   forbidden by the row's mask:  x = -inf
+ *
+ *  logits, out  [B, R, V] dtype, R <= BS_MAX_GAMMA + 1: target rows (R = Gmax + 1, extra = 1) or draft rows (R = Gmax, extra = 0).  out may
+ *               be logits (only what changes is then written); other overlaps are not supported
+ *  gamma        [B] or NULL (all R rows): rows row_begin <= j < min(row_end, gamma_b + extra) are adjusted, the others are neither
+ *               read nor written
+ *  draft_tokens [B, Nmax] or NULL, Nmax >= R - 1: row j stands behind tokens 0 .. j - 1 of a chain, or with node_parent [B, Nmax]
+ *               (bs_tree_verify_greedy) behind node j and its ancestors.  They count as emitted; one outside [0, V) does not count
+ *  history      [B, V] or NULL (= 0)
+ *  repetition r > 0, presence p, frequency f  [B] fp32 or NULL (1, 0, 0); any of them needs a history or draft_tokens
+ *  bias_begin   [B + 1] or NULL: entries bias_begin[b] .. bias_begin[b + 1] - 1 of bias_tokens and bias_values (n_bias of them) are those
+ *               of sequence b; a token listed twice gets both, in the order of the list.  Meant for lists that are short
+ *               against V: 32 entries cost about 10 instructions for every 256 tokens of the vocabulary
+ *  masks        [n_masks, ceil(V / 32)]: bit v % 32 of word v / 32 is set where token v is allowed; mask_row [B, R] or NULL: the
+ *               row's mask, -1 for none.  A row whose mask allows nothing becomes -inf throughout (BS_DEV_NONFINITE when it is verified)
+ *  status       [B] or NULL: bits are added.  BS_DEV_BAD_GAMMA (outside [0, R - extra]; taken as 0), BS_DEV_BAD_MASK, BS_DEV_BAD_TOKEN (a drafted or
+ *               a listed one), BS_DEV_BAD_TREE (a parent that is not an earlier node counts as the root), BS_DEV_BAD_LENGTH (biases
+ *               outside their arrays, left out)
+ * Arithmetic is fp32, rounded once.  Any V works; a multiple of 8 with pointers on 16 bytes takes the widest accesses. */
+bs_status bs_logits_adjust(const void* logits, void* out, bs_dtype dtype, const int32_t* gamma, int extra, int row_begin, int row_end,
+                           const int32_t* draft_tokens, const int32_t* node_parent, int Nmax, const int16_t* history,
+                           const float* repetition, const float* presence, const float* frequency, const int32_t* bias_begin,
+                           const int32_t* bias_tokens, const float* bias_values, int n_bias, const uint32_t* masks, int n_masks,
+                           const int32_t* mask_row, int B, int R, int V, int32_t* status, void* stream);
 
 /* ---- arm selection (Algorithm 3, select and history lines) ---------------------------- */
 

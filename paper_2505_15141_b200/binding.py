@@ -29,6 +29,8 @@ BS_UCB, BS_EXP3, BS_UCB_REWARD = 0, 1, 2
 BS_DEV_BAD_GAMMA, BS_DEV_BAD_TOKEN, BS_DEV_NONFINITE, BS_DEV_RESIDUAL_FALLBACK, BS_DEV_DRAFT_MISSING = 1, 2, 4, 8, 16
 BS_DEV_BAD_TREE = 32
 BS_DEV_BAD_LENGTH, BS_DEV_NO_BLOCKS, BS_DEV_NO_ROOM, BS_DEV_BAD_BLOCK, BS_DEV_TIMEOUT = 64, 128, 256, 512, 1024
+BS_DEV_BAD_MASK = 2048
+BS_ROTARY_PLAIN, BS_ROTARY_LINEAR, BS_ROTARY_BANDS, BS_ROTARY_YARN = 0, 1, 2, 3
 BS_MAX_GAMMA, BS_MAX_ARMS, BS_MAX_BATCH, BS_MAX_SEQ_BLOCKS = 31, 32, 4096, 1 << 18
 
 _vp, _i, _f, _d, _sz, _ll = C.c_void_p, C.c_int, C.c_float, C.c_double, C.c_size_t, C.c_longlong
@@ -61,6 +63,13 @@ SIGNATURES = {
     "bs_cache_attention": (_i, [_vp, _ll, _ll, _vp, _vp, _vp, _i, _vp, _i, _vp, _vp, _vp, _vp, _i, _i, _i, _i, _i, _i, _i,
                                 _i, _f, _vp, _ll, _ll, _vp, _vp, _sz, _vp]),
     "bs_cache_keep_path": (_i, [_vp, _vp, _vp, _i, _i, _vp, _i, _i, _i, _vp, _vp, _vp, _vp, _i, _i, _vp, _vp]),
+    "bs_rotary_frequencies": (_i, [_i, _i, _d, _d, _d, _d, _d, _vp, _vp]),
+    "bs_rotary": (_i, [_vp, _ll, _ll, _vp, _ll, _ll, _i, _vp, _vp, _f, _i, _i, _vp, _vp, _i, _i, _i, _i, _i, _i, _vp, _ll, _ll, _vp, _ll,
+                       _ll, _vp]),
+    "bs_prompt_attention": (_i, [_vp, _ll, _ll, _vp, _ll, _ll, _vp, _ll, _ll, _vp, _i, _i, _i, _i, _i, _f, _vp, _ll, _ll, _vp, _vp]),
+    "bs_history_update": (_i, [_vp, _i, _i, _vp, _vp, _vp, _i, _vp, _vp, _i, _vp, _vp]),
+    "bs_logits_adjust": (_i, [_vp, _vp, _i, _vp, _i, _i, _i, _vp, _vp, _i, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i, _vp, _i, _vp, _i, _i, _i,
+                              _vp, _vp]),
     "bs_bandit_state_bytes": (_sz, [_i, _i, _i]),
     "bs_bandit_init": (_i, [_vp, _sz, _i, _i, _i, _vp, _d, _vp]),
     "bs_bandit_select": (_i, [_vp, _sz, _i, _i, _i, _vp, _vp, _vp, _vp, _vp, _vp]),
@@ -459,6 +468,132 @@ def bs_cache_keep_path(out_nodes, accept_len, seq_len, block_table, k_cache, k_s
     _call(_lib.bs_cache_keep_path, "bs_cache_keep_path", index, stream, _i32(out_nodes, B * Nmax, index), _i32(accept_len, B, index),
           _i32(seq_len, B, index), B, Nmax, _i32(block_table, B * W, index), W, Hkv, d, k_cache.data_ptr(), k_scale.data_ptr(), v_cache.data_ptr(),
           v_scale.data_ptr(), n_blocks, bt, _i32(status, B, index))
+
+
+def _of(t, dtype, n: int, index: int) -> Optional[int]:
+    """Pointer of a contiguous tensor of n elements of that type on GPU `index` (None stays NULL)."""
+    if t is None:
+        return None
+    assert t.dtype is dtype and t.numel() == n and t.is_contiguous(), f"contiguous {dtype} of {n} elements expected, got {t.dtype} {tuple(t.shape)}"
+    assert t.get_device() == index, _ELSEWHERE
+    return t.data_ptr()
+
+
+# ---- rotary positions --------------------------------------------------------------------------
+
+@dataclass
+class RotaryTable:
+    """Frequencies of bs_rotary on one GPU."""
+    freq: torch.Tensor         # [rot / 2] int64: turns a position x 2^64
+    amplitude: float
+    rot: int                   # rotated elements of a head
+
+
+_SCALINGS = {"none": BS_ROTARY_PLAIN, "linear": BS_ROTARY_LINEAR, "bands": BS_ROTARY_BANDS, "yarn": BS_ROTARY_YARN}
+
+
+def new_rotary_table(rot: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0, low: float = 1.0,
+                     high: float = 32.0, original: float = 8192.0, device="cuda") -> RotaryTable:
+    """Frequencies base^(-2 i / rot), scaled: "none", "linear", "bands" or "yarn" (bs_rotary_frequencies)."""
+    freq, amplitude = np.zeros(max(int(rot), 0) // 2 + 1, dtype=np.uint64), C.c_float(0.0)
+    _check(_lib.bs_rotary_frequencies(_SCALINGS[scaling], rot, base, factor, low, high, original, freq.ctypes.data_as(_vp),
+                                      C.byref(amplitude)), "bs_rotary_frequencies")
+    return RotaryTable(torch.from_numpy(freq[: rot // 2].view(np.int64)).to(device), amplitude.value, rot)
+
+
+def _heads(x, index: int):
+    """Pointer, strides and heads of [T, H, d] on GPU `index`, last dimension contiguous; an absent one has no heads."""
+    if x is None:
+        return 0, 0, 0, 0
+    assert x.get_device() == index, _ELSEWHERE
+    t, h, one = x.stride()
+    assert one == 1 or x.shape[2] == 1, "the last dimension must be contiguous"
+    return x.data_ptr(), t, h, x.shape[1]
+
+
+def bs_rotary(q, k, positions, table: RotaryTable, interleaved: bool, q_out, k_out, cu_new=None, node_parent=None, stream=None) -> None:
+    """q, q_out [T, Hq, d] and k, k_out [T, Hkv, d] (bf16 or fp32; either pair may be None; q_out may be q) rotated to `positions`
+    [T] int32.  node_parent [B, Nmax] with cu_new [B + 1]: trees of drafts, a node stands its depth behind its root."""
+    some = q if q is not None else k
+    T, _, d = some.shape
+    index, dtype, freq = _gpu(some), some.dtype, table.freq
+    assert (q is None) == (q_out is None) and (k is None) == (k_out is None)
+    assert q is None or (q.shape[0] == T and q.shape[2] == d and q_out.shape == q.shape and q.dtype is dtype and q_out.dtype is dtype)
+    assert k is None or (k.shape[0] == T and k.shape[2] == d and k_out.shape == k.shape and k.dtype is dtype and k_out.dtype is dtype)
+    table_at = _of(freq, torch.int64, table.rot // 2, index)
+    B, Nmax = (0, 0) if node_parent is None else node_parent.shape
+    parent = _i32(node_parent, B * Nmax, index)
+    if node_parent is not None:
+        assert cu_new is not None, "trees need cu_new"
+        if Nmax == 0:                                        # an empty tensor has no address, and NULL would mean chains
+            parent = positions.data_ptr()
+    qp, qt, qh, Hq = _heads(q, index)
+    kp, kt, kh, Hkv = _heads(k, index)
+    qop, qot, qoh, _ = _heads(q_out, index)
+    kop, kot, koh, _ = _heads(k_out, index)
+    _call(_lib.bs_rotary, "bs_rotary", index, stream, qp, qt, qh, kp, kt, kh, _dtype_code(some), _i32(positions, T, index), table_at,
+          table.amplitude, table.rot, 1 if interleaved else 0, None if node_parent is None else _i32(cu_new, B + 1, index), parent, B, Nmax,
+          T, Hq, Hkv, d, qop, qot, qoh, kop, kot, koh)
+
+
+# ---- attention of whole prompts ------------------------------------------------------------------
+
+def bs_prompt_attention(q, k, v, cu_seqlens, softmax_scale: float, out, status=None, stream=None) -> None:
+    """q, out [T, Hq, d], k, v [T, Hkv, d] bf16 (last dimension contiguous): causal attention within the sequences of cu_seqlens [B + 1]."""
+    T, Hq, d = q.shape
+    index, B = _gpu(q), cu_seqlens.numel() - 1
+    assert q.dtype is _bf16 and k.dtype is _bf16 and v.dtype is _bf16 and out.dtype is _bf16
+    assert out.shape == q.shape and k.shape == v.shape and k.shape[0] == T and k.shape[2] == d
+    qp, qt, qh, _ = _heads(q, index)
+    kp, kt, kh, Hkv = _heads(k, index)
+    vp, vt, vh, _ = _heads(v, index)
+    op, ot, oh, _ = _heads(out, index)
+    _call(_lib.bs_prompt_attention, "bs_prompt_attention", index, stream, qp, qt, qh, kp, kt, kh, vp, vt, vh, _i32(cu_seqlens, B + 1, index),
+          B, T, Hq, Hkv, d, softmax_scale, op, ot, oh, _i32(status, B, index))
+
+
+# ---- logits before the verification ------------------------------------------------------------
+
+def new_history(B: int, V: int, device="cuda") -> torch.Tensor:
+    """Token histories without an entry: int16 [B, V]."""
+    return torch.zeros(B, V, dtype=torch.int16, device=device)
+
+
+def bs_history_update(history, fresh=None, cu_prompt=None, prompt_tokens=None, out_tokens=None, out_len=None, status=None,
+                      stream=None) -> None:
+    """Enters prompt_tokens (packed by cu_prompt) and the first out_len[b] of out_tokens [B, W] in history [B, V] int16; histories
+    with fresh[b] begin anew."""
+    B, V = history.shape
+    index = _gpu(history)
+    assert (out_tokens is None) == (out_len is None) and (cu_prompt is None) == (prompt_tokens is None)
+    Tp = 0 if prompt_tokens is None else prompt_tokens.numel()
+    W = 0 if out_tokens is None else out_tokens.shape[1]
+    _call(_lib.bs_history_update, "bs_history_update", index, stream, _of(history, torch.int16, B * V, index), B, V,
+          _of(fresh, torch.uint8, B, index), _i32(cu_prompt, B + 1, index), _i32(prompt_tokens, Tp, index), Tp,
+          _i32(out_tokens, B * W, index), _i32(out_len, B, index), W, _i32(status, B, index))
+
+
+def bs_logits_adjust(logits, out, gamma, extra: int, rows=None, draft_tokens=None, node_parent=None, history=None, repetition=None,
+                     presence=None, frequency=None, bias_begin=None, bias_tokens=None, bias_values=None, masks=None, mask_row=None,
+                     status=None, stream=None) -> None:
+    """Penalties, biases and grammar masks on rows (begin, end) of logits [B, R, V] below gamma_b + extra; out may be logits."""
+    B, R, V = logits.shape
+    index = _gpu(logits)
+    begin, end = (0, R) if rows is None else rows
+    N = 0 if draft_tokens is None else draft_tokens.shape[1]
+    n_bias = 0 if bias_tokens is None else bias_tokens.numel()
+    assert (bias_begin is None) == (bias_tokens is None) == (bias_values is None)
+    assert (masks is None) == (mask_row is None)
+    n_masks = 0 if masks is None else masks.shape[0]
+    tokens, parent = _i32(draft_tokens, B * N, index), _i32(node_parent, B * N, index)
+    if draft_tokens is not None and N == 0:                  # an empty tensor has no address; nothing of it is read
+        tokens, parent = logits.data_ptr(), None
+    _call(_lib.bs_logits_adjust, "bs_logits_adjust", index, stream, _of(logits, logits.dtype, B * R * V, index),
+          _of(out, logits.dtype, B * R * V, index), _dtype_code(logits), _i32(gamma, B, index), extra, begin, end, tokens, parent, N,
+          _of(history, torch.int16, B * V, index), _of(repetition, _f32, B, index), _of(presence, _f32, B, index),
+          _of(frequency, _f32, B, index), _i32(bias_begin, B + 1, index), _i32(bias_tokens, n_bias, index),
+          _of(bias_values, _f32, n_bias, index), n_bias, _i32(masks, n_masks * ((V + 31) // 32), index), n_masks,
+          _i32(mask_row, B * R, index), B, R, V, _i32(status, B, index))
 
 
 # ---- bandits ---------------------------------------------------------------------------

@@ -1,0 +1,481 @@
+// bs_logits_adjust and bs_history_update: what is done to the logits of a round before they are verified, and the token
+// history that it reads.
+//
+//   x = logit;  seen (in the prompt, emitted, or drafted on the way to this row): x = x > 0 ? x / r : x r
+//   x -= f c + p [c > 0],  c = times emitted or drafted on the way;   x += bias;   forbidden by the row's grammar mask: -inf
+//
+// adjust: bound by HBM; the rows are read and written once, the history once for all rows of a sequence.  A warp takes 256
+// tokens of the vocabulary of one sequence, eight a lane, and passes over the rows of that sequence.  It needs nothing from other
+// warps: it looks through the biases and drafted tokens for those in its range itself, in the order of the list, so that sums do
+// not depend on timing.  In place, lanes with nothing to change touch nothing, and tokens that are all forbidden are
+// written without being read.
+//
+// history: entries of 16 bits, 2 x (times emitted, up to 16383) + (in the prompt).  A history that begins anew is built in
+// shared memory piece by piece and written once; what a round adds goes to its few entries by compare-and-swap.  Only whole
+// numbers are added: the order does not show.
+#include "bs_common.cuh"
+
+namespace bs {
+
+// Ancestors of node `lane` in a tree, itself included (bit n: node n; the root is bit 0): lane n holds the parent of node n.
+__device__ __forceinline__ uint32_t tree_ancestors(int parent, int nodes) {
+    const int lane = threadIdx.x & 31;
+    uint32_t anc = 1u << lane;
+    for (int n = 1; n <= nodes; ++n) {                        // parents come before their children
+        const int up = __shfl_sync(0xffffffffu, parent, n);
+        const uint32_t of_up = __shfl_sync(0xffffffffu, anc, up);
+        if (lane == n) anc |= of_up;
+    }
+    return anc | 1u;
+}
+
+struct AdjustParams {
+    const void* x;
+    void* y;
+    const int32_t* gamma;
+    const int32_t* draft_tokens;
+    const int32_t* node_parent;
+    const int16_t* history;
+    const float *repetition, *presence, *frequency;
+    const int32_t *bias_begin, *bias_tokens;
+    const float* bias_values;
+    const uint32_t* masks;
+    const int32_t* mask_row;
+    int32_t* status;
+    int extra, row_begin, row_end, B, R, N, V, n_masks, n_bias, in_place;
+};
+
+constexpr int kAdWarps = 8;
+constexpr int kAdLane = 8;                     // tokens of a lane
+constexpr int kAdWarp = 32 * kAdLane;          // of a warp
+constexpr int kAdRows = 4;                     // rows in flight
+constexpr uint32_t kAdNothing = 0x100u;        // beside the allowed elements: nothing to do in this row
+
+// Eight elements of a lane.  VEC: neighbours, two or one 16-byte accesses; else 32 apart, for rows that begin anywhere.
+template <typename T, bool VEC> struct AdIo;
+template <typename T> struct AdIo<T, true> {
+    static constexpr int kWords = (int)sizeof(T) * 2;
+    __device__ static __forceinline__ void load(const T* p, int, uint32_t (&w)[kWords]) {
+#pragma unroll
+        for (int i = 0; i < kWords; i += 4) {
+            const uint4 v = *reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(p) + 4 * i);
+            w[i] = v.x; w[i + 1] = v.y; w[i + 2] = v.z; w[i + 3] = v.w;
+        }
+    }
+    __device__ static __forceinline__ void store(T* p, int, const uint32_t (&w)[kWords]) {
+#pragma unroll
+        for (int i = 0; i < kWords; i += 4)
+            *reinterpret_cast<uint4*>(reinterpret_cast<char*>(p) + 4 * i) = make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]);
+    }
+};
+template <> struct AdIo<float, false> {
+    static constexpr int kWords = 8;
+    __device__ static __forceinline__ void load(const float* p, int n, uint32_t (&w)[8]) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] = 32 * e < n ? __float_as_uint(p[32 * e]) : 0u;
+    }
+    __device__ static __forceinline__ void store(float* p, int n, const uint32_t (&w)[8]) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (32 * e < n) p[32 * e] = __uint_as_float(w[e]);
+    }
+};
+template <> struct AdIo<__nv_bfloat16, false> {
+    static constexpr int kWords = 4;
+    __device__ static __forceinline__ void load(const __nv_bfloat16* p, int n, uint32_t (&w)[4]) {
+        const unsigned short* u = reinterpret_cast<const unsigned short*>(p);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            w[e] = (64 * e < n ? (uint32_t)u[64 * e] : 0u) | (64 * e + 32 < n ? (uint32_t)u[64 * e + 32] << 16 : 0u);
+    }
+    __device__ static __forceinline__ void store(__nv_bfloat16* p, int n, const uint32_t (&w)[4]) {
+        unsigned short* u = reinterpret_cast<unsigned short*>(p);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (64 * e < n) u[64 * e] = (unsigned short)w[e];
+            if (64 * e + 32 < n) u[64 * e + 32] = (unsigned short)(w[e] >> 16);
+        }
+    }
+};
+__device__ __forceinline__ void ad_unpack(const uint32_t (&w)[8], float (&f)[8]) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] = __uint_as_float(w[e]);
+}
+__device__ __forceinline__ void ad_unpack(const uint32_t (&w)[4], float (&f)[8]) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        f[2 * e] = __uint_as_float(w[e] << 16);
+        f[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
+    }
+}
+__device__ __forceinline__ void ad_pack(const float (&f)[8], uint32_t (&w)[8]) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) w[e] = __float_as_uint(f[e]);
+}
+__device__ __forceinline__ void ad_pack(const float (&f)[8], uint32_t (&w)[4]) {   // the one rounding
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const __nv_bfloat162 b = __floats2bfloat162_rn(f[2 * e], f[2 * e + 1]);
+        w[e] = *reinterpret_cast<const uint32_t*>(&b);
+    }
+}
+
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(kAdWarps * 32) logits_adjust_kernel(const AdjustParams p) {
+    using Io = AdIo<T, VEC>;
+    __shared__ float s_bias[kAdWarps][kAdWarp];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, b = blockIdx.y;
+    const int chunk = blockIdx.x * kAdWarps + warp, v0 = chunk * kAdWarp;
+    pdl_enter();
+    if (v0 >= p.V) return;
+    const int first = VEC ? v0 + lane * kAdLane : v0 + lane;  // token of element 0
+    const int left = p.V - first;                             // VEC: >= 8 or <= 0; else: elements 32 e < left are there
+    int bits = 0, rows = p.row_end;
+    if (p.gamma) {
+        int g = __ldg(p.gamma + b);
+        if (g < 0 || g + p.extra > p.R) { g = 0; bits |= BS_DEV_BAD_GAMMA; }
+        rows = min(rows, g + p.extra);
+    }
+    if (rows <= p.row_begin && !(p.status && chunk == 0)) return;
+    // grammar mask of every row, row by lane
+    int mask = -1;
+    if (p.mask_row && lane < p.R) {
+        mask = __ldg(p.mask_row + (size_t)b * p.R + lane);
+        if (mask < -1 || mask >= p.n_masks) {
+            mask = -1;
+            if (lane >= p.row_begin && lane < rows) bits |= BS_DEV_BAD_MASK;
+        }
+    }
+    const bool pen = p.repetition || p.presence || p.frequency;
+    const float rep = p.repetition ? __ldg(p.repetition + b) : 1.f, inv = 1.f / rep;
+    const float pres = p.presence ? __ldg(p.presence + b) : 0.f, freq = p.frequency ? __ldg(p.frequency + b) : 0.f;
+    // drafted tokens, one a lane, and the rows (a bit each) that stand behind them
+    int tok = -1;
+    uint32_t behind = 0u;
+    if (pen && p.draft_tokens) {
+        if (lane < p.N) tok = __ldg(p.draft_tokens + (size_t)b * p.N + lane);
+        if (p.node_parent) {
+            int parent = lane >= 1 && lane <= p.N ? __ldg(p.node_parent + (size_t)b * p.N + lane - 1) : 0;
+            if (parent < 0 || (lane > 0 && parent >= lane)) {
+                if (lane < rows) bits |= BS_DEV_BAD_TREE;
+                parent = 0;
+            }
+            const uint32_t anc = tree_ancestors(parent, p.N);
+#pragma unroll 1
+            for (int r = 1; r < rows; ++r) {                  // node lane + 1 among the ancestors of node r
+                const uint32_t of_row = __shfl_sync(0xffffffffu, anc, r);
+                if (lane < 31 && (of_row >> (lane + 1)) & 1u) behind |= 1u << r;
+            }
+        } else {
+            behind = lane < 31 ? ~0u << (lane + 1) : 0u;
+        }
+        if (lane < p.N && (tok < 0 || tok >= p.V) && lane < rows - 1) bits |= BS_DEV_BAD_TOKEN;
+    }
+    const uint32_t drafted = __ballot_sync(0xffffffffu, behind && tok >= v0 && tok < min(v0 + kAdWarp, p.V));
+
+    // history: factor and summand of every element
+    const bool here = left > 0;
+    uint32_t h[4] = {0u, 0u, 0u, 0u};
+    if (pen && p.history && here)
+        AdIo<__nv_bfloat16, VEC>::load(reinterpret_cast<const __nv_bfloat16*>(p.history) + (size_t)b * p.V + first, left, h);
+    float add[8];
+    uint32_t seen = 0u, counted = 0u;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) add[e] = 0.f;
+    if (h[0] | h[1] | h[2] | h[3]) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const uint32_t v = (h[e >> 1] >> (16 * (e & 1))) & 0xffffu;
+            if (v) seen |= 1u << e;
+            if (v >> 1) {
+                counted |= 1u << e;
+                add[e] = -fmaf(freq, (float)(v >> 1), pres);
+            }
+        }
+    }
+    uint32_t any = seen;
+    if (p.bias_begin) {
+        const int lo = __ldg(p.bias_begin + b), hi = __ldg(p.bias_begin + b + 1);
+        if (lo < 0 || hi > p.n_bias || lo > hi) {
+            bits |= BS_DEV_BAD_LENGTH;
+        } else if (lo < hi) {
+            float* sb = s_bias[warp];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sb[32 * e + lane] = 0.f;
+            __syncwarp();
+            bool hits = false;
+            int next = lo + lane < hi ? __ldg(p.bias_tokens + lo + lane) : -1;
+#pragma unroll 1
+            for (int i = lo; i < hi; i += 32) {
+                const int t = next - v0;
+                if (i + lane < hi && (next < 0 || next >= p.V)) bits |= BS_DEV_BAD_TOKEN;
+                next = i + 32 + lane < hi ? __ldg(p.bias_tokens + i + 32 + lane) : -1;
+                const bool hit = t >= 0 && t < kAdWarp;       // the end of a list reads as token -1: t < 0
+                uint32_t who = __ballot_sync(0xffffffffu, hit);
+                hits = hits || who;
+                const float v = hit ? __ldg(p.bias_values + i + lane) : 0.f;
+                while (who) {                                 // in the order of the list: a token may be listed twice
+                    const int l = __ffs(who) - 1;
+                    who &= who - 1;
+                    if (lane == l) sb[t] += v;
+                    __syncwarp();
+                }
+            }
+            if (hits) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float v = sb[VEC ? lane * 8 + e : 32 * e + lane];
+                    add[e] += v;
+                    if (v != 0.f) any |= 1u << e;
+                }
+            }
+        }
+    }
+
+    if (p.status && chunk == 0) {
+        bits = (int)__reduce_or_sync(0xffffffffu, (unsigned)bits);
+        if (lane == 0 && bits) atomicOr(p.status + b, bits);
+    }
+
+    const T* x = reinterpret_cast<const T*>(p.x) + (size_t)b * p.R * p.V + first;
+    T* y = reinterpret_cast<T*>(p.y) + (size_t)b * p.R * p.V + first;
+    const size_t mask_words = (size_t)((p.V + 31) >> 5);
+#pragma unroll 1
+    for (int r0 = p.row_begin; r0 < rows; r0 += kAdRows) {
+        uint32_t w[kAdRows][Io::kWords], allowed[kAdRows], own[kAdRows];
+        // allowed elements of every row
+#pragma unroll
+        for (int k = 0; k < kAdRows; ++k) {
+            const int m = __shfl_sync(0xffffffffu, mask, (r0 + k) & 31);
+            allowed[k] = 0xffu;
+            if (m >= 0 && r0 + k < rows) {
+                const uint32_t* words = p.masks + (size_t)m * mask_words + (v0 >> 5);
+                if (VEC) {
+                    if (here) allowed[k] = __ldg(reinterpret_cast<const unsigned char*>(words) + lane);
+                } else {
+                    const uint32_t word = lane < 8 && v0 + 32 * lane < p.V ? __ldg(words + lane) : 0u;
+                    uint32_t a = 0u;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) a |= ((__shfl_sync(0xffffffffu, word, e) >> lane) & 1u) << e;
+                    allowed[k] = a;
+                }
+            }
+        }
+        // what of a lane's elements the drafted tokens before a row fall on
+        auto drafted_on = [&](int row, auto&& found) {
+            uint32_t d = drafted;
+#pragma unroll 1
+            while (d) {
+                const int l = __ffs(d) - 1;
+                d &= d - 1;
+                const int t = __shfl_sync(0xffffffffu, tok, l) - v0;
+                const uint32_t rr = __shfl_sync(0xffffffffu, behind, l);
+                if ((VEC ? t >> 3 : t & 31) == lane && ((rr >> (row & 31)) & 1u)) found(VEC ? t & 7 : t >> 5);
+            }
+        };
+#pragma unroll
+        for (int k = 0; k < kAdRows; ++k) {
+            own[k] = 0u;
+            if (drafted) drafted_on(r0 + k, [&](int e) { own[k] |= 1u << e; });
+            const bool active = here && r0 + k < rows;
+            if (!active || (p.in_place && allowed[k] == 0xffu && !(any | own[k]))) allowed[k] = kAdNothing;
+#pragma unroll
+            for (int i = 0; i < Io::kWords; ++i) w[k][i] = 0u;
+            if (allowed[k] & 0xffu) Io::load(x + (size_t)(r0 + k) * p.V, left, w[k]);
+        }
+#pragma unroll
+        for (int k = 0; k < kAdRows; ++k) {
+            float f[8];
+            ad_unpack(w[k], f);
+            if (any | own[k]) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    if (((seen | own[k]) >> e) & 1u) f[e] *= f[e] > 0.f ? inv : rep;
+                    f[e] += add[e];
+                }
+            }
+            if (drafted) {                                    // they count like emitted ones
+                uint32_t known = counted;
+                drafted_on(r0 + k, [&](int hit) {
+                    const float less = (known >> hit) & 1u ? freq : freq + pres;
+                    known |= 1u << hit;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (e == hit) f[e] -= less;
+                });
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (!((allowed[k] >> e) & 1u)) f[e] = -INFINITY;
+            if (!(allowed[k] & kAdNothing)) {
+                uint32_t o[Io::kWords];
+                ad_pack(f, o);
+                Io::store(y + (size_t)(r0 + k) * p.V, left, o);
+            }
+        }
+    }
+}
+
+// ---- the token history --------------------------------------------------------------------------------------
+
+constexpr int kHiThreads = 256;
+constexpr int kHiPiece = 8192;                 // entries of a CTA of a history that begins anew: 16 KB of shared memory
+constexpr int kHiMost = 16383;
+
+struct HistoryParams {
+    int16_t* history;
+    const uint8_t* fresh;
+    const int32_t *cu_prompt, *prompt, *out_tokens, *out_len;
+    int32_t* status;
+    int V, Tp, W;
+};
+
+// One more of token `tok`: emitted (2, no further than the largest count) or in the prompt (1).
+__device__ __forceinline__ void history_add(int16_t* row, int tok, bool prompt) {
+    unsigned short* at = reinterpret_cast<unsigned short*>(row) + tok;
+    unsigned short old = *at;
+    for (;;) {
+        const unsigned short to = prompt ? old | 1u : (old >> 1) >= kHiMost ? old : (unsigned short)(old + 2u);
+        if (to == old) return;
+        const unsigned short was = atomicCAS(at, old, to);
+        if (was == old) return;
+        old = was;
+    }
+}
+// Its tokens: false, and none, if the lengths make no sense.
+__device__ __forceinline__ bool history_lengths(const HistoryParams& p, int b, int& c0, int& n, int& m) {
+    c0 = n = m = 0;
+    if (p.cu_prompt) {
+        c0 = __ldg(p.cu_prompt + b);
+        n = __ldg(p.cu_prompt + b + 1) - c0;
+    }
+    if (p.out_len) m = __ldg(p.out_len + b);
+    const bool ok = c0 >= 0 && n >= 0 && c0 <= p.Tp - n && m >= 0 && m <= p.W;
+    if (!ok) n = m = 0;
+    return ok;
+}
+
+// A round, or pieces of prompts: a CTA (a warp where there are no prompts) for every sequence.
+template <int THREADS>
+__device__ __forceinline__ void history_scatter(const HistoryParams& p, int b, int t, int c0, int n, int m, bool ok) {
+    int16_t* row = p.history + (size_t)b * p.V;
+    bool bad = false;
+    for (int i = t; i < n; i += THREADS) {
+        const int tok = __ldg(p.prompt + c0 + i);
+        if (tok < 0 || tok >= p.V) bad = true;
+        else history_add(row, tok, true);
+    }
+    for (int i = t; i < m; i += THREADS) {
+        const int tok = __ldg(p.out_tokens + (size_t)b * p.W + i);
+        if (tok < 0 || tok >= p.V) bad = true;
+        else history_add(row, tok, false);
+    }
+    if (p.status && bad) atomicOr(p.status + b, BS_DEV_BAD_TOKEN);
+    if (p.status && !ok && t == 0) atomicOr(p.status + b, BS_DEV_BAD_LENGTH);
+}
+__global__ void __launch_bounds__(kHiThreads) history_round_kernel(const HistoryParams p, int B) {
+    pdl_enter();
+    const int b = blockIdx.x * (kHiThreads / 32) + (threadIdx.x >> 5);
+    if (b >= B) return;
+    int c0, n, m;
+    const bool ok = history_lengths(p, b, c0, n, m);
+    history_scatter<32>(p, b, threadIdx.x & 31, c0, n, m, ok);
+}
+
+// blockIdx.y: sequence, blockIdx.x: piece of its vocabulary
+__global__ void __launch_bounds__(kHiThreads) history_prompts_kernel(const HistoryParams p) {
+    __shared__ __align__(16) uint32_t s_words[kHiPiece / 2 + 4];
+    const int b = blockIdx.y, tid = threadIdx.x;
+    pdl_enter();
+    int c0, n, m;
+    const bool ok = history_lengths(p, b, c0, n, m);
+    if (!p.fresh || !__ldg(p.fresh + b)) {
+        if (blockIdx.x == 0) history_scatter<kHiThreads>(p, b, tid, c0, n, m, ok);
+        return;
+    }
+    // entry v lies at place v - v0 + shift, so that 16-byte pieces are the same here and in the history
+    const int v0 = blockIdx.x * kHiPiece, nv = min(kHiPiece, p.V - v0);
+    int16_t* row = p.history + (size_t)b * p.V + v0;
+    const int shift = (int)((reinterpret_cast<uintptr_t>(row) >> 1) & 7);
+    for (int i = tid; i < kHiPiece / 2 + 4; i += kHiThreads) s_words[i] = 0u;
+    __syncthreads();
+    bool bad = false;
+    for (int i = tid; i < n; i += kHiThreads) {
+        const int t = __ldg(p.prompt + c0 + i), at = t - v0 + shift;
+        if (t < 0 || t >= p.V) bad = true;
+        else if (t >= v0 && t < v0 + nv) atomicOr(s_words + (at >> 1), 1u << (16 * (at & 1)));
+    }
+    for (int i = tid; i < m; i += kHiThreads) {               // W <= 32: no count overflows
+        const int t = __ldg(p.out_tokens + (size_t)b * p.W + i), at = t - v0 + shift;
+        if (t < 0 || t >= p.V) bad = true;
+        else if (t >= v0 && t < v0 + nv) atomicAdd(s_words + (at >> 1), 2u << (16 * (at & 1)));
+    }
+    if (p.status && blockIdx.x == 0) {
+        if (bad) atomicOr(p.status + b, BS_DEV_BAD_TOKEN);
+        if (!ok && tid == 0) atomicOr(p.status + b, BS_DEV_BAD_LENGTH);
+    }
+    __syncthreads();
+    int16_t* base = row - shift;                              // on a 16-byte boundary
+    const int16_t* s_entry = reinterpret_cast<const int16_t*>(s_words);
+    for (int i = tid; i * 8 < nv + shift; i += kHiThreads) {
+        const int lo = max(i * 8, shift), hi = min(i * 8 + 8, nv + shift);
+        if (hi - lo == 8) {
+            *reinterpret_cast<uint4*>(base + i * 8) = *reinterpret_cast<const uint4*>(s_words + i * 4);
+        } else {
+            for (int j = lo; j < hi; ++j) base[j] = s_entry[j];
+        }
+    }
+}
+
+template <typename T>
+static cudaError_t launch_adjust(const AdjustParams& p, bool vec, cudaStream_t st) {
+    const dim3 grid(div_up(div_up(p.V, kAdWarp), kAdWarps), p.B);
+    return vec ? launch_pdl(logits_adjust_kernel<T, true>, grid, kAdWarps * 32, 0, st, p)
+               : launch_pdl(logits_adjust_kernel<T, false>, grid, kAdWarps * 32, 0, st, p);
+}
+
+}  // namespace bs
+
+using namespace bs;
+
+extern "C" bs_status bs_history_update(int16_t* history, int B, int V, const uint8_t* fresh, const int32_t* cu_prompt,
+                                       const int32_t* prompt_tokens, int Tp, const int32_t* out_tokens, const int32_t* out_len, int W,
+                                       int32_t* status, void* stream) {
+    if (!history || B < 1 || V < 1 || Tp < 0 || W < 0 || (cu_prompt && Tp > 0 && !prompt_tokens) || (out_len && W > 0 && !out_tokens))
+        return BS_ERR_INVALID_ARG;
+    if (B > BS_MAX_BATCH || V > BS_MAX_VOCAB || W > BS_MAX_GAMMA + 1) return BS_ERR_UNSUPPORTED;
+    if (reinterpret_cast<uintptr_t>(history) & 1) return BS_ERR_INVALID_ARG;
+    HistoryParams p = {history, fresh, cu_prompt, prompt_tokens, out_tokens, out_len, status, V, cu_prompt ? Tp : 0, W};
+    const cudaStream_t st = (cudaStream_t)stream;
+    if (!fresh && !cu_prompt) {
+        if (!out_len) return BS_OK;
+        return cuda_status(launch_pdl(history_round_kernel, div_up(B, kHiThreads / 32), kHiThreads, 0, st, p, B));
+    }
+    const dim3 grid(fresh ? div_up(V, kHiPiece) : 1, B);
+    return cuda_status(launch_pdl(history_prompts_kernel, grid, kHiThreads, 0, st, p));
+}
+
+extern "C" bs_status bs_logits_adjust(const void* logits, void* out, bs_dtype dtype, const int32_t* gamma, int extra, int row_begin,
+                                      int row_end, const int32_t* draft_tokens, const int32_t* node_parent, int Nmax,
+                                      const int16_t* history, const float* repetition, const float* presence, const float* frequency,
+                                      const int32_t* bias_begin, const int32_t* bias_tokens, const float* bias_values, int n_bias,
+                                      const uint32_t* masks, int n_masks, const int32_t* mask_row, int B, int R, int V, int32_t* status,
+                                      void* stream) {
+    if (B < 1 || R < 1 || V < 1 || !logits || !out || Nmax < 0 || n_bias < 0 || n_masks < 0) return BS_ERR_INVALID_ARG;
+    if (dtype != BS_F32 && dtype != BS_BF16) return BS_ERR_INVALID_ARG;
+    if (extra < 0 || extra > 1 || row_begin < 0 || row_end < row_begin || row_end > R) return BS_ERR_INVALID_ARG;
+    if (B > BS_MAX_BATCH || R > BS_MAX_GAMMA + 1 || V > BS_MAX_VOCAB || Nmax > BS_MAX_GAMMA) return BS_ERR_UNSUPPORTED;
+    if (draft_tokens && Nmax < R - 1) return BS_ERR_INVALID_ARG;
+    if (node_parent && !draft_tokens) return BS_ERR_INVALID_ARG;
+    if ((repetition || presence || frequency) && !history && !draft_tokens) return BS_ERR_INVALID_ARG;
+    if (bias_begin && n_bias > 0 && (!bias_tokens || !bias_values)) return BS_ERR_INVALID_ARG;
+    if (mask_row && n_masks > 0 && !masks) return BS_ERR_INVALID_ARG;
+    AdjustParams p = {logits, out, gamma, draft_tokens, node_parent, history, repetition, presence, frequency, bias_begin,
+                      bias_tokens, bias_values, masks, mask_row, status, extra, row_begin, row_end, B, R, Nmax, V, n_masks, n_bias,
+                      logits == out};
+    // Eight neighbours a lane where every row starts on 16 bytes and ends with a lane; else elements 32 apart.
+    const uintptr_t at = reinterpret_cast<uintptr_t>(logits) | reinterpret_cast<uintptr_t>(out) | (history ? reinterpret_cast<uintptr_t>(history) : 0);
+    const bool vec = V % kAdLane == 0 && at % 16 == 0;
+    return cuda_status(dtype == BS_F32 ? launch_adjust<float>(p, vec, (cudaStream_t)stream)
+                                       : launch_adjust<__nv_bfloat16>(p, vec, (cudaStream_t)stream));
+}

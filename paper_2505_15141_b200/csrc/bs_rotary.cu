@@ -1,0 +1,207 @@
+// bs_rotary, bs_rotary_frequencies: rotary positions of queries and keys.
+//
+//   (a, b) -> (a cos w - b sin w, b cos w + a sin w),   w = position * frequency of the pair
+//
+// A frequency is held in turns as a 64-bit binary fraction, so the angle modulo one turn is the low half of an integer
+// product: exact at every position, where the product in fp32 is off by 0.01 radians at position 100000.
+//
+// Bound by HBM: every element is read and written once.  A CTA takes a few tokens; its threads first compute the sines and
+// cosines of those tokens into shared memory (one pair of functions a thread), then sweep over heads x chunks of pairs: a sine is
+// computed once for all heads.  Four tokens of 64 pairs give each of 256 threads one pair; calls of few tokens take one token
+// a CTA, so that the heads of a token are spread over all its threads.
+#include "bs_common.cuh"
+
+namespace bs {
+
+constexpr int kRoThreads = 256;
+constexpr int kRoTokens = 4;                   // tokens of a CTA where there are enough of them
+constexpr int kRoMaxRot = 256;
+
+struct RotaryParams {
+    const void *q, *k;
+    void *q_out, *k_out;
+    long long q_st, q_sh, k_st, k_sh, qo_st, qo_sh, ko_st, ko_sh;
+    const int32_t* positions;
+    const uint64_t* freq;                      // [rot / 2] turns x 2^64
+    const int32_t* cu_new;
+    const int32_t* node_parent;                // NULL: chains
+    float amplitude;
+    int rot, T, Hq, H, d, B, Nmax;             // H: heads of q and k
+    int tokens, copy_rest;                     // of a CTA; the elements behind rot have to be copied
+};
+
+template <typename T, int P> struct alignas(sizeof(T) * P) RoVec { T v[P]; };
+
+__device__ __forceinline__ float ro_float(float x) { return x; }
+__device__ __forceinline__ float ro_float(__nv_bfloat16 x) { return __bfloat162float(x); }
+__device__ __forceinline__ void ro_set(float& y, float x) { y = x; }
+__device__ __forceinline__ void ro_set(__nv_bfloat16& y, float x) { y = __float2bfloat16_rn(x); }
+
+// Position of token t (a converged warp asks); < 0: the row is left alone.  A tree's node n stands depth(n) behind its root.
+__device__ __forceinline__ int ro_position(const RotaryParams& p, int t) {
+    const int lane = threadIdx.x & 31;
+    const int pos = __ldg(p.positions + t);
+    if (!p.node_parent || pos < 0) return pos;
+    // the sequence: the last b with cu_new[b] <= t, 32 candidates at a time
+    int lo = 0, n = p.B;
+    while (n > 1) {
+        const int step = (n + 31) / 32;
+        const int at = lane * step;
+        const unsigned le = __ballot_sync(0xffffffffu, at < n && __ldg(p.cu_new + lo + at) <= t);
+        if (!le) return -1;
+        const int last = 31 - __clz(le);
+        lo += last * step;
+        n = min(step, n - last * step);
+    }
+    const int c0 = __ldg(p.cu_new + lo), c1 = __ldg(p.cu_new + lo + 1), row = t - c0;
+    if (row < 0 || t >= c1 || row > p.Nmax) return -1;
+    int parent = 0;
+    if (lane < p.Nmax) {
+        parent = __ldg(p.node_parent + (size_t)lo * p.Nmax + lane);
+        if (parent < 0 || parent > lane) parent = 0;           // not an earlier node: hangs under the root
+    }
+    int depth = 0;
+    for (int node = row; node > 0; ++depth) node = __shfl_sync(0xffffffffu, parent, node - 1);
+    return pos - row + depth;
+}
+
+// P pairs are loaded as two vectors of P elements: the halves' (HALF), or 2P neighbours' (two by two).
+template <typename T, int P, bool HALF>
+__global__ void __launch_bounds__(kRoThreads) rotary_kernel(const RotaryParams p) {
+    __shared__ int s_pos[kRoTokens];
+    __shared__ __align__(16) float s_cos[kRoTokens * kRoMaxRot / 2], s_sin[kRoTokens * kRoMaxRot / 2];
+    const int tid = threadIdx.x, half = p.rot / 2, t0 = blockIdx.x * p.tokens, nt = min(p.tokens, p.T - t0);
+    pdl_enter();
+    for (int i = tid >> 5; i < nt; i += kRoThreads / 32) {
+        const int pos = ro_position(p, t0 + i);
+        if ((tid & 31) == 0) s_pos[i] = pos;
+    }
+    __syncthreads();
+    for (int i = tid; i < nt * half; i += kRoThreads) {
+        const int tok = i / half, j = i - tok * half, pos = s_pos[tok];
+        if (pos < 0) continue;
+        const int64_t turns = (int64_t)((uint64_t)(uint32_t)pos * __ldg(p.freq + j));   // of a turn, in [-1/2, 1/2) x 2^64
+        float s, c;
+        sincospif((float)turns * 1.0842021724855044e-19f, &s, &c);                      // 2^-63: half turns
+        // pair j of chunk j / P: the chunks of a warp's lanes lie side by side
+        const int at = tok * half + (j % P) * (half / P) + j / P;
+        s_cos[at] = c * p.amplitude;
+        s_sin[at] = s * p.amplitude;
+    }
+    __syncthreads();
+    const int n_rot = half / P, n_chunks = p.copy_rest ? p.d / (2 * P) : n_rot, per_token = p.H * n_chunks;
+    using Vec = RoVec<T, P>;
+    for (int i = tid; i < nt * per_token; i += kRoThreads) {
+        const int tok = i / per_token, w = i - tok * per_token, head = w / n_chunks, c = w - head * n_chunks;
+        if (s_pos[tok] < 0) continue;
+        const long long t = t0 + tok;
+        const bool is_q = head < p.Hq;
+        const long long hh = is_q ? head : head - p.Hq;
+        const T* x = is_q ? (const T*)p.q + t * p.q_st + hh * p.q_sh : (const T*)p.k + t * p.k_st + hh * p.k_sh;
+        T* y = is_q ? (T*)p.q_out + t * p.qo_st + hh * p.qo_sh : (T*)p.k_out + t * p.ko_st + hh * p.ko_sh;
+        const bool rotates = c < n_rot;
+        const int ia = HALF && rotates ? c * P : c * 2 * P, ib = HALF && rotates ? half + c * P : ia + P;   // rot = 2 P n_rot
+        Vec a = *reinterpret_cast<const Vec*>(x + ia), b = *reinterpret_cast<const Vec*>(x + ib);
+        if (rotates) {
+            const float *cs = s_cos + tok * half + c, *sn = s_sin + tok * half + c;
+#pragma unroll
+            for (int e = 0; e < P; ++e) {
+                T& ra = HALF ? a.v[e] : (2 * e < P ? a.v[(2 * e) % P] : b.v[(2 * e) % P]);
+                T& rb = HALF ? b.v[e] : (2 * e + 1 < P ? a.v[(2 * e + 1) % P] : b.v[(2 * e + 1) % P]);
+                const float fa = ro_float(ra), fb = ro_float(rb), co = cs[e * n_rot], si = sn[e * n_rot];
+                ro_set(ra, fmaf(fa, co, -fb * si));           // the one rounding to T
+                ro_set(rb, fmaf(fb, co, fa * si));
+            }
+        }
+        *reinterpret_cast<Vec*>(y + ia) = a;
+        *reinterpret_cast<Vec*>(y + ib) = b;
+    }
+}
+
+template <typename T, int P>
+static cudaError_t launch_rotary(const RotaryParams& p, bool half, cudaStream_t st) {
+    const int grid = div_up(p.T, p.tokens);
+    return half ? launch_pdl(rotary_kernel<T, P, true>, grid, kRoThreads, 0, st, p)
+                : launch_pdl(rotary_kernel<T, P, false>, grid, kRoThreads, 0, st, p);
+}
+
+}  // namespace bs
+
+using namespace bs;
+
+extern "C" bs_status bs_rotary_frequencies(bs_rotary_scaling scaling, int rot, double base, double factor, double low, double high,
+                                           double original, uint64_t* freq_host, float* amplitude_host) {
+    if (!freq_host || !amplitude_host) return BS_ERR_INVALID_ARG;
+    if (rot < 2 || rot > kRoMaxRot || (rot & 1)) return BS_ERR_UNSUPPORTED;
+    if (scaling < BS_ROTARY_PLAIN || scaling > BS_ROTARY_YARN || !(base > 1.0) || !isfinite(base)) return BS_ERR_INVALID_ARG;
+    if (scaling != BS_ROTARY_PLAIN && (!(factor >= 1.0) || !isfinite(factor))) return BS_ERR_INVALID_ARG;
+    if (scaling >= BS_ROTARY_BANDS && (!(original >= 1.0) || !(low > 0.0) || !(high > low) || !isfinite(high) || !isfinite(original)))
+        return BS_ERR_INVALID_ARG;
+    const double two_pi = 6.283185307179586476925;
+    double first = 0, last = 0;
+    if (scaling == BS_ROTARY_YARN) {
+        // the pairs that turn `high` and `low` times within the original length
+        first = fmax(floor(rot * log(original / (high * two_pi)) / (2 * log(base))), 0.0);
+        last = fmin(ceil(rot * log(original / (low * two_pi)) / (2 * log(base))), rot - 1.0);
+    }
+    for (int i = 0; i < rot / 2; ++i) {
+        double f = pow(base, -2.0 * i / rot);
+        if (scaling == BS_ROTARY_LINEAR) f /= factor;
+        if (scaling == BS_ROTARY_BANDS) {
+            const double keep = fmin(fmax((original * f / two_pi - low) / (high - low), 0.0), 1.0);
+            f *= keep + (1.0 - keep) / factor;
+        }
+        if (scaling == BS_ROTARY_YARN) {
+            const double ramp = fmin(fmax((i - first) / fmax(last - first, 0.001), 0.0), 1.0);
+            f *= 1.0 - ramp + ramp / factor;
+        }
+        freq_host[i] = (uint64_t)(f / two_pi * 18446744073709551616.0 + 0.5);    // f <= 1
+    }
+    *amplitude_host = scaling == BS_ROTARY_YARN ? (float)(0.1 * log(factor) + 1.0) : 1.0f;
+    return BS_OK;
+}
+
+extern "C" bs_status bs_rotary(const void* q, long long q_stride_t, long long q_stride_h, const void* k, long long k_stride_t,
+                               long long k_stride_h, bs_dtype dtype, const int32_t* positions, const uint64_t* freq,
+                               float amplitude, int rot, int interleaved, const int32_t* cu_new, const int32_t* node_parent, int B,
+                               int Nmax, int T, int Hq, int Hkv, int d, void* q_out, long long qo_stride_t, long long qo_stride_h,
+                               void* k_out, long long ko_stride_t, long long ko_stride_h, void* stream) {
+    if (T < 0 || Hq < 0 || Hkv < 0 || Hq + Hkv < 1 || d < 2 || !freq || (T > 0 && !positions)) return BS_ERR_INVALID_ARG;
+    if (dtype != BS_F32 && dtype != BS_BF16) return BS_ERR_INVALID_ARG;
+    if (T > 0 && ((Hq && (!q || !q_out)) || (Hkv && (!k || !k_out)))) return BS_ERR_INVALID_ARG;
+    if (node_parent && (!cu_new || B < 1 || Nmax < 0)) return BS_ERR_INVALID_ARG;
+    if (node_parent && (Nmax > BS_MAX_GAMMA || B > BS_MAX_BATCH)) return BS_ERR_UNSUPPORTED;
+    if (rot < 2 || rot > d || (rot & 1) || (d & 1) || rot > kRoMaxRot || Hq > 4096 || Hkv > 4096 || d > 4096) return BS_ERR_UNSUPPORTED;
+    if (!isfinite(amplitude)) return BS_ERR_INVALID_ARG;
+    if (T == 0) return BS_OK;
+    RotaryParams p = {};
+    p.q = q; p.k = k; p.q_out = q_out; p.k_out = k_out;
+    p.q_st = q_stride_t; p.q_sh = q_stride_h; p.k_st = k_stride_t; p.k_sh = k_stride_h;
+    p.qo_st = qo_stride_t; p.qo_sh = qo_stride_h; p.ko_st = ko_stride_t; p.ko_sh = ko_stride_h;
+    p.positions = positions; p.freq = freq; p.cu_new = cu_new; p.node_parent = node_parent;
+    p.amplitude = amplitude;
+    p.rot = rot; p.T = T; p.Hq = Hq; p.H = Hq + Hkv; p.d = d; p.B = B; p.Nmax = Nmax;
+    p.tokens = T >= 4 * kRoTokens * sm_count() ? kRoTokens : 1;
+    const bool q_moves = Hq && (q != q_out || q_stride_t != qo_stride_t || q_stride_h != qo_stride_h);
+    const bool k_moves = Hkv && (k != k_out || k_stride_t != ko_stride_t || k_stride_h != ko_stride_h);
+    p.copy_rest = rot < d && (q_moves || k_moves);
+    // the widest vector that divides both parts of a head and that every row starts on
+    const int es = dtype == BS_F32 ? 4 : 2;
+    auto fits = [&](int P) {
+        auto ok = [&](const void* x, long long st, long long sh) {
+            return reinterpret_cast<uintptr_t>(x) % (uintptr_t)(P * es) == 0 && st % P == 0 && sh % P == 0;
+        };
+        return (rot / 2) % P == 0 && (d - rot) % (2 * P) == 0 &&
+               (!Hq || (ok(q, q_stride_t, q_stride_h) && ok(q_out, qo_stride_t, qo_stride_h))) &&
+               (!Hkv || (ok(k, k_stride_t, k_stride_h) && ok(k_out, ko_stride_t, ko_stride_h)));
+    };
+    const cudaStream_t st = (cudaStream_t)stream;
+    const bool half = !interleaved;
+    if (dtype == BS_F32)
+        return cuda_status(fits(4) ? launch_rotary<float, 4>(p, half, st) : fits(2) ? launch_rotary<float, 2>(p, half, st)
+                                                                                    : launch_rotary<float, 1>(p, half, st));
+    return cuda_status(fits(8)   ? launch_rotary<__nv_bfloat16, 8>(p, half, st)
+                       : fits(4) ? launch_rotary<__nv_bfloat16, 4>(p, half, st)
+                       : fits(2) ? launch_rotary<__nv_bfloat16, 2>(p, half, st)
+                                 : launch_rotary<__nv_bfloat16, 1>(p, half, st));
+}

@@ -5,10 +5,10 @@
 //   x -= f c + p [c > 0],  c = times emitted or drafted on the way;   x += bias;   forbidden by the row's grammar mask: -inf
 //
 // adjust: bound by HBM; the rows are read and written once, the history once for all rows of a sequence.  A warp takes 256
-// tokens of the vocabulary of one sequence, eight a lane, and passes over the rows of that sequence.  It needs nothing from other
-// warps: it looks through the biases and drafted tokens for those in its range itself, in the order of the list, so that sums do
-// not depend on timing.  In place, lanes with nothing to change touch nothing, and tokens that are all forbidden are
-// written without being read.
+// tokens of the vocabulary of one sequence, eight a lane, and passes over the rows of that sequence; what the history and the biases
+// do to an element is worked out once for all rows.  Biases are added in the order of the list, so that sums do not
+// depend on timing.  In place, lanes with nothing to change touch nothing, and tokens that are all forbidden are written
+// without being read.
 //
 // history: entries of 16 bits, 2 x (times emitted, up to 16383) + (in the prompt).  A history that begins anew is built in
 // shared memory piece by piece and written once; what a round adds goes to its few entries by compare-and-swap.  Only whole
@@ -48,21 +48,23 @@ struct AdjustParams {
 constexpr int kAdWarps = 8;
 constexpr int kAdLane = 8;                     // tokens of a lane
 constexpr int kAdWarp = 32 * kAdLane;          // of a warp
-constexpr int kAdRows = 4;                     // rows in flight
-constexpr uint32_t kAdNothing = 0x100u;        // beside the allowed elements: nothing to do in this row
+constexpr int kAdTokens = kAdWarps * kAdWarp;  // of a CTA
 
-// Eight elements of a lane.  VEC: neighbours, two or one 16-byte accesses; else 32 apart, for rows that begin anywhere.
+// Eight elements of a lane.  VEC: neighbours, two or one 16-byte accesses of all of them; else 32 apart, one by one, for rows that
+// begin anywhere.  `need`: a bit for each element.
 template <typename T, bool VEC> struct AdIo;
 template <typename T> struct AdIo<T, true> {
     static constexpr int kWords = (int)sizeof(T) * 2;
-    __device__ static __forceinline__ void load(const T* p, int, uint32_t (&w)[kWords]) {
+    __device__ static __forceinline__ void load(const T* p, uint32_t need, uint32_t (&w)[kWords]) {
+        if (!need) return;
 #pragma unroll
         for (int i = 0; i < kWords; i += 4) {
             const uint4 v = *reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(p) + 4 * i);
             w[i] = v.x; w[i + 1] = v.y; w[i + 2] = v.z; w[i + 3] = v.w;
         }
     }
-    __device__ static __forceinline__ void store(T* p, int, const uint32_t (&w)[kWords]) {
+    __device__ static __forceinline__ void store(T* p, uint32_t need, const uint32_t (&w)[kWords]) {
+        if (!need) return;
 #pragma unroll
         for (int i = 0; i < kWords; i += 4)
             *reinterpret_cast<uint4*>(reinterpret_cast<char*>(p) + 4 * i) = make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]);
@@ -70,31 +72,30 @@ template <typename T> struct AdIo<T, true> {
 };
 template <> struct AdIo<float, false> {
     static constexpr int kWords = 8;
-    __device__ static __forceinline__ void load(const float* p, int n, uint32_t (&w)[8]) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) w[e] = 32 * e < n ? __float_as_uint(p[32 * e]) : 0u;
-    }
-    __device__ static __forceinline__ void store(float* p, int n, const uint32_t (&w)[8]) {
+    __device__ static __forceinline__ void load(const float* p, uint32_t need, uint32_t (&w)[8]) {
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-            if (32 * e < n) p[32 * e] = __uint_as_float(w[e]);
+            if ((need >> e) & 1u) w[e] = __float_as_uint(p[32 * e]);
+    }
+    __device__ static __forceinline__ void store(float* p, uint32_t need, const uint32_t (&w)[8]) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if ((need >> e) & 1u) p[32 * e] = __uint_as_float(w[e]);
     }
 };
 template <> struct AdIo<__nv_bfloat16, false> {
     static constexpr int kWords = 4;
-    __device__ static __forceinline__ void load(const __nv_bfloat16* p, int n, uint32_t (&w)[4]) {
+    __device__ static __forceinline__ void load(const __nv_bfloat16* p, uint32_t need, uint32_t (&w)[4]) {
         const unsigned short* u = reinterpret_cast<const unsigned short*>(p);
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            w[e] = (64 * e < n ? (uint32_t)u[64 * e] : 0u) | (64 * e + 32 < n ? (uint32_t)u[64 * e + 32] << 16 : 0u);
+        for (int e = 0; e < 8; ++e)
+            if ((need >> e) & 1u) w[e >> 1] |= (uint32_t)u[32 * e] << (16 * (e & 1));
     }
-    __device__ static __forceinline__ void store(__nv_bfloat16* p, int n, const uint32_t (&w)[4]) {
+    __device__ static __forceinline__ void store(__nv_bfloat16* p, uint32_t need, const uint32_t (&w)[4]) {
         unsigned short* u = reinterpret_cast<unsigned short*>(p);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            if (64 * e < n) u[64 * e] = (unsigned short)w[e];
-            if (64 * e + 32 < n) u[64 * e + 32] = (unsigned short)(w[e] >> 16);
-        }
+        for (int e = 0; e < 8; ++e)
+            if ((need >> e) & 1u) u[32 * e] = (unsigned short)(w[e >> 1] >> (16 * (e & 1)));
     }
 };
 __device__ __forceinline__ void ad_unpack(const uint32_t (&w)[8], float (&f)[8]) {
@@ -119,48 +120,103 @@ __device__ __forceinline__ void ad_pack(const float (&f)[8], uint32_t (&w)[4]) {
         w[e] = *reinterpret_cast<const uint32_t*>(&b);
     }
 }
+// What is not allowed becomes -inf, in the type's own bits.
+__device__ __forceinline__ void ad_forbid(uint32_t allowed, uint32_t (&w)[8]) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        if (!((allowed >> e) & 1u)) w[e] = 0xff800000u;
+}
+__device__ __forceinline__ void ad_forbid(uint32_t allowed, uint32_t (&w)[4]) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const uint32_t keep = ((allowed >> (2 * e)) & 1u ? 0x0000ffffu : 0u) | ((allowed >> (2 * e + 1)) & 1u ? 0xffff0000u : 0u);
+        w[e] = (w[e] & keep) | (0xff80ff80u & ~keep);
+    }
+}
+
+// The biases of a CTA's tokens, summed in the order of the list: 256 entries at a time, those that fall into the CTA's range added
+// warp after warp and lane after lane.  True if there were any in this warp's range.
+__device__ __forceinline__ bool ad_biases(const AdjustParams& p, int b, int v0, int& bits, float* s_bias, uint32_t* s_warps, uint32_t* s_ranges) {
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int lo = __ldg(p.bias_begin + b), hi = __ldg(p.bias_begin + b + 1);
+    if (lo < 0 || hi > p.n_bias || lo > hi) bits |= BS_DEV_BAD_LENGTH;
+    if (lo < 0 || hi > p.n_bias || lo >= hi) return false;    // the same for the whole CTA
+    for (int i = tid; i < kAdTokens; i += kAdWarps * 32) s_bias[i] = 0.f;
+    if (tid == 0) *s_ranges = 0u;
+#pragma unroll 1
+    for (int i = lo; i < hi; i += kAdWarps * 32) {
+        if (tid == 0) *s_warps = 0u;
+        const int t = i + tid < hi ? __ldg(p.bias_tokens + i + tid) : 0;
+        const float v = i + tid < hi ? __ldg(p.bias_values + i + tid) : 0.f;
+        const bool good = t >= 0 && t < p.V;
+        if (!good) bits |= BS_DEV_BAD_TOKEN;
+        const bool hit = i + tid < hi && good && t >= v0 && t < v0 + kAdTokens;
+        const uint32_t who = __ballot_sync(0xffffffffu, hit);
+        __syncthreads();                                      // cleared, and the batch before is through
+        if (hit) atomicOr(s_ranges, 1u << ((t - v0) / kAdWarp));
+        if (who && lane == 0) atomicOr(s_warps, 1u << warp);
+        __syncthreads();
+        uint32_t turn = *s_warps;
+        while (turn) {
+            const int w = __ffs(turn) - 1;
+            turn &= turn - 1;
+            if (warp == w)
+                for (uint32_t m = who; m; m &= m - 1) {
+                    if (lane == __ffs(m) - 1) s_bias[t - v0] += v;
+                    __syncwarp();
+                }
+            __syncthreads();
+        }
+    }
+    return (*s_ranges >> warp) & 1u;
+}
 
 template <typename T, bool VEC>
-__global__ void __launch_bounds__(kAdWarps * 32) logits_adjust_kernel(const AdjustParams p) {
+__global__ void __launch_bounds__(kAdWarps * 32, 4) logits_adjust_kernel(const AdjustParams p) {
     using Io = AdIo<T, VEC>;
-    __shared__ float s_bias[kAdWarps][kAdWarp];
+    constexpr int kRows = 8 / sizeof(T);                      // in flight: 64 bytes a lane
+    __shared__ float s_bias[kAdTokens];
+    __shared__ uint32_t s_warps, s_ranges;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, b = blockIdx.y;
-    const int chunk = blockIdx.x * kAdWarps + warp, v0 = chunk * kAdWarp;
+    const int cta_v0 = blockIdx.x * kAdTokens, v0 = cta_v0 + warp * kAdWarp;
     pdl_enter();
-    if (v0 >= p.V) return;
     const int first = VEC ? v0 + lane * kAdLane : v0 + lane;  // token of element 0
-    const int left = p.V - first;                             // VEC: >= 8 or <= 0; else: elements 32 e < left are there
+    // elements of this lane that are there (VEC: V is a multiple of 8)
+    const uint32_t there = VEC ? (first < p.V ? 0xffu : 0u)
+                               : (first < p.V ? 0xffu >> (7 - min(7, (p.V - 1 - first) >> 5)) : 0u);
+    const bool pen = p.repetition || p.presence || p.frequency;
+    uint32_t h[4] = {0u, 0u, 0u, 0u};
+    if (pen && p.history)
+        AdIo<__nv_bfloat16, VEC>::load(reinterpret_cast<const __nv_bfloat16*>(p.history) + (size_t)b * p.V + first, there, h);
+    const float rep = p.repetition ? __ldg(p.repetition + b) : 1.f, pres = p.presence ? __ldg(p.presence + b) : 0.f,
+                freq = p.frequency ? __ldg(p.frequency + b) : 0.f;
+    int mask = p.mask_row && lane < p.R ? __ldg(p.mask_row + (size_t)b * p.R + lane) : -1;   // of row `lane`
+    int tok = -1, parent = 0;                                 // drafted token `lane`; parent of node `lane`
+    if (pen && p.draft_tokens) {
+        if (lane < p.N) tok = __ldg(p.draft_tokens + (size_t)b * p.N + lane);
+        if (p.node_parent && lane >= 1 && lane <= p.N) parent = __ldg(p.node_parent + (size_t)b * p.N + lane - 1);
+    }
     int bits = 0, rows = p.row_end;
     if (p.gamma) {
         int g = __ldg(p.gamma + b);
         if (g < 0 || g + p.extra > p.R) { g = 0; bits |= BS_DEV_BAD_GAMMA; }
         rows = min(rows, g + p.extra);
     }
-    if (rows <= p.row_begin && !(p.status && chunk == 0)) return;
-    // grammar mask of every row, row by lane
-    int mask = -1;
-    if (p.mask_row && lane < p.R) {
-        mask = __ldg(p.mask_row + (size_t)b * p.R + lane);
-        if (mask < -1 || mask >= p.n_masks) {
-            mask = -1;
-            if (lane >= p.row_begin && lane < rows) bits |= BS_DEV_BAD_MASK;
-        }
+    if (rows <= p.row_begin && !(p.status && blockIdx.x == 0)) return;   // the whole CTA
+    const bool biased = p.bias_begin && ad_biases(p, b, cta_v0, bits, s_bias, &s_warps, &s_ranges);
+    if (mask < -1 || mask >= p.n_masks) {
+        mask = -1;
+        if (lane >= p.row_begin && lane < rows) bits |= BS_DEV_BAD_MASK;
     }
-    const bool pen = p.repetition || p.presence || p.frequency;
-    const float rep = p.repetition ? __ldg(p.repetition + b) : 1.f, inv = 1.f / rep;
-    const float pres = p.presence ? __ldg(p.presence + b) : 0.f, freq = p.frequency ? __ldg(p.frequency + b) : 0.f;
-    // drafted tokens, one a lane, and the rows (a bit each) that stand behind them
-    int tok = -1;
+    // the rows (a bit each) that stand behind drafted token `lane`
     uint32_t behind = 0u;
     if (pen && p.draft_tokens) {
-        if (lane < p.N) tok = __ldg(p.draft_tokens + (size_t)b * p.N + lane);
         if (p.node_parent) {
-            int parent = lane >= 1 && lane <= p.N ? __ldg(p.node_parent + (size_t)b * p.N + lane - 1) : 0;
             if (parent < 0 || (lane > 0 && parent >= lane)) {
                 if (lane < rows) bits |= BS_DEV_BAD_TREE;
                 parent = 0;
             }
-            const uint32_t anc = tree_ancestors(parent, p.N);
+            const uint32_t anc = tree_ancestors(parent, min(p.N, rows - 1));
 #pragma unroll 1
             for (int r = 1; r < rows; ++r) {                  // node lane + 1 among the ancestors of node r
                 const uint32_t of_row = __shfl_sync(0xffffffffu, anc, r);
@@ -171,15 +227,12 @@ __global__ void __launch_bounds__(kAdWarps * 32) logits_adjust_kernel(const Adju
         }
         if (lane < p.N && (tok < 0 || tok >= p.V) && lane < rows - 1) bits |= BS_DEV_BAD_TOKEN;
     }
+    if (p.status && blockIdx.x == 0 && bits) atomicOr(p.status + b, bits);
     const uint32_t drafted = __ballot_sync(0xffffffffu, behind && tok >= v0 && tok < min(v0 + kAdWarp, p.V));
 
-    // history: factor and summand of every element
-    const bool here = left > 0;
-    uint32_t h[4] = {0u, 0u, 0u, 0u};
-    if (pen && p.history && here)
-        AdIo<__nv_bfloat16, VEC>::load(reinterpret_cast<const __nv_bfloat16*>(p.history) + (size_t)b * p.V + first, left, h);
+    // what the history and the biases do to every element
     float add[8];
-    uint32_t seen = 0u, counted = 0u;
+    uint32_t seen = 0u, counted = 0u, any = 0u;
 #pragma unroll
     for (int e = 0; e < 8; ++e) add[e] = 0.f;
     if (h[0] | h[1] | h[2] | h[3]) {
@@ -193,125 +246,93 @@ __global__ void __launch_bounds__(kAdWarps * 32) logits_adjust_kernel(const Adju
             }
         }
     }
-    uint32_t any = seen;
-    if (p.bias_begin) {
-        const int lo = __ldg(p.bias_begin + b), hi = __ldg(p.bias_begin + b + 1);
-        if (lo < 0 || hi > p.n_bias || lo > hi) {
-            bits |= BS_DEV_BAD_LENGTH;
-        } else if (lo < hi) {
-            float* sb = s_bias[warp];
+    any = seen;
+    if (biased) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) sb[32 * e + lane] = 0.f;
-            __syncwarp();
-            bool hits = false;
-            int next = lo + lane < hi ? __ldg(p.bias_tokens + lo + lane) : -1;
-#pragma unroll 1
-            for (int i = lo; i < hi; i += 32) {
-                const int t = next - v0;
-                if (i + lane < hi && (next < 0 || next >= p.V)) bits |= BS_DEV_BAD_TOKEN;
-                next = i + 32 + lane < hi ? __ldg(p.bias_tokens + i + 32 + lane) : -1;
-                const bool hit = t >= 0 && t < kAdWarp;       // the end of a list reads as token -1: t < 0
-                uint32_t who = __ballot_sync(0xffffffffu, hit);
-                hits = hits || who;
-                const float v = hit ? __ldg(p.bias_values + i + lane) : 0.f;
-                while (who) {                                 // in the order of the list: a token may be listed twice
-                    const int l = __ffs(who) - 1;
-                    who &= who - 1;
-                    if (lane == l) sb[t] += v;
-                    __syncwarp();
-                }
-            }
-            if (hits) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float v = sb[VEC ? lane * 8 + e : 32 * e + lane];
-                    add[e] += v;
-                    if (v != 0.f) any |= 1u << e;
-                }
-            }
+        for (int e = 0; e < 8; ++e) {
+            const float v = s_bias[warp * kAdWarp + (VEC ? lane * 8 + e : 32 * e + lane)];
+            add[e] += v;
+            if (v != 0.f) any |= 1u << e;
         }
     }
-
-    if (p.status && chunk == 0) {
-        bits = (int)__reduce_or_sync(0xffffffffu, (unsigned)bits);
-        if (lane == 0 && bits) atomicOr(p.status + b, bits);
-    }
+    any &= there;
+    const bool special = drafted || __any_sync(0xffffffffu, any);
+    const float inv = 1.f / rep;
 
     const T* x = reinterpret_cast<const T*>(p.x) + (size_t)b * p.R * p.V + first;
     T* y = reinterpret_cast<T*>(p.y) + (size_t)b * p.R * p.V + first;
     const size_t mask_words = (size_t)((p.V + 31) >> 5);
+    // what of a lane's elements the drafted tokens before a row fall on
+    auto drafted_on = [&](int row, auto&& found) {
+        uint32_t d = drafted;
 #pragma unroll 1
-    for (int r0 = p.row_begin; r0 < rows; r0 += kAdRows) {
-        uint32_t w[kAdRows][Io::kWords], allowed[kAdRows], own[kAdRows];
-        // allowed elements of every row
+        while (d) {
+            const int l = __ffs(d) - 1;
+            d &= d - 1;
+            const int t = __shfl_sync(0xffffffffu, tok, l) - v0;
+            const uint32_t rr = __shfl_sync(0xffffffffu, behind, l);
+            if ((VEC ? t >> 3 : t & 31) == lane && ((rr >> (row & 31)) & 1u)) found(VEC ? t & 7 : t >> 5);
+        }
+    };
+#pragma unroll 1
+    for (int r0 = p.row_begin; r0 < rows; r0 += kRows) {
+        uint32_t w[kRows][Io::kWords], allowed[kRows], own[kRows];
 #pragma unroll
-        for (int k = 0; k < kAdRows; ++k) {
+        for (int k = 0; k < kRows; ++k) {                   // allowed elements of every row
             const int m = __shfl_sync(0xffffffffu, mask, (r0 + k) & 31);
-            allowed[k] = 0xffu;
+            allowed[k] = there;
+            own[k] = 0u;
             if (m >= 0 && r0 + k < rows) {
                 const uint32_t* words = p.masks + (size_t)m * mask_words + (v0 >> 5);
                 if (VEC) {
-                    if (here) allowed[k] = __ldg(reinterpret_cast<const unsigned char*>(words) + lane);
+                    if (there) allowed[k] = __ldg(reinterpret_cast<const unsigned char*>(words) + lane);
                 } else {
                     const uint32_t word = lane < 8 && v0 + 32 * lane < p.V ? __ldg(words + lane) : 0u;
                     uint32_t a = 0u;
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) a |= ((__shfl_sync(0xffffffffu, word, e) >> lane) & 1u) << e;
-                    allowed[k] = a;
+                    for (int e = 0; e < 8; ++e)
+                        if ((__shfl_sync(0xffffffffu, word, e) >> lane) & 1u) a |= 1u << e;
+                    allowed[k] = a & there;
                 }
             }
         }
-        // what of a lane's elements the drafted tokens before a row fall on
-        auto drafted_on = [&](int row, auto&& found) {
-            uint32_t d = drafted;
-#pragma unroll 1
-            while (d) {
-                const int l = __ffs(d) - 1;
-                d &= d - 1;
-                const int t = __shfl_sync(0xffffffffu, tok, l) - v0;
-                const uint32_t rr = __shfl_sync(0xffffffffu, behind, l);
-                if ((VEC ? t >> 3 : t & 31) == lane && ((rr >> (row & 31)) & 1u)) found(VEC ? t & 7 : t >> 5);
-            }
-        };
 #pragma unroll
-        for (int k = 0; k < kAdRows; ++k) {
-            own[k] = 0u;
-            if (drafted) drafted_on(r0 + k, [&](int e) { own[k] |= 1u << e; });
-            const bool active = here && r0 + k < rows;
-            if (!active || (p.in_place && allowed[k] == 0xffu && !(any | own[k]))) allowed[k] = kAdNothing;
+        for (int k = 0; k < kRows; ++k) {
 #pragma unroll
             for (int i = 0; i < Io::kWords; ++i) w[k][i] = 0u;
-            if (allowed[k] & 0xffu) Io::load(x + (size_t)(r0 + k) * p.V, left, w[k]);
+            if (r0 + k >= rows) continue;
+            if (drafted) drafted_on(r0 + k, [&](int e) { own[k] |= 1u << e; });
+            // in place only what changes is needed (VEC: all eight, unless none changes or all are forbidden)
+            uint32_t need = allowed[k];
+            if (p.in_place && (!VEC || allowed[k] == there)) need &= any | own[k];
+            Io::load(x + (size_t)(r0 + k) * p.V, need, w[k]);
         }
 #pragma unroll
-        for (int k = 0; k < kAdRows; ++k) {
-            float f[8];
-            ad_unpack(w[k], f);
-            if (any | own[k]) {
+        for (int k = 0; k < kRows; ++k) {
+            if (r0 + k >= rows) continue;
+            if (special) {
+                float f[8];
+                ad_unpack(w[k], f);
+                const uint32_t penalised = seen | own[k];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    if (((seen | own[k]) >> e) & 1u) f[e] *= f[e] > 0.f ? inv : rep;
+                    if ((penalised >> e) & 1u) f[e] *= f[e] > 0.f ? inv : rep;
                     f[e] += add[e];
                 }
-            }
-            if (drafted) {                                    // they count like emitted ones
-                uint32_t known = counted;
-                drafted_on(r0 + k, [&](int hit) {
-                    const float less = (known >> hit) & 1u ? freq : freq + pres;
-                    known |= 1u << hit;
+                if (drafted) {                                // they count like emitted ones
+                    uint32_t known = counted;
+                    drafted_on(r0 + k, [&](int hit) {
+                        const float less = (known >> hit) & 1u ? freq : freq + pres;
+                        known |= 1u << hit;
 #pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if (e == hit) f[e] -= less;
-                });
+                        for (int e = 0; e < 8; ++e)
+                            if (e == hit) f[e] -= less;
+                    });
+                }
+                ad_pack(f, w[k]);
             }
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (!((allowed[k] >> e) & 1u)) f[e] = -INFINITY;
-            if (!(allowed[k] & kAdNothing)) {
-                uint32_t o[Io::kWords];
-                ad_pack(f, o);
-                Io::store(y + (size_t)(r0 + k) * p.V, left, o);
-            }
+            if (allowed[k] != there) ad_forbid(allowed[k], w[k]);
+            Io::store(y + (size_t)(r0 + k) * p.V, p.in_place ? there & (any | own[k] | ~allowed[k]) : there, w[k]);
         }
     }
 }

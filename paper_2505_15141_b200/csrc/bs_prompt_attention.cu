@@ -47,6 +47,7 @@ template <int D> struct PaLayout {
     static constexpr int kRing = D == 128 ? 5 : 10;
     static constexpr int kDynamic = (2 + kRing) * kTileBytes + 1024;
     static constexpr int kColO = 256;
+    static constexpr int kPoly = D == 128 ? 4 : 6;            // of 16 pairs of exponentials, those that the FMA units compute
     static constexpr uint32_t kTmemCols = 512;
 };
 
@@ -115,10 +116,27 @@ __device__ __forceinline__ uint64_t pa_add2(uint64_t a, uint64_t b) {
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
     return r;
 }
-__device__ __forceinline__ float pa_max3(float a, float b, float c) {
+__device__ __forceinline__ float pa_max3(float a, float b, float c) {   // NaN if one is
     float r;
-    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
     return r;
+}
+// 2^x of two numbers up to 2^22 without the special-function unit: x = n + f, |f| <= 1/2, n by rounding to whole numbers in
+// fp32; 2^f as a cubic through 1 at 0, fitted to the smallest largest relative error (1.02e-4, a fortieth of what rounding to bf16
+// adds); n goes to the exponent.  Below -127 the result is 0, in the last step above it something below 2^-126.
+__device__ __forceinline__ uint64_t pa_exp2x2(uint64_t x2) {
+    float x, y, rx, ry;
+    pa_upk(x2, x, y);
+    x2 = pa_pk(fmaxf(x, -127.f), fmaxf(y, -127.f));
+    const uint64_t r2 = pa_add2(x2, pa_pk(12582912.f, 12582912.f));          // 1.5 x 2^23: n in the low bits
+    const uint64_t f2 = pa_fma2(pa_add2(r2, pa_pk(-12582912.f, -12582912.f)), pa_pk(-1.f, -1.f), x2);
+    uint64_t p2 = pa_fma2(f2, pa_pk(0.05500767f, 0.05500767f), pa_pk(0.2422092f, 0.2422092f));
+    p2 = pa_fma2(p2, f2, pa_pk(0.69328287f, 0.69328287f));
+    p2 = pa_fma2(p2, f2, pa_pk(1.f, 1.f));
+    pa_upk(r2, rx, ry);
+    pa_upk(p2, x, y);
+    return pa_pk(__uint_as_float(__float_as_uint(x) + (__float_as_uint(rx) << 23)),
+                 __uint_as_float(__float_as_uint(y) + (__float_as_uint(ry) << 23)));
 }
 __device__ __forceinline__ uint32_t pa_bf16x2(float lo, float hi) {
     uint32_t r;
@@ -239,7 +257,7 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
     extern __shared__ unsigned char pa_smem_raw[];
     unsigned char* s_q = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(pa_smem_raw) + 1023) & ~(uintptr_t)1023);
     unsigned char* s_kv = s_q + 2 * L::kTileBytes;            // K and V of a tile of keys follow one another in the ring
-    __shared__ __align__(8) unsigned long long b_full[RING], b_empty[RING], b_qfull[2], b_qempty[2], b_s[2], b_p[2], b_o[2],
+    __shared__ __align__(8) unsigned long long b_full[RING], b_empty[RING], b_qfull[2], b_qempty[2], b_s[2], b_p[2][2], b_o[2],
         b_item[kPaItems], b_done[kPaItems], b_next, b_drain;
     __shared__ PaItem s_item[kPaItems];
     __shared__ int s_first[kPaItems][D];                      // see pa_clean_v
@@ -258,7 +276,8 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
             mbar_init(smem_u32(&b_qfull[i]), 1);
             mbar_init(smem_u32(&b_qempty[i]), 1);
             mbar_init(smem_u32(&b_s[i]), 1);
-            mbar_init(smem_u32(&b_p[i]), 4);
+            mbar_init(smem_u32(&b_p[i][0]), 4);               // the first half of the keys, the second
+            mbar_init(smem_u32(&b_p[i][1]), 4);
             mbar_init(smem_u32(&b_o[i]), 1);
         }
         for (int s = 0; s < kPaItems; ++s) {
@@ -427,14 +446,19 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 if (have_p && jp < (i ? prev.nt1 : prev.nt0)) {
-                    ok = ok && wait(&b_full[v_at], v_ph) && wait(&b_p[i], steps[i] & 1);
-                    if (!ok) break;
-                    ++steps[i];
-                    tc_fence_after();
+                    ok = ok && wait(&b_full[v_at], v_ph);
                     const uint64_t dv = ca_desc(smem_u32(s_kv + v_at * L::kTileBytes), L::kChunk, 1024, 2);
 #pragma unroll
-                    for (int s = 0; s < kPaKeys / 16; ++s)
+                    for (int s = 0; s < kPaKeys / 16; ++s) {
+                        if (s % (kPaKeys / 32) == 0) {        // half of P is there
+                            ok = ok && wait(&b_p[i][s / (kPaKeys / 32)], steps[i] & 1);
+                            if (!ok) break;
+                            tc_fence_after();
+                        }
                         pa_mma_ts(tmem + L::kColO + i * D, tmem + i * 128 + s * 8, dv + ((s * 2048) >> 4), id_o, (jp | s) ? 1u : 0u, elected);
+                    }
+                    if (!ok) break;
+                    ++steps[i];
                     ca_commit(smem_u32(&b_o[i]), elected);
                 }
                 if (have_p && i == 1) ca_commit(smem_u32(&b_empty[v_at]), elected);
@@ -490,6 +514,7 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
             const PaItem it = s_item[slot];
             if (it.nt0 == 0) break;
             const int nt = (i ? it.nt1 : it.nt0), i0 = it.i0 + i * p.TQ, pos = i0 + tok;
+            const bool valid = tok < p.TQ && pos < it.n;
             float m = -INFINITY, l = 0.f;
 #pragma unroll 1
             for (int j = 0; j < nt; ++j, ++steps) {
@@ -518,20 +543,23 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
                 }
                 float a[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) a[e] = fmaxf(s[e], s[e + 4]);
+                for (int e = 0; e < 4; ++e) a[e] = pa_max3(s[e], s[e + 4], s[e + 8]);
 #pragma unroll
-                for (int c = 8; c < 128; c += 8)
+                for (int c = 12; c < 124; c += 8)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) a[e] = pa_max3(a[e], s[c + e], s[c + e + 4]);
-                const float mx = fmaxf(fmaxf(a[0], a[1]), fmaxf(a[2], a[3])) * p.c;
+                float mx = pa_max3(pa_max3(a[0], a[1], a[2]), pa_max3(a[3], s[124], s[125]), pa_max3(s[126], s[127], s[127])) * p.c;
+                if (!(mx < INFINITY)) mx = __int_as_float(0x7fc00000);   // a row that sees a NaN or an infinite score: all NaN
+                const bool moves = valid && !(mx <= m + kPaSlack);
                 if (j == 0) {
                     m = mx;
-                } else if (__any_sync(0xffffffffu, mx > m + kPaSlack)) {
+                } else if (__any_sync(0xffffffffu, moves)) {
                     // the products so far
                     ok = pa_wait(smem_u32(&b_o[i]), (steps - 1) & 1);
                     if (!ok) break;
                     tc_fence_after();
-                    const float mn = fmaxf(m, mx), f = mn == -INFINITY ? 1.f : ex2(m - mn);
+                    // a row's own scores alone decide when its reference moves: its result does not depend on the others
+                    const float mn = moves ? mx : m, f = moves ? ex2(m - mn) : 1.f;
                     m = mn;
                     l *= f;
 #pragma unroll 1
@@ -553,22 +581,31 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
                     uint32_t w[16];
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
+                        uint64_t x2 = pa_fma2(pa_pk(s[c + 2 * e], s[c + 2 * e + 1]), c2, nm2);
                         float x, y;
-                        pa_upk(pa_fma2(pa_pk(s[c + 2 * e], s[c + 2 * e + 1]), c2, nm2), x, y);
-                        x = ex2(x);
-                        y = ex2(y);
-                        sum[e & 1] = pa_add2(sum[e & 1], pa_pk(x, y));
+                        if ((e * L::kPoly) % 16 < L::kPoly) {
+                            x2 = pa_exp2x2(x2);
+                            pa_upk(x2, x, y);
+                        } else {
+                            pa_upk(x2, x, y);
+                            x = ex2(x);
+                            y = ex2(y);
+                            x2 = pa_pk(x, y);
+                        }
+                        sum[e & 1] = pa_add2(sum[e & 1], x2);
                         w[e] = pa_bf16x2(x, y);
                     }
                     pa_st16(t_s + (c >> 1), w);
+                    if (c & 32) {                             // half of P: the product may begin
+                        ca_st_wait();
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(smem_u32(&b_p[i][c >> 6]));
+                    }
                 }
                 float s0, s1;
                 pa_upk(pa_add2(sum[0], sum[1]), s0, s1);
                 l += s0 + s1;
-                ca_st_wait();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&b_p[i]));
             }
             if (!ok) break;
             if (nt > 0) {
@@ -576,7 +613,6 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
                 if (!ok) break;
                 tc_fence_after();
                 const float inv = 1.f / l;
-                const bool valid = tok < p.TQ && pos < it.n;
                 __nv_bfloat16* o = p.out + (long long)(it.row0 + pos) * p.o_st + (long long)(it.h * p.G + head) * p.o_sh;
                 const int* first = s_first[slot];
 #pragma unroll 1

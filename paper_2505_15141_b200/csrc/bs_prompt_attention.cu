@@ -12,11 +12,13 @@
 // group share the copies of K and V and short prompts fill the tiles.  Two tiles are in flight: while the softmax of one
 // runs, the tensor cores work on the other.
 //
-// Warps: 0-3 and 4-7 softmax of the two tiles, a row a thread; 8 MMA issuer; 9 copies (TMA); 10 scheduler.  The grid has a CTA for
-// every item, each sequence's last rows, the longest, first; a running CTA takes over the item of one that has not begun
+// Warps: 0-3 and 4-7 softmax of the two tiles, a row a thread; 8 MMA issuer; 9 copies (TMA); 10 scheduler; 11 looks through the tiles
+// of V that are seen in part.  The grid has a CTA for
+// every item, the longest first; a running CTA takes over the item of one that has not begun
 // (cluster launch control), so that copies and products of the next item begin under the end of the one before.
 //
-// Tensor memory: S / P of the tiles at columns 0 and 128, O at 256 and 256 + D.
+// Heads of 128 fill tensor memory with S and O of two tiles, and P takes the place of S; the chain of a tile is then S, softmax, P V, S of
+// the next keys.  Heads of 64 leave room for P beside S, which takes the products out of that chain.
 #include "bs_cache_attention.cuh"
 
 namespace bs {
@@ -44,10 +46,15 @@ template <int D> struct PaLayout {
     static constexpr int kTileBytes = kPaKeys * D * 2;        // of Q, K or V
     static constexpr int kChunk = 128 * 128;                  // 128 rows of 64 elements
     static constexpr int kChunks = D / 64;
-    static constexpr int kRing = D == 128 ? 5 : 10;
-    static constexpr int kDynamic = (2 + kRing) * kTileBytes + 1024;
-    static constexpr int kColO = 256;
-    static constexpr int kPoly = D == 128 ? 4 : 6;            // of 16 pairs of exponentials, those that the FMA units compute
+    static constexpr int kRing = D == 128 ? 4 : 8;            // even
+    static constexpr int kOut = 32 * 128;                     // 32 rows of 64 results, for each softmax warp
+    static constexpr int kDynamic = (2 + kRing) * kTileBytes + 8 * kOut + 1024;
+    // Tensor memory: the scores of row tile i at i * kColS, its probabilities kColP further, its accumulator at kColO + i * D.  Heads of 64
+    // leave room for P beside S.
+    static constexpr bool kApart = D == 64;
+    static constexpr int kColS = kApart ? 192 : 128, kColP = kApart ? 128 : 0, kColO = 2 * kColS;
+    static_assert(kColO + 2 * D <= 512, "tensor memory");
+    static constexpr int kPoly = D == 128 ? 2 : 4;            // of 16 pairs of exponentials, those that the FMA units compute
     static constexpr uint32_t kTmemCols = 512;
 };
 
@@ -146,8 +153,11 @@ __device__ __forceinline__ uint32_t pa_bf16x2(float lo, float hi) {
 
 __device__ __forceinline__ void pa_few_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 80;"); }
 
-// Bounded wait of a converged warp, in line: with a call anywhere in the kernel its registers cannot be split unevenly.
-__device__ __forceinline__ bool pa_wait(uint32_t bar, uint32_t parity) {
+// Bounded wait of a converged warp; false if it gave up or another role has.  In line: with a call anywhere in the kernel its
+// registers cannot be split unevenly.  What has arrived already, the usual case, costs one try and one vote; looking at the other
+// roles' word there as well made it 150 cycles, on the path from product to product.
+__device__ __forceinline__ bool pa_wait(const void* barrier, uint32_t parity, const volatile int* gave_up) {
+    const uint32_t bar = smem_u32(barrier);
     if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
     const long long t0 = clock64();
     uint32_t ok;
@@ -157,45 +167,62 @@ __device__ __forceinline__ bool pa_wait(uint32_t bar, uint32_t parity) {
             "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
             "selp.u32 %0, 1, 0, p;\n\t}"
             : "=r"(ok) : "r"(bar), "r"(parity), "r"(1000000u) : "memory");
-    } while (!ok && clock64() - t0 <= kWaitCycles);
+    } while (!ok && !*gave_up && clock64() - t0 <= kWaitCycles);
     return __all_sync(0xffffffffu, ok != 0);
 }
 
 // A tile of V that some rows see only in part: 0 * NaN is NaN, so what a row must not see may not be there.  Tokens behind the
 // sequence become zero.  Elements that are not finite become zero, too, and first[element] the first token that has one there:
-// rows from that token on see it, and get NaN.  `t` of 128 threads.
+// rows from that token on see it, and get NaN.  One warp; where everything is finite it only reads: x * 0 is added up, which is NaN
+// once x is not finite.
 template <int D>
-__device__ __forceinline__ void pa_clean_v(unsigned char* tile, int pos0, int n, int t, int* first) {
+__device__ __forceinline__ void pa_clean_v(unsigned char* tile, int pos0, int n, int* first, volatile int* marked) {
+    const int lane = threadIdx.x & 31;
+    constexpr int kBatch = 8;                                 // pieces of 16 bytes in flight
+    const __nv_bfloat162 zero = __floats2bfloat162_rn(0.f, 0.f);
+    __nv_bfloat162 strange = zero;
+    auto look = [&](uint32_t w) { strange = __hfma2(*reinterpret_cast<const __nv_bfloat162*>(&w), zero, strange); };
 #pragma unroll 1
-    for (int i = t; i < kPaKeys * D / 8; i += 128) {          // 16-byte pieces
-        const int tok = (i >> 3) & (kPaKeys - 1), chunk = i >> 10, c = i & 7;
-        uint4* at = reinterpret_cast<uint4*>(tile + chunk * PaLayout<D>::kChunk + tok * 128 + ((c ^ (tok & 7)) << 4));
-        if (pos0 + tok >= n) {
-            *at = make_uint4(0u, 0u, 0u, 0u);
-            continue;
-        }
-        const uint4 v = *at;
-        // halves that are all ones in the exponent
-        const uint32_t bx = __vcmpeq2(v.x & 0x7f807f80u, 0x7f807f80u), by = __vcmpeq2(v.y & 0x7f807f80u, 0x7f807f80u);
-        const uint32_t bz = __vcmpeq2(v.z & 0x7f807f80u, 0x7f807f80u), bw = __vcmpeq2(v.w & 0x7f807f80u, 0x7f807f80u);
-        if (bx | by | bz | bw) {
-            *at = make_uint4(v.x & ~bx, v.y & ~by, v.z & ~bz, v.w & ~bw);
-            const int e0 = chunk * 64 + c * 8;
-#pragma unroll 1
-            for (int e = 0; e < 8; ++e) {
-                const uint32_t w = e < 2 ? bx : e < 4 ? by : e < 6 ? bz : bw;
-                if ((w >> (16 * (e & 1))) & 1u) atomicMin(first + e0 + e, pos0 + tok);
+    for (int i0 = lane; i0 < kPaKeys * D / 8; i0 += 32 * kBatch) {
+        uint4 v[kBatch];
+#pragma unroll
+        for (int z = 0; z < kBatch; ++z) {
+            uint4* at = reinterpret_cast<uint4*>(tile + (i0 + 32 * z) * 16);
+            if (pos0 + (((i0 + 32 * z) >> 3) & (kPaKeys - 1)) < n) {
+                v[z] = *at;
+            } else {
+                v[z] = make_uint4(0u, 0u, 0u, 0u);
+                *at = v[z];
             }
         }
+#pragma unroll
+        for (int z = 0; z < kBatch; ++z) { look(v[z].x); look(v[z].y); look(v[z].z); look(v[z].w); }
+    }
+    if (!__any_sync(0xffffffffu, !(__low2float(strange) == 0.f && __high2float(strange) == 0.f))) return;
+    *marked = 1;
+#pragma unroll 1
+    for (int i = lane; i < kPaKeys * D / 8; i += 32) {
+        const int tok = (i >> 3) & (kPaKeys - 1), e0 = (i >> 10) * 64 + ((i & 7) ^ (tok & 7)) * 8;   // the copy's swizzle
+        uint16_t* at = reinterpret_cast<uint16_t*>(tile + i * 16);
+#pragma unroll 1
+        for (int e = 0; e < 8; ++e)
+            if ((at[e] & 0x7f80u) == 0x7f80u) {
+                at[e] = 0;
+                atomicMin(first + e0 + e, pos0 + tok);
+            }
     }
 }
+// Whether some row of the tile of rows that begins at token i0 does not see all of tile j of the keys.
+__device__ __forceinline__ bool pa_masked(int i0, int j) { return (j + 1) * kPaKeys > i0 + 1; }
+__device__ __forceinline__ int pa_first_masked(int i0) { return (i0 + 1) / kPaKeys; }
 
-// Items in the order of their numbers: sequence by sequence, the last rows first, the key heads of the same rows together.
+// Items in the order of their numbers: 32 sequences at a time, and of these the items with the most keys first, whichever sequence
+// they are of, so that none of the long ones begins last (sequence after sequence: 4 prompts of 1000 to 4095, 157 us for PLACE); the key
+// heads of the same rows together.
 struct PaWalk {
     int b0;                                    // 32 sequences, one a lane
-    long long before, tokens;                  // items and tokens of the sequences before them
-    int row0, n;                               // this lane's
-    long long upto;                            // items up to this lane's sequence, itself included
+    long long before, tokens, items;           // items and tokens of the sequences before them; their own items
+    int row0, n, pairs;                        // this lane's
 };
 __device__ __forceinline__ void pa_walk_load(const PromptAttnParams& p, PaWalk& w) {
     const int lane = threadIdx.x & 31, b = w.b0 + lane;
@@ -213,39 +240,41 @@ __device__ __forceinline__ void pa_walk_load(const PromptAttnParams& p, PaWalk& 
     if (!ok && p.status) atomicOr(p.status + b, BS_DEV_BAD_LENGTH);
     w.row0 = c0;
     w.n = ok ? n : 0;
-    long long items = (long long)((w.n + 2 * p.TQ - 1) / (2 * p.TQ)) * p.Hkv;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const long long up = __shfl_up_sync(0xffffffffu, items, o);
-        if (lane >= o) items += up;
-    }
-    w.upto = w.before + items;
+    w.pairs = (w.n + 2 * p.TQ - 1) / (2 * p.TQ);
     w.tokens += __shfl_sync(0xffffffffu, sum, 31);
+    w.items = (long long)__reduce_add_sync(0xffffffffu, (unsigned)w.pairs) * p.Hkv;
 }
 __device__ __forceinline__ bool pa_walk_to(const PromptAttnParams& p, PaWalk& w, long long item, PaItem& it) {
     if (item < w.before) {
         w.b0 = 0; w.before = 0; w.tokens = 0;
         pa_walk_load(p, w);
     }
-    for (;;) {
-        const unsigned in = __ballot_sync(0xffffffffu, w.upto > item);
-        if (in) {
-            const int l = __ffs(in) - 1;
-            const long long last = __shfl_sync(0xffffffffu, w.upto, l);
-            const int left = (int)(last - 1 - item);          // items of the sequence behind this one
-            it.h = p.Hkv - 1 - left % p.Hkv;
-            it.i0 = (left / p.Hkv) * 2 * p.TQ;
-            it.row0 = __shfl_sync(0xffffffffu, w.row0, l);
-            it.n = __shfl_sync(0xffffffffu, w.n, l);
-            it.nt0 = (min(it.n, it.i0 + p.TQ) + kPaKeys - 1) / kPaKeys;
-            it.nt1 = it.i0 + p.TQ < it.n ? (min(it.n, it.i0 + 2 * p.TQ) + kPaKeys - 1) / kPaKeys : 0;
-            return true;
-        }
+    while (item >= w.before + w.items) {
         if (w.b0 + 32 >= p.B) return false;
-        w.before = __shfl_sync(0xffffffffu, w.upto, 31);
+        w.before += w.items;
         w.b0 += 32;
         pa_walk_load(p, w);
     }
+    // pairs from the `level`-th on come first: the largest level at which there are enough of them
+    const long long t = item - w.before;
+    auto from = [&](int level) { return (long long)__reduce_add_sync(0xffffffffu, (unsigned)max(0, w.pairs - level)) * p.Hkv; };
+    int lo = 0, hi = (int)__reduce_max_sync(0xffffffffu, (unsigned)w.pairs);   // from(lo) > t >= from(hi)
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (from(mid) > t) lo = mid;
+        else hi = mid;
+    }
+    const int rank = (int)(t - from(hi));                     // among the items of this level
+    uint32_t who = __ballot_sync(0xffffffffu, w.pairs > lo);
+    for (int skip = rank / p.Hkv; skip > 0; --skip) who &= who - 1;
+    const int l = __ffs(who) - 1;
+    it.h = rank % p.Hkv;
+    it.i0 = lo * 2 * p.TQ;
+    it.row0 = __shfl_sync(0xffffffffu, w.row0, l);
+    it.n = __shfl_sync(0xffffffffu, w.n, l);
+    it.nt0 = (min(it.n, it.i0 + p.TQ) + kPaKeys - 1) / kPaKeys;
+    it.nt1 = it.i0 + p.TQ < it.n ? (min(it.n, it.i0 + 2 * p.TQ) + kPaKeys - 1) / kPaKeys : 0;
+    return true;
 }
 
 template <int D>
@@ -257,37 +286,41 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
     extern __shared__ unsigned char pa_smem_raw[];
     unsigned char* s_q = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(pa_smem_raw) + 1023) & ~(uintptr_t)1023);
     unsigned char* s_kv = s_q + 2 * L::kTileBytes;            // K and V of a tile of keys follow one another in the ring
-    __shared__ __align__(8) unsigned long long b_full[RING], b_empty[RING], b_qfull[2], b_qempty[2], b_s[2], b_p[2][2], b_o[2],
+    unsigned char* s_out = s_kv + RING * L::kTileBytes;
+    __shared__ __align__(8) unsigned long long b_full[RING], b_empty[RING], b_part[RING / 2], b_qfull[2], b_qempty[2], b_s[2], b_sfree[2], b_p[2][2], b_o[2],
         b_item[kPaItems], b_done[kPaItems], b_next, b_drain;
     __shared__ PaItem s_item[kPaItems];
     __shared__ int s_first[kPaItems][D];                      // see pa_clean_v
+    __shared__ volatile int s_marked[kPaItems];               // some element of it is
     __shared__ __align__(16) uint4 s_next;                    // answer of the launch control
     __shared__ uint32_t s_tmem;
     __shared__ volatile int s_abort;
-    __shared__ uint32_t s_copies, s_qcopies[2];               // tiles whose copies were issued
+    __shared__ uint32_t s_copies, s_parts, s_last, s_qcopies[2];   // copies issued; of the last 32, those by way of warp 11
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     if (tid == 0) {
         for (uint32_t s = 0; s < RING; ++s) {
             mbar_init(smem_u32(&b_full[s]), 1);
             mbar_init(smem_u32(&b_empty[s]), 1);
+            if (s < RING / 2) mbar_init(smem_u32(&b_part[s]), 1);
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(smem_u32(&b_qfull[i]), 1);
             mbar_init(smem_u32(&b_qempty[i]), 1);
             mbar_init(smem_u32(&b_s[i]), 1);
+            mbar_init(smem_u32(&b_sfree[i]), 4);
             mbar_init(smem_u32(&b_p[i][0]), 4);               // the first half of the keys, the second
             mbar_init(smem_u32(&b_p[i][1]), 4);
             mbar_init(smem_u32(&b_o[i]), 1);
         }
         for (int s = 0; s < kPaItems; ++s) {
             mbar_init(smem_u32(&b_item[s]), 1);
-            mbar_init(smem_u32(&b_done[s]), 10);              // copies, MMAs, eight softmax warps
+            mbar_init(smem_u32(&b_done[s]), 11);              // copies, MMAs, V, eight softmax warps
         }
         mbar_init(smem_u32(&b_next), 1);
         mbar_init(smem_u32(&b_drain), 1);
         s_abort = 0;
-        s_copies = s_qcopies[0] = s_qcopies[1] = 0u;
+        s_copies = s_parts = s_last = s_qcopies[0] = s_qcopies[1] = 0u;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 8) tc_alloc(smem_u32(&s_tmem), L::kTmemCols);
@@ -303,13 +336,13 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
 
     // Registers: 208 for the softmax warps, 80 for the others; 256 * 208 + 128 * 80 of the 384 * 168 that the launch gives.
     bool ok = true;
-    auto wait = [&](unsigned long long* bar, uint32_t parity) { return pa_wait(smem_u32(bar), parity) && !__any_sync(0xffffffffu, s_abort); };
+    auto wait = [&](const unsigned long long* bar, uint32_t parity) { return pa_wait(bar, parity, &s_abort); };
 
     if (warp == 10) {
         // ================================= scheduler =================================
         pa_few_registers();
         const uint32_t elected = ca_elect();
-        PaWalk w = {0, 0, 0, 0, 0, 0};
+        PaWalk w = {0, 0, 0, 0, 0, 0, 0};
         pa_walk_load(p, w);
         long long item = blockIdx.x;
         bool more = true;
@@ -322,7 +355,7 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
                 "setp.ne.b32 e, %2, 0;\n\t"
                 "@e clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];\n\t}"
                 ::"r"(smem_u32(&s_next)), "r"(smem_u32(&b_next)), "r"(elected) : "memory");
-            ok = pa_wait(smem_u32(&b_next), asked++ & 1);
+            ok = wait(&b_next, asked++ & 1);
             if (!ok) return;
             uint32_t canceled, x;
             asm volatile(
@@ -346,7 +379,10 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
             if (k >= kPaItems) ok = wait(&b_done[slot], (k / kPaItems - 1) & 1);
             if (!ok) break;
             for (int i = lane; i < D; i += 32) s_first[slot][i] = 0x7fffffff;
-            if (lane == 0) s_item[slot] = it;
+            if (lane == 0) {
+                s_item[slot] = it;
+                s_marked[slot] = 0;
+            }
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&b_item[slot]));
             if (!there) break;
@@ -359,12 +395,16 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
         // ================================== copies ==================================
         pa_few_registers();
         const uint32_t elected = ca_elect();
-        uint32_t at = 0, ph = 0, count = 0, uses[2] = {0u, 0u};
+        uint32_t at = 0, ph = 0, count = 0, parts = 0, last = 0, uses[2] = {0u, 0u};
         const uint32_t q_bytes = (uint32_t)(p.TQ * p.G * D * 2);
-        auto tile = [&](const CUtensorMap* tm, const PaItem& it, int j) {
+        // A tile of V that is seen in part goes by way of warp 11, which tells b_full when it has looked through it.  It has done so
+        // long before its barrier is needed again: RING / 2 tiles of V further on, where the tile's place is, too.
+        auto tile = [&](const CUtensorMap* tm, const PaItem& it, int j, bool part) {
             ok = wait(&b_empty[at], ph ^ 1u);
             if (!ok) return;
-            const uint32_t bar = smem_u32(&b_full[at]), dst = smem_u32(s_kv + at * L::kTileBytes);
+            const uint32_t bar = smem_u32(part ? &b_part[parts % (RING / 2)] : &b_full[at]), dst = smem_u32(s_kv + at * L::kTileBytes);
+            parts += part;
+            last = last << 1 | (part ? 1u : 0u);
             if (lane == 0) mbar_arrive_expect_tx(bar, L::kTileBytes);
             __syncwarp();
 #pragma unroll
@@ -382,7 +422,7 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
             if (nt == 0) break;
 #pragma unroll 1
             for (int j = 0; j < nt && ok; ++j) {
-                tile(&tm_k, it, j);
+                tile(&tm_k, it, j, false);
                 if (j == 0)
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
@@ -397,13 +437,15 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
                             pa_tma(dst + c * L::kChunk, &tm_q, c * 64, it.h * p.G, it.row0 + it.i0 + i * p.TQ, bar, elected);
                         ++uses[i];
                     }
-                if (ok) tile(&tm_v, it, j);
+                if (ok) tile(&tm_v, it, j, pa_masked(it.i0, j));
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&b_done[slot]));
         }
         if (lane == 0) {
             s_copies = count;
+            s_parts = parts;
+            s_last = last;
             s_qcopies[0] = uses[0];
             s_qcopies[1] = uses[1];
             if (!ok) s_abort = 1;
@@ -412,12 +454,13 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
         // ================================= MMA issuer =================================
         pa_few_registers();
         // Step g is a tile of keys of an item.  In the order of issue: P V of step g - 1 and Q K^T of step g for row tile 0, then for row
-        // tile 1; MMAs are carried out in this order, so S may overwrite the P that the product before it has read.
+        // tile 1; MMAs are carried out in this order, so S may overwrite the P that the product before it has read.  Where P has
+        // a place of its own, Q K^T goes first, as soon as the scores of step g - 1 are in registers.
         constexpr uint32_t id_s = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kPaKeys >> 3) << 17) | (8u << 24);
         constexpr uint32_t id_o = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)(D >> 3) << 17) | (8u << 24);
         const uint32_t elected = ca_elect();
         uint32_t at = 0, ph = 0;                              // place in the ring: K of step g, or V of step g - 1 behind it
-        uint32_t items = 0, steps[2] = {0u, 0u}, q_uses[2] = {0u, 0u};
+        uint32_t items = 0, steps[2] = {0u, 0u}, q_steps[2] = {0u, 0u}, q_uses[2] = {0u, 0u};
         PaItem cur = {0, 0, 0, 0, 0, 0}, prev = cur;
         int j = 0, jp = 0, nt = 0;                            // step of the current item; that of the step before
         uint32_t prev_slot = 0, v_at = 0, v_ph = 0;
@@ -443,43 +486,55 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
             if (have_q) {
                 if (++at == RING) { at = 0; ph ^= 1u; }
             }
+            // what has arrived long since is waited for before what has not: the probabilities
+            if (have_p) ok = wait(&b_full[v_at], v_ph);
+            if (have_q) ok = ok && wait(&b_full[k_at], k_ph);
+            if (!ok) break;
+            auto pv = [&](int i) {
+                if (!have_p || jp >= (i ? prev.nt1 : prev.nt0)) return;
+                const uint64_t dv = ca_desc(smem_u32(s_kv + v_at * L::kTileBytes), L::kChunk, 1024, 2);
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                if (have_p && jp < (i ? prev.nt1 : prev.nt0)) {
-                    ok = ok && wait(&b_full[v_at], v_ph);
-                    const uint64_t dv = ca_desc(smem_u32(s_kv + v_at * L::kTileBytes), L::kChunk, 1024, 2);
-#pragma unroll
-                    for (int s = 0; s < kPaKeys / 16; ++s) {
-                        if (s % (kPaKeys / 32) == 0) {        // half of P is there
-                            ok = ok && wait(&b_p[i][s / (kPaKeys / 32)], steps[i] & 1);
-                            if (!ok) break;
-                            tc_fence_after();
-                        }
-                        pa_mma_ts(tmem + L::kColO + i * D, tmem + i * 128 + s * 8, dv + ((s * 2048) >> 4), id_o, (jp | s) ? 1u : 0u, elected);
+                for (int s = 0; s < kPaKeys / 16; ++s) {
+                    if (s % (kPaKeys / 32) == 0) {            // half of P is there
+                        ok = ok && wait(&b_p[i][s / (kPaKeys / 32)], steps[i] & 1);
+                        if (!ok) return;
+                        tc_fence_after();
                     }
-                    if (!ok) break;
-                    ++steps[i];
-                    ca_commit(smem_u32(&b_o[i]), elected);
+                    pa_mma_ts(tmem + L::kColO + i * D, tmem + i * L::kColS + L::kColP + s * 8, dv + ((s * 2048) >> 4), id_o, (jp | s) ? 1u : 0u, elected);
                 }
-                if (have_p && i == 1) ca_commit(smem_u32(&b_empty[v_at]), elected);
-                if (have_q && j < (i ? cur.nt1 : cur.nt0)) {
-                    ok = ok && wait(&b_full[k_at], k_ph) && (j > 0 || wait(&b_qfull[i], q_uses[i] & 1));
-                    if (!ok) break;
-                    tc_fence_after();
-                    const uint64_t dq = ca_desc(smem_u32(s_q + i * L::kTileBytes), 16, 1024, 2);
-                    const uint64_t dk = ca_desc(smem_u32(s_kv + k_at * L::kTileBytes), 16, 1024, 2);
+                ++steps[i];
+                ca_commit(smem_u32(&b_o[i]), elected);
+            };
+            auto qk = [&](int i) {
+                if (!ok || !have_q || j >= (i ? cur.nt1 : cur.nt0)) return;
+                if (j == 0) ok = wait(&b_qfull[i], q_uses[i] & 1);
+                if (L::kApart && q_steps[i]) ok = ok && wait(&b_sfree[i], (q_steps[i] - 1) & 1);
+                if (!ok) return;
+                ++q_steps[i];
+                tc_fence_after();
+                const uint64_t dq = ca_desc(smem_u32(s_q + i * L::kTileBytes), 16, 1024, 2);
+                const uint64_t dk = ca_desc(smem_u32(s_kv + k_at * L::kTileBytes), 16, 1024, 2);
 #pragma unroll
-                    for (int s = 0; s < D / 16; ++s) {
-                        const uint32_t off = ((s >> 2) * L::kChunk + (s & 3) * 32) >> 4;
-                        pa_mma_ss(tmem + i * 128, dq + off, dk + off, id_s, s ? 1u : 0u, elected);
-                    }
-                    ca_commit(smem_u32(&b_s[i]), elected);
-                    if (j == (i ? cur.nt1 : cur.nt0) - 1) {
-                        ca_commit(smem_u32(&b_qempty[i]), elected);
-                        ++q_uses[i];
-                    }
+                for (int s = 0; s < D / 16; ++s) {
+                    const uint32_t off = ((s >> 2) * L::kChunk + (s & 3) * 32) >> 4;
+                    pa_mma_ss(tmem + i * L::kColS, dq + off, dk + off, id_s, s ? 1u : 0u, elected);
                 }
-                if (have_q && i == 1) ca_commit(smem_u32(&b_empty[k_at]), elected);
+                ca_commit(smem_u32(&b_s[i]), elected);
+                if (j == (i ? cur.nt1 : cur.nt0) - 1) {
+                    ca_commit(smem_u32(&b_qempty[i]), elected);
+                    ++q_uses[i];
+                }
+            };
+            if (L::kApart) {
+                qk(0); pv(0); qk(1);
+                if (ok && have_q) ca_commit(smem_u32(&b_empty[k_at]), elected);
+                pv(1);
+                if (ok && have_p) ca_commit(smem_u32(&b_empty[v_at]), elected);
+            } else {
+                pv(0); qk(0); pv(1);
+                if (ok && have_p) ca_commit(smem_u32(&b_empty[v_at]), elected);
+                qk(1);
+                if (ok && have_q) ca_commit(smem_u32(&b_empty[k_at]), elected);
             }
             if (!ok) break;
             if (have_p && jp == max(prev.nt0, prev.nt1) - 1 && lane == 0) mbar_arrive(smem_u32(&b_done[prev_slot]));
@@ -494,7 +549,8 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
         }
         // every product is through before this CTA's memory goes
         ca_commit(smem_u32(&b_drain), elected);
-        if (!pa_wait(smem_u32(&b_drain), 0)) ok = false;
+        const int zero = 0;                                   // whoever gave up: this one is waited for
+        if (!pa_wait(&b_drain, 0, &zero)) ok = false;
         if (!ok && lane == 0) s_abort = 1;
         __syncwarp();
     } else if (warp < 8) {
@@ -502,7 +558,8 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
         asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
         const int i = warp >> 2;                              // row tile
         const int row = (warp & 3) * 32 + lane;
-        const uint32_t t_s = tmem + ((uint32_t)((warp & 3) * 32) << 16) + i * 128, t_o = t_s - i * 128 + L::kColO + i * D;
+        const uint32_t t_lane = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+        const uint32_t t_s = t_lane + i * L::kColS, t_p = t_s + L::kColP, t_o = t_lane + L::kColO + i * D;
         const int tok = row / p.G, head = row - tok * p.G;
         uint32_t steps = 0;                                   // tiles of keys so far, over all items
         uint32_t ring = 0;                                    // K and V tiles of the items so far
@@ -519,43 +576,52 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
 #pragma unroll 1
             for (int j = 0; j < nt; ++j, ++steps) {
                 const int pos0 = j * kPaKeys;
-                const bool masked = pos0 + kPaKeys > i0 + 1;
-                if (masked && (i == 0 || j >= it.nt0)) {    // row tile 1 goes after row tile 0
-                    const uint32_t r = ring + 2 * j + 1;
-                    ok = wait(&b_full[r % RING], (r / RING) & 1);
-                    if (!ok) break;
-                    pa_clean_v<D>(s_kv + (r % RING) * L::kTileBytes, pos0, it.n, row, s_first[slot]);
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                }
+                const bool masked = pa_masked(i0, j);
                 ok = wait(&b_s[i], steps & 1);
                 if (!ok) break;
                 tc_fence_after();
-                float s[128];
+                // the scores, 64 at a time: the largest of the first are found while the others are on their way
+                float s[128], top[2];
+                pa_ld32(t_s, s);
+                pa_ld32(t_s + 32, s + 32);
+                const int sees = pos - pos0;                  // columns up to this one
+                const int all = i0 + (warp & 3) * 32 / p.G - pos0;   // columns that the warp's first row sees, and so every one
 #pragma unroll
-                for (int c = 0; c < 128; c += 32) pa_ld32(t_s + c, s + c);
+                for (int c0 = 0; c0 < 128; c0 += 64) {
+                    pa_ld32_wait(s + c0);
+                    pa_ld32_wait(s + c0 + 32);
+                    if (c0 == 0) {
+                        pa_ld32(t_s + 64, s + 64);
+                        pa_ld32(t_s + 96, s + 96);
+                    } else if (L::kApart) {                   // S may be written again
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(smem_u32(&b_sfree[i]));
+                    }
+                    if (masked)
 #pragma unroll
-                for (int c = 0; c < 128; c += 32) pa_ld32_wait(s + c);
-                if (masked) {
-                    const int sees = pos - pos0;              // columns up to this one
+                        for (int c = c0; c < c0 + 64; c += 16)
+                            if (c + 15 > all)
 #pragma unroll
-                    for (int c = 0; c < 128; ++c)
-                        if (c > sees) s[c] = -INFINITY;
+                                for (int e = c; e < c + 16; ++e)
+                                    if (e > sees) s[e] = -INFINITY;
+                    float a[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) a[e] = pa_max3(s[c0 + e], s[c0 + e + 4], s[c0 + e + 8]);
+#pragma unroll
+                    for (int c = c0 + 12; c < c0 + 60; c += 8)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) a[e] = pa_max3(a[e], s[c + e], s[c + e + 4]);
+                    top[c0 / 64] = pa_max3(pa_max3(a[0], a[1], a[2]), pa_max3(a[3], s[c0 + 60], s[c0 + 61]), pa_max3(s[c0 + 62], s[c0 + 63], s[c0 + 63]));
                 }
-                float a[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) a[e] = pa_max3(s[e], s[e + 4], s[e + 8]);
-#pragma unroll
-                for (int c = 12; c < 124; c += 8)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) a[e] = pa_max3(a[e], s[c + e], s[c + e + 4]);
-                float mx = pa_max3(pa_max3(a[0], a[1], a[2]), pa_max3(a[3], s[124], s[125]), pa_max3(s[126], s[127], s[127])) * p.c;
+                float mx = pa_max3(top[0], top[1], top[1]) * p.c;
                 if (!(mx < INFINITY)) mx = __int_as_float(0x7fc00000);   // a row that sees a NaN or an infinite score: all NaN
                 const bool moves = valid && !(mx <= m + kPaSlack);
                 if (j == 0) {
                     m = mx;
                 } else if (__any_sync(0xffffffffu, moves)) {
                     // the products so far
-                    ok = pa_wait(smem_u32(&b_o[i]), (steps - 1) & 1);
+                    ok = wait(&b_o[i], (steps - 1) & 1);
                     if (!ok) break;
                     tc_fence_after();
                     // a row's own scores alone decide when its reference moves: its result does not depend on the others
@@ -572,6 +638,11 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
                         ca_st16(t_o + c, o);
                     }
                     ca_st_wait();
+                }
+                if (L::kApart && j > 0) {                     // the product before has read its P
+                    ok = wait(&b_o[i], (steps - 1) & 1);
+                    if (!ok) break;
+                    tc_fence_after();
                 }
                 const float nm = m == -INFINITY ? 0.f : -m;
                 const uint64_t c2 = pa_pk(p.c, p.c), nm2 = pa_pk(nm, nm);
@@ -595,7 +666,12 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
                         sum[e & 1] = pa_add2(sum[e & 1], x2);
                         w[e] = pa_bf16x2(x, y);
                     }
-                    pa_st16(t_s + (c >> 1), w);
+                    pa_st16(t_p + (c >> 1), w);
+                    if (c == 96 && masked) {                  // what was marked in V is seen behind this
+                        const uint32_t r = ring + 2 * j + 1;
+                        ok = wait(&b_full[r % RING], (r / RING) & 1);
+                        if (!ok) break;
+                    }
                     if (c & 32) {                             // half of P: the product may begin
                         ca_st_wait();
                         tc_fence_before();
@@ -606,6 +682,7 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
                 float s0, s1;
                 pa_upk(pa_add2(sum[0], sum[1]), s0, s1);
                 l += s0 + s1;
+                if (!ok) break;
             }
             if (!ok) break;
             if (nt > 0) {
@@ -613,27 +690,39 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
                 if (!ok) break;
                 tc_fence_after();
                 const float inv = 1.f / l;
-                __nv_bfloat16* o = p.out + (long long)(it.row0 + pos) * p.o_st + (long long)(it.h * p.G + head) * p.o_sh;
+                // Results leave through shared memory, so that eight lanes store the 128 bytes of a row side by side: a lane storing
+                // its own row touches 32 lines per instruction, 2000 cycles a tile.
+                __nv_bfloat16* mine = valid ? p.out + (long long)(it.row0 + pos) * p.o_st + (long long)(it.h * p.G + head) * p.o_sh : nullptr;
+                unsigned char* stage = s_out + warp * L::kOut;
                 const int* first = s_first[slot];
+                const bool marked = s_marked[slot] != 0;
 #pragma unroll 1
-                for (int c = 0; c < D; c += 32) {
-                    float y[32];
-                    pa_ld32(t_o + c, y);
-                    pa_ld32_wait(y);
-                    if (valid) {
+                for (int c0 = 0; c0 < D; c0 += 64) {
+#pragma unroll 1
+                    for (int c = c0; c < c0 + 64; c += 32) {
+                        float y[32];
+                        pa_ld32(t_o + c, y);
+                        pa_ld32_wait(y);
 #pragma unroll
-                        for (int e = 0; e < 32; e += 8) {
-                            uint32_t w[4];
+                        for (int e = 0; e < 32; ++e) y[e] *= inv;
+                        if (marked)
 #pragma unroll
-                            for (int z = 0; z < 4; ++z) {
-                                float u = y[e + 2 * z] * inv, v = y[e + 2 * z + 1] * inv;
-                                if (first[c + e + 2 * z] <= pos) u = __int_as_float(0x7fc00000);
-                                if (first[c + e + 2 * z + 1] <= pos) v = __int_as_float(0x7fc00000);
-                                w[z] = pa_bf16x2(u, v);
-                            }
-                            *reinterpret_cast<uint4*>(o + c + e) = make_uint4(w[0], w[1], w[2], w[3]);
-                        }
+                            for (int e = 0; e < 32; ++e)
+                                if (first[c + e] <= pos) y[e] = __int_as_float(0x7fc00000);
+#pragma unroll
+                        for (int e = 0; e < 32; e += 8)
+                            *reinterpret_cast<uint4*>(stage + lane * 128 + ((((c - c0 + e) >> 3) ^ (lane & 7)) << 4)) =
+                                make_uint4(pa_bf16x2(y[e], y[e + 1]), pa_bf16x2(y[e + 2], y[e + 3]), pa_bf16x2(y[e + 4], y[e + 5]), pa_bf16x2(y[e + 6], y[e + 7]));
                     }
+                    __syncwarp();
+#pragma unroll
+                    for (int r0 = 0; r0 < 32; r0 += 4) {
+                        const int r = r0 + (lane >> 3), piece = lane & 7;
+                        __nv_bfloat16* o = reinterpret_cast<__nv_bfloat16*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(mine), r));
+                        const uint4 v = *reinterpret_cast<const uint4*>(stage + r * 128 + ((piece ^ (r & 7)) << 4));
+                        if (o) *reinterpret_cast<uint4*>(o + c0 + piece * 8) = v;
+                    }
+                    __syncwarp();
                 }
                 tc_fence_before();
             }
@@ -643,7 +732,32 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
         }
         if (!ok && lane == 0) s_abort = 1;
     } else {
-        pa_few_registers();                                   // the warps of a group give them back together
+        // ============================ V, seen in part =============================
+        pa_few_registers();
+        uint32_t ring = 0, parts = 0;                         // copies of K and V of the items so far; tiles looked through
+#pragma unroll 1
+        for (uint32_t k = 0; ok; ++k) {
+            const uint32_t slot = k % kPaItems;
+            ok = wait(&b_item[slot], (k / kPaItems) & 1);
+            if (!ok) break;
+            const PaItem it = s_item[slot];
+            const int nt = max(it.nt0, it.nt1);
+            if (nt == 0) break;
+#pragma unroll 1
+            for (int j = pa_first_masked(it.i0); j < nt; ++j, ++parts) {
+                const uint32_t at = (ring + 2 * j + 1) % RING;
+                ok = wait(&b_part[parts % (RING / 2)], (parts / (RING / 2)) & 1);
+                if (!ok) break;
+                pa_clean_v<D>(s_kv + at * L::kTileBytes, j * kPaKeys, it.n, s_first[slot], &s_marked[slot]);
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&b_full[at]));
+            }
+            ring += 2 * nt;
+            __syncwarp();
+            if (ok && lane == 0) mbar_arrive(smem_u32(&b_done[slot]));
+        }
+        if (!ok && lane == 0) s_abort = 1;
     }
 
     // ---- all roles meet; tensor memory goes back ----
@@ -654,10 +768,13 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
         // a wait gave up: nothing is issued any more, and no copy may be in flight when the memory goes (the products have been
         // waited for)
         if (warp == 9) {
-            const uint32_t n = s_copies;
-            for (uint32_t f = n > RING ? n - RING : 0u; f < n; ++f) pa_wait(smem_u32(&b_full[f % RING]), (f / RING) & 1);
+            const uint32_t n = s_copies, m = s_parts;
+            const int zero = 0;
+            for (uint32_t f = n > RING ? n - RING : 0u; f < n; ++f)
+                if (!((s_last >> (n - 1 - f)) & 1u)) pa_wait(&b_full[f % RING], (f / RING) & 1, &zero);
+            for (uint32_t f = m > RING / 2 ? m - RING / 2 : 0u; f < m; ++f) pa_wait(&b_part[f % (RING / 2)], (f / (RING / 2)) & 1, &zero);
             for (int i = 0; i < 2; ++i)
-                if (s_qcopies[i]) pa_wait(smem_u32(&b_qfull[i]), (s_qcopies[i] - 1) & 1);
+                if (s_qcopies[i]) pa_wait(&b_qfull[i], (s_qcopies[i] - 1) & 1, &zero);
         }
         if (tid == 0 && p.status) atomicOr(p.status, BS_DEV_TIMEOUT);
         __syncthreads();

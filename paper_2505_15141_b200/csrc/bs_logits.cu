@@ -4,11 +4,14 @@
 //   x = logit;  seen (in the prompt, emitted, or drafted on the way to this row): x = x > 0 ? x / r : x r
 //   x -= f c + p [c > 0],  c = times emitted or drafted on the way;   x += bias;   forbidden by the row's grammar mask: -inf
 //
-// adjust: bound by HBM; the rows are read and written once, the history once for all rows of a sequence.  A warp takes 256
-// tokens of the vocabulary of one sequence, eight a lane, and passes over the rows of that sequence; what the history and the biases
-// do to an element is worked out once for all rows.  Biases are added in the order of the list, so that sums do not
-// depend on timing.  In place, lanes with nothing to change touch nothing, and tokens that are all forbidden are written
-// without being read.
+// adjust: bound by HBM, the rows are read and written once, the history once for all rows of a sequence.  A warp takes 256 tokens of
+// the vocabulary of one sequence, eight a lane.  Few of them change by more than the mask (700 tokens of a history in 152064 are one in
+// a warp), so the rows are copied as they are, masked in the type's own bits, and the elements that change are mended behind it,
+// each in each row by a lane.  With the arithmetic in the rows for all elements the kernel was bound by instructions (73 us instead of
+// 60 for 64 sequences of 3 to 9 bf16 rows of 152064: 0.25 GB, 4.2 TB/s; rows with masks alone 6.0).  Where many change
+// (frequent tokens, long histories on small vocabularies) the rows are worked on whole.  Two rows of bf16 in flight and 40 warps an SM
+// were faster than four rows and 32.  Biases are added in the order of the list, so that sums do not depend on timing.
+// In place, only what is forbidden and those elements are written, nothing else is read.
 //
 // history: entries of 16 bits, 2 x (times emitted, up to 16383) + (in the prompt).  A history that begins anew is built in
 // shared memory piece by piece and written once; what a round adds goes to its few entries by compare-and-swap.  Only whole
@@ -45,10 +48,10 @@ struct AdjustParams {
     int extra, row_begin, row_end, B, R, N, V, n_masks, n_bias, in_place;
 };
 
-constexpr int kAdWarps = 8;
+constexpr int kAdWarps = 4;
 constexpr int kAdLane = 8;                     // tokens of a lane
 constexpr int kAdWarp = 32 * kAdLane;          // of a warp
-constexpr int kAdTokens = kAdWarps * kAdWarp;  // of a CTA
+constexpr int kAdFew = 32;                     // elements of a warp that are mended one by one: up to about 40 it is less work than in the rows
 
 // Eight elements of a lane.  VEC: neighbours, two or one 16-byte accesses of all of them; else 32 apart, one by one, for rows that
 // begin anywhere.  `need`: a bit for each element.
@@ -59,7 +62,7 @@ template <typename T> struct AdIo<T, true> {
         if (!need) return;
 #pragma unroll
         for (int i = 0; i < kWords; i += 4) {
-            const uint4 v = *reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(p) + 4 * i);
+            const uint4 v = __ldcg(reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(p) + 4 * i));
             w[i] = v.x; w[i + 1] = v.y; w[i + 2] = v.z; w[i + 3] = v.w;
         }
     }
@@ -67,7 +70,7 @@ template <typename T> struct AdIo<T, true> {
         if (!need) return;
 #pragma unroll
         for (int i = 0; i < kWords; i += 4)
-            *reinterpret_cast<uint4*>(reinterpret_cast<char*>(p) + 4 * i) = make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]);
+            __stcg(reinterpret_cast<uint4*>(reinterpret_cast<char*>(p) + 4 * i), make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]));
     }
 };
 template <> struct AdIo<float, false> {
@@ -120,6 +123,11 @@ __device__ __forceinline__ void ad_pack(const float (&f)[8], uint32_t (&w)[4]) {
         w[e] = *reinterpret_cast<const uint32_t*>(&b);
     }
 }
+// One element; in place it may just have been written by another lane.
+__device__ __forceinline__ float ad_one(const float* p) { return __ldcg(p); }
+__device__ __forceinline__ float ad_one(const __nv_bfloat16* p) {
+    return __uint_as_float((uint32_t)__ldcg(reinterpret_cast<const unsigned short*>(p)) << 16);
+}
 // What is not allowed becomes -inf, in the type's own bits.
 __device__ __forceinline__ void ad_forbid(uint32_t allowed, uint32_t (&w)[8]) {
 #pragma unroll
@@ -134,51 +142,49 @@ __device__ __forceinline__ void ad_forbid(uint32_t allowed, uint32_t (&w)[4]) {
     }
 }
 
-// The biases of a CTA's tokens, summed in the order of the list: 256 entries at a time, those that fall into the CTA's range added
-// warp after warp and lane after lane.  True if there were any in this warp's range.
-__device__ __forceinline__ bool ad_biases(const AdjustParams& p, int b, int v0, int& bits, float* s_bias, uint32_t* s_warps, uint32_t* s_ranges) {
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int lo = __ldg(p.bias_begin + b), hi = __ldg(p.bias_begin + b + 1);
-    if (lo < 0 || hi > p.n_bias || lo > hi) bits |= BS_DEV_BAD_LENGTH;
-    if (lo < 0 || hi > p.n_bias || lo >= hi) return false;    // the same for the whole CTA
-    for (int i = tid; i < kAdTokens; i += kAdWarps * 32) s_bias[i] = 0.f;
-    if (tid == 0) *s_ranges = 0u;
+// The biases of this warp's 256 tokens, summed into s_sum in the order of the list; true if there are any.  Every warp looks
+// through the list by itself, 128 entries at a time.
+__device__ __forceinline__ bool ad_biases(const AdjustParams& p, int lo, int hi, int v0, int& bits, float* s_sum) {
+    const int lane = threadIdx.x & 31;
+    bool found = false;
 #pragma unroll 1
-    for (int i = lo; i < hi; i += kAdWarps * 32) {
-        if (tid == 0) *s_warps = 0u;
-        const int t = i + tid < hi ? __ldg(p.bias_tokens + i + tid) : 0;
-        const float v = i + tid < hi ? __ldg(p.bias_values + i + tid) : 0.f;
-        const bool good = t >= 0 && t < p.V;
-        if (!good) bits |= BS_DEV_BAD_TOKEN;
-        const bool hit = i + tid < hi && good && t >= v0 && t < v0 + kAdTokens;
-        const uint32_t who = __ballot_sync(0xffffffffu, hit);
-        __syncthreads();                                      // cleared, and the batch before is through
-        if (hit) atomicOr(s_ranges, 1u << ((t - v0) / kAdWarp));
-        if (who && lane == 0) atomicOr(s_warps, 1u << warp);
-        __syncthreads();
-        uint32_t turn = *s_warps;
-        while (turn) {
-            const int w = __ffs(turn) - 1;
-            turn &= turn - 1;
-            if (warp == w)
-                for (uint32_t m = who; m; m &= m - 1) {
-                    if (lane == __ffs(m) - 1) s_bias[t - v0] += v;
-                    __syncwarp();
-                }
-            __syncthreads();
+    for (int i = lo + lane; i - lane < hi; i += 128) {
+        int t[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) t[k] = i + 32 * k < hi ? __ldg(p.bias_tokens + i + 32 * k) : p.V;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (i + 32 * k < hi && (t[k] < 0 || t[k] >= p.V)) bits |= BS_DEV_BAD_TOKEN;
+            const int off = t[k] - v0;
+            const bool hit = off >= 0 && off < kAdWarp && t[k] < p.V;
+            if (!__any_sync(0xffffffffu, hit)) continue;
+            if (!found) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) s_sum[32 * e + lane] = 0.f;
+                found = true;
+            }
+            const float v = hit ? __ldg(p.bias_values + i + 32 * k) : 0.f;
+            // entries of the same token one after the other, the others at once
+            const uint32_t same = __match_any_sync(0xffffffffu, hit ? off : -1);
+            int turn = __popc(same & ((1u << lane) - 1u));
+            const int turns = __reduce_max_sync(0xffffffffu, hit ? turn + 1 : 0);
+            for (int z = 0; z < turns; ++z) {
+                __syncwarp();
+                if (hit && turn == z) s_sum[off] += v;
+            }
         }
     }
-    return (*s_ranges >> warp) & 1u;
+    __syncwarp();
+    return found;
 }
 
 template <typename T, bool VEC>
-__global__ void __launch_bounds__(kAdWarps * 32, 4) logits_adjust_kernel(const AdjustParams p) {
+__global__ void __launch_bounds__(kAdWarps * 32, VEC ? 10 : 8) logits_adjust_kernel(const AdjustParams p) {
     using Io = AdIo<T, VEC>;
-    constexpr int kRows = 8 / sizeof(T);                      // in flight: 64 bytes a lane
-    __shared__ float s_bias[kAdTokens];
-    __shared__ uint32_t s_warps, s_ranges;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, b = blockIdx.y;
-    const int cta_v0 = blockIdx.x * kAdTokens, v0 = cta_v0 + warp * kAdWarp;
+    __shared__ float s_sum[kAdWarps][kAdWarp];                // biases
+    __shared__ float2 s_list[kAdWarps][kAdFew];               // elements that change
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, b = blockIdx.x;
+    const int v0 = ((int)blockIdx.y * kAdWarps + warp) * kAdWarp;
     pdl_enter();
     const int first = VEC ? v0 + lane * kAdLane : v0 + lane;  // token of element 0
     // elements of this lane that are there (VEC: V is a multiple of 8)
@@ -202,8 +208,23 @@ __global__ void __launch_bounds__(kAdWarps * 32, 4) logits_adjust_kernel(const A
         if (g < 0 || g + p.extra > p.R) { g = 0; bits |= BS_DEV_BAD_GAMMA; }
         rows = min(rows, g + p.extra);
     }
-    if (rows <= p.row_begin && !(p.status && blockIdx.x == 0)) return;   // the whole CTA
-    const bool biased = p.bias_begin && ad_biases(p, b, cta_v0, bits, s_bias, &s_warps, &s_ranges);
+    if (rows <= p.row_begin && !(p.status && blockIdx.y == 0)) return;   // the whole CTA
+    float add[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) add[e] = 0.f;
+    uint32_t any = 0u;
+    if (p.bias_begin) {
+        const int lo = __ldg(p.bias_begin + b), hi = __ldg(p.bias_begin + b + 1);
+        if (lo < 0 || hi > p.n_bias || lo > hi) {
+            bits |= BS_DEV_BAD_LENGTH;
+        } else if (ad_biases(p, lo, hi, v0, bits, s_sum[warp])) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                add[e] = s_sum[warp][VEC ? lane * 8 + e : 32 * e + lane];
+                if (add[e] != 0.f) any |= 1u << e;
+            }
+        }
+    }
     if (mask < -1 || mask >= p.n_masks) {
         mask = -1;
         if (lane >= p.row_begin && lane < rows) bits |= BS_DEV_BAD_MASK;
@@ -227,14 +248,11 @@ __global__ void __launch_bounds__(kAdWarps * 32, 4) logits_adjust_kernel(const A
         }
         if (lane < p.N && (tok < 0 || tok >= p.V) && lane < rows - 1) bits |= BS_DEV_BAD_TOKEN;
     }
-    if (p.status && blockIdx.x == 0 && bits) atomicOr(p.status + b, bits);
+    if (p.status && blockIdx.y == 0 && bits) atomicOr(p.status + b, bits);
     const uint32_t drafted = __ballot_sync(0xffffffffu, behind && tok >= v0 && tok < min(v0 + kAdWarp, p.V));
 
     // what the history and the biases do to every element
-    float add[8];
-    uint32_t seen = 0u, counted = 0u, any = 0u;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) add[e] = 0.f;
+    uint32_t seen = 0u, counted = 0u;
     if (h[0] | h[1] | h[2] | h[3]) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
@@ -242,23 +260,13 @@ __global__ void __launch_bounds__(kAdWarps * 32, 4) logits_adjust_kernel(const A
             if (v) seen |= 1u << e;
             if (v >> 1) {
                 counted |= 1u << e;
-                add[e] = -fmaf(freq, (float)(v >> 1), pres);
+                add[e] -= fmaf(freq, (float)(v >> 1), pres);
             }
         }
     }
-    any = seen;
-    if (biased) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float v = s_bias[warp * kAdWarp + (VEC ? lane * 8 + e : 32 * e + lane)];
-            add[e] += v;
-            if (v != 0.f) any |= 1u << e;
-        }
-    }
+    any |= seen;
     any &= there;
-    const bool special = drafted || __any_sync(0xffffffffu, any);
     const float inv = 1.f / rep;
-
     const T* x = reinterpret_cast<const T*>(p.x) + (size_t)b * p.R * p.V + first;
     T* y = reinterpret_cast<T*>(p.y) + (size_t)b * p.R * p.V + first;
     const size_t mask_words = (size_t)((p.V + 31) >> 5);
@@ -274,66 +282,173 @@ __global__ void __launch_bounds__(kAdWarps * 32, 4) logits_adjust_kernel(const A
             if ((VEC ? t >> 3 : t & 31) == lane && ((rr >> (row & 31)) & 1u)) found(VEC ? t & 7 : t >> 5);
         }
     };
+
+    // ---- few elements of this warp change by more than the mask, the usual case: rows are copied, those elements mended behind it ----
+    uint32_t mine = any;                                      // drafted tokens among them, whatever the row
+    for (uint32_t d = drafted; d; d &= d - 1) {
+        const int t = __shfl_sync(0xffffffffu, tok, __ffs(d) - 1) - v0;
+        if ((VEC ? t >> 3 : t & 31) == lane) mine |= 1u << (VEC ? t & 7 : t >> 5);
+    }
+    const int count = __reduce_add_sync(0xffffffffu, __popc(mine));
+    if (count <= kAdFew) {
+        if (p.in_place) {                                     // only what is forbidden is written, nothing read
+            const uint32_t bit = 1u << lane;
+            T* at = reinterpret_cast<T*>(p.y) + ((size_t)b * p.R + p.row_begin) * p.V + v0 + lane;
+            auto word_of = [&](int r) {                       // lane e < 8: tokens v0 + 32 e ..
+                const int m = __shfl_sync(0xffffffffu, mask, r & 31);
+                return m >= 0 && r < rows && lane < 8 && v0 + 32 * lane < p.V ? __ldg(p.masks + (size_t)m * mask_words + (v0 >> 5) + lane) : ~0u;
+            };
+            uint32_t next = word_of(p.row_begin);
 #pragma unroll 1
-    for (int r0 = p.row_begin; r0 < rows; r0 += kRows) {
-        uint32_t w[kRows][Io::kWords], allowed[kRows], own[kRows];
-#pragma unroll
-        for (int k = 0; k < kRows; ++k) {                   // allowed elements of every row
-            const int m = __shfl_sync(0xffffffffu, mask, (r0 + k) & 31);
-            allowed[k] = there;
-            own[k] = 0u;
-            if (m >= 0 && r0 + k < rows) {
-                const uint32_t* words = p.masks + (size_t)m * mask_words + (v0 >> 5);
-                if (VEC) {
-                    if (there) allowed[k] = __ldg(reinterpret_cast<const unsigned char*>(words) + lane);
-                } else {
-                    const uint32_t word = lane < 8 && v0 + 32 * lane < p.V ? __ldg(words + lane) : 0u;
-                    uint32_t a = 0u;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if ((__shfl_sync(0xffffffffu, word, e) >> lane) & 1u) a |= 1u << e;
-                    allowed[k] = a & there;
-                }
-            }
-        }
-#pragma unroll
-        for (int k = 0; k < kRows; ++k) {
-#pragma unroll
-            for (int i = 0; i < Io::kWords; ++i) w[k][i] = 0u;
-            if (r0 + k >= rows) continue;
-            if (drafted) drafted_on(r0 + k, [&](int e) { own[k] |= 1u << e; });
-            // in place only what changes is needed (VEC: all eight, unless none changes or all are forbidden)
-            uint32_t need = allowed[k];
-            if (p.in_place && (!VEC || allowed[k] == there)) need &= any | own[k];
-            Io::load(x + (size_t)(r0 + k) * p.V, need, w[k]);
-        }
-#pragma unroll
-        for (int k = 0; k < kRows; ++k) {
-            if (r0 + k >= rows) continue;
-            if (special) {
-                float f[8];
-                ad_unpack(w[k], f);
-                const uint32_t penalised = seen | own[k];
+            for (int r = p.row_begin; r < rows; ++r, at += p.V) {
+                const uint32_t word = next;
+                next = word_of(r + 1);
+                if (!__any_sync(0xffffffffu, word != ~0u)) continue;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    if ((penalised >> e) & 1u) f[e] *= f[e] > 0.f ? inv : rep;
-                    f[e] += add[e];
+                    const uint32_t word_e = __shfl_sync(0xffffffffu, word, e);
+                    if (!(word_e & bit) && v0 + lane + 32 * e < p.V) at[32 * e] = static_cast<T>(-INFINITY);
                 }
-                if (drafted) {                                // they count like emitted ones
-                    uint32_t known = counted;
-                    drafted_on(r0 + k, [&](int hit) {
-                        const float less = (known >> hit) & 1u ? freq : freq + pres;
-                        known |= 1u << hit;
-#pragma unroll
-                        for (int e = 0; e < 8; ++e)
-                            if (e == hit) f[e] -= less;
-                    });
-                }
-                ad_pack(f, w[k]);
             }
-            if (allowed[k] != there) ad_forbid(allowed[k], w[k]);
-            Io::store(y + (size_t)(r0 + k) * p.V, p.in_place ? there & (any | own[k] | ~allowed[k]) : there, w[k]);
+        } else {
+            constexpr int kRows = 4 / sizeof(T);              // in flight: 32 bytes a lane
+#pragma unroll 1
+            for (int r0 = p.row_begin; r0 < rows; r0 += kRows) {
+                uint32_t w[kRows][Io::kWords], allowed[kRows];
+#pragma unroll
+                for (int k = 0; k < kRows; ++k) {
+                    const int m = __shfl_sync(0xffffffffu, mask, (r0 + k) & 31);
+                    allowed[k] = there;
+                    if (m >= 0 && r0 + k < rows) {
+                        const uint32_t* words = p.masks + (size_t)m * mask_words + (v0 >> 5);
+                        if (VEC) {
+                            if (there) allowed[k] = __ldg(reinterpret_cast<const unsigned char*>(words) + lane);
+                        } else {
+                            const uint32_t word = lane < 8 && v0 + 32 * lane < p.V ? __ldg(words + lane) : 0u;
+                            uint32_t a = 0u;
+#pragma unroll
+                            for (int e = 0; e < 8; ++e)
+                                if ((__shfl_sync(0xffffffffu, word, e) >> lane) & 1u) a |= 1u << e;
+                            allowed[k] = a & there;
+                        }
+                    }
+                }
+#pragma unroll
+                for (int k = 0; k < kRows; ++k) {
+#pragma unroll
+                    for (int i = 0; i < Io::kWords; ++i) w[k][i] = 0u;
+                    if (r0 + k < rows) Io::load(x + (size_t)(r0 + k) * p.V, allowed[k], w[k]);
+                }
+#pragma unroll
+                for (int k = 0; k < kRows; ++k)
+                    if (r0 + k < rows) {
+                        if (allowed[k] != there) ad_forbid(allowed[k], w[k]);
+                        Io::store(y + (size_t)(r0 + k) * p.V, there, w[k]);
+                    }
+            }
         }
+        if (!count) return;
+        // the elements, one behind the other: place in the warp's tokens, whether seen and counted, summand
+        float2* list = s_list[warp];
+        int at = __popc(mine);
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int up = __shfl_up_sync(0xffffffffu, at, o);
+            if (lane >= o) at += up;
+        }
+        at -= __popc(mine);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if ((mine >> e) & 1u)
+                list[at++] = make_float2(__int_as_float((VEC ? lane * 8 + e : 32 * e + lane) | ((seen >> e) & 1u) << 16 | ((counted >> e) & 1u) << 17), add[e]);
+        __syncwarp();                                         // behind it, too: what the other lanes have stored of the rows
+        const int tasks = count * (rows - p.row_begin);       // an element in a row: a lane each
+        const uint32_t per = 65536u / (uint32_t)count + 1u;   // t / count for t < 1024, count <= 32
+#pragma unroll 1
+        for (int t0 = 0; t0 < tasks; t0 += 32) {
+            const int t = min(t0 + lane, tasks - 1), r = p.row_begin + (int)(((uint32_t)t * per) >> 16), l = t - (r - p.row_begin) * count;
+            const float2 entry = list[l];
+            const int info = __float_as_int(entry.x), off = info & 0xffff;
+            const size_t place = ((size_t)b * p.R + r) * p.V + v0 + off;
+            float f = ad_one(reinterpret_cast<const T*>(p.x) + place);
+            const int m = __shfl_sync(0xffffffffu, mask, r);
+            const uint32_t word = m >= 0 ? __ldg(p.masks + (size_t)m * mask_words + ((v0 + off) >> 5)) : ~0u;
+            bool is_seen = (info >> 16) & 1, is_counted = (info >> 17) & 1;
+            float less = 0.f;
+            for (uint32_t d = drafted; d; d &= d - 1) {       // they count like emitted ones
+                const int j = __ffs(d) - 1;
+                const int at_j = __shfl_sync(0xffffffffu, tok, j) - v0;
+                const uint32_t rr = __shfl_sync(0xffffffffu, behind, j);
+                if (at_j == off && ((rr >> r) & 1u)) {
+                    less += is_counted ? freq : freq + pres;
+                    is_seen = is_counted = true;
+                }
+            }
+            if (is_seen) f *= f > 0.f ? inv : rep;
+            f += entry.y - less;
+            if (!((word >> ((v0 + off) & 31)) & 1u)) f = -INFINITY;
+            if (t0 + lane < tasks) reinterpret_cast<T*>(p.y)[place] = static_cast<T>(f);
+        }
+        return;
+    }
+
+    // ---- many: worked on in the rows, the next one on its way while one is ----
+    struct Row { uint32_t w[Io::kWords], allowed, own; };
+    auto load = [&](int r, Row& row) {
+        row.own = 0u;
+        row.allowed = there;
+#pragma unroll
+        for (int i = 0; i < Io::kWords; ++i) row.w[i] = 0u;
+        const int m = __shfl_sync(0xffffffffu, mask, r & 31);
+        if (r >= rows) return;
+        if (m >= 0) {
+            const uint32_t* words = p.masks + (size_t)m * mask_words + (v0 >> 5);
+            if (VEC) {
+                if (there) row.allowed = __ldg(reinterpret_cast<const unsigned char*>(words) + lane);
+            } else {
+                const uint32_t word = lane < 8 && v0 + 32 * lane < p.V ? __ldg(words + lane) : 0u;
+                uint32_t a = 0u;
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if ((__shfl_sync(0xffffffffu, word, e) >> lane) & 1u) a |= 1u << e;
+                row.allowed = a & there;
+            }
+        }
+        if (drafted) drafted_on(r, [&](int e) { row.own |= 1u << e; });
+        // in place only what changes is needed (VEC: all eight, unless none changes or all are forbidden)
+        uint32_t need = row.allowed;
+        if (p.in_place && (!VEC || row.allowed == there)) need &= any | row.own;
+        Io::load(x + (size_t)r * p.V, need, row.w);
+    };
+    Row next;
+    load(p.row_begin, next);
+#pragma unroll 1
+    for (int r = p.row_begin; r < rows; ++r) {
+        Row row = next;
+        load(r + 1, next);
+        float f[8];
+        ad_unpack(row.w, f);
+        const uint32_t penalised = seen | row.own;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float g = f[e] > 0.f ? inv : rep;
+            f[e] = fmaf(f[e], (penalised >> e) & 1u ? g : 1.f, add[e]);
+        }
+        if (drafted) {                                    // they count like emitted ones
+            uint32_t known = counted;
+            drafted_on(r, [&](int hit) {
+                const float less = (known >> hit) & 1u ? freq : freq + pres;
+                known |= 1u << hit;
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (e == hit) f[e] -= less;
+            });
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (!((row.allowed >> e) & 1u)) f[e] = -INFINITY;
+        ad_pack(f, row.w);
+        Io::store(y + (size_t)r * p.V, p.in_place ? there & (any | row.own | ~row.allowed) : there, row.w);
     }
 }
 
@@ -450,7 +565,8 @@ __global__ void __launch_bounds__(kHiThreads) history_prompts_kernel(const Histo
 
 template <typename T>
 static cudaError_t launch_adjust(const AdjustParams& p, bool vec, cudaStream_t st) {
-    const dim3 grid(div_up(div_up(p.V, kAdWarp), kAdWarps), p.B);
+    // the low tokens of all sequences first: they are the frequent ones, of which there is more to change
+    const dim3 grid(p.B, div_up(div_up(p.V, kAdWarp), kAdWarps));
     return vec ? launch_pdl(logits_adjust_kernel<T, true>, grid, kAdWarps * 32, 0, st, p)
                : launch_pdl(logits_adjust_kernel<T, false>, grid, kAdWarps * 32, 0, st, p);
 }

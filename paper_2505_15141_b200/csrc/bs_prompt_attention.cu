@@ -212,6 +212,10 @@ __device__ __forceinline__ void pa_clean_v(unsigned char* tile, int pos0, int n,
             }
     }
 }
+// Keys of tile j that a row tile beginning at token i0 sees any of, as many as the products take.
+__device__ __forceinline__ int pa_keys(const PromptAttnParams& p, int n, int i0, int j) {
+    return min(kPaKeys, (min(n, i0 + p.TQ) - j * kPaKeys + 15) & ~15);
+}
 // Whether some row of the tile of rows that begins at token i0 does not see all of tile j of the keys.
 __device__ __forceinline__ bool pa_masked(int i0, int j) { return (j + 1) * kPaKeys > i0 + 1; }
 __device__ __forceinline__ int pa_first_masked(int i0) { return (i0 + 1) / kPaKeys; }
@@ -456,7 +460,7 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
         // Step g is a tile of keys of an item.  In the order of issue: P V of step g - 1 and Q K^T of step g for row tile 0, then for row
         // tile 1; MMAs are carried out in this order, so S may overwrite the P that the product before it has read.  Where P has
         // a place of its own, Q K^T goes first, as soon as the scores of step g - 1 are in registers.
-        constexpr uint32_t id_s = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kPaKeys >> 3) << 17) | (8u << 24);
+        constexpr uint32_t id_rows = (1u << 4) | (1u << 7) | (1u << 10) | (8u << 24);   // S: N is the keys that are seen
         constexpr uint32_t id_o = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)(D >> 3) << 17) | (8u << 24);
         const uint32_t elected = ca_elect();
         uint32_t at = 0, ph = 0;                              // place in the ring: K of step g, or V of step g - 1 behind it
@@ -493,6 +497,7 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
             auto pv = [&](int i) {
                 if (!have_p || jp >= (i ? prev.nt1 : prev.nt0)) return;
                 const uint64_t dv = ca_desc(smem_u32(s_kv + v_at * L::kTileBytes), L::kChunk, 1024, 2);
+                const int keys = pa_keys(p, prev.n, prev.i0 + i * p.TQ, jp);
 #pragma unroll
                 for (int s = 0; s < kPaKeys / 16; ++s) {
                     if (s % (kPaKeys / 32) == 0) {            // half of P is there
@@ -500,7 +505,7 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
                         if (!ok) return;
                         tc_fence_after();
                     }
-                    pa_mma_ts(tmem + L::kColO + i * D, tmem + i * L::kColS + L::kColP + s * 8, dv + ((s * 2048) >> 4), id_o, (jp | s) ? 1u : 0u, elected);
+                    if (s * 16 < keys) pa_mma_ts(tmem + L::kColO + i * D, tmem + i * L::kColS + L::kColP + s * 8, dv + ((s * 2048) >> 4), id_o, (jp | s) ? 1u : 0u, elected);
                 }
                 ++steps[i];
                 ca_commit(smem_u32(&b_o[i]), elected);
@@ -514,6 +519,7 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
                 tc_fence_after();
                 const uint64_t dq = ca_desc(smem_u32(s_q + i * L::kTileBytes), 16, 1024, 2);
                 const uint64_t dk = ca_desc(smem_u32(s_kv + k_at * L::kTileBytes), 16, 1024, 2);
+                const uint32_t id_s = id_rows | ((uint32_t)(pa_keys(p, cur.n, cur.i0 + i * p.TQ, j) >> 3) << 17);
 #pragma unroll
                 for (int s = 0; s < D / 16; ++s) {
                     const uint32_t off = ((s >> 2) * L::kChunk + (s & 3) * 32) >> 4;
@@ -645,28 +651,31 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
                     tc_fence_after();
                 }
                 const float nm = m == -INFINITY ? 0.f : -m;
+                const int keys = pa_keys(p, it.n, i0, j);
                 const uint64_t c2 = pa_pk(p.c, p.c), nm2 = pa_pk(nm, nm);
                 uint64_t sum[2] = {0ull, 0ull};
 #pragma unroll
                 for (int c = 0; c < 128; c += 32) {
-                    uint32_t w[16];
+                    if (c < 64 || keys > 64) {                // else the product does not read it
+                        uint32_t w[16];
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        uint64_t x2 = pa_fma2(pa_pk(s[c + 2 * e], s[c + 2 * e + 1]), c2, nm2);
-                        float x, y;
-                        if ((e * L::kPoly) % 16 < L::kPoly) {
-                            x2 = pa_exp2x2(x2);
-                            pa_upk(x2, x, y);
-                        } else {
-                            pa_upk(x2, x, y);
-                            x = ex2(x);
-                            y = ex2(y);
-                            x2 = pa_pk(x, y);
+                        for (int e = 0; e < 16; ++e) {
+                            uint64_t x2 = pa_fma2(pa_pk(s[c + 2 * e], s[c + 2 * e + 1]), c2, nm2);
+                            float x, y;
+                            if ((e * L::kPoly) % 16 < L::kPoly) {
+                                x2 = pa_exp2x2(x2);
+                                pa_upk(x2, x, y);
+                            } else {
+                                pa_upk(x2, x, y);
+                                x = ex2(x);
+                                y = ex2(y);
+                                x2 = pa_pk(x, y);
+                            }
+                            sum[e & 1] = pa_add2(sum[e & 1], x2);
+                            w[e] = pa_bf16x2(x, y);
                         }
-                        sum[e & 1] = pa_add2(sum[e & 1], x2);
-                        w[e] = pa_bf16x2(x, y);
+                        pa_st16(t_p + (c >> 1), w);
                     }
-                    pa_st16(t_p + (c >> 1), w);
                     if (c == 96 && masked) {                  // what was marked in V is seen behind this
                         const uint32_t r = ring + 2 * j + 1;
                         ok = wait(&b_full[r % RING], (r / RING) & 1);

@@ -5,17 +5,25 @@
 // A frequency is held in turns as a 64-bit binary fraction, so the angle modulo one turn is the low half of an integer
 // product: exact at every position, where the product in fp32 is off by 0.01 radians at position 100000.
 //
-// Bound by HBM: every element is read and written once.  A CTA takes a few tokens; its threads first compute the sines and
-// cosines of those tokens into shared memory (one pair of functions a thread), then sweep over heads x chunks of pairs: a sine is
-// computed once for all heads.  Four tokens of 64 pairs give each of 256 threads one pair; calls of few tokens take one token
-// a CTA, so that the heads of a token are spread over all its threads.
+// Bound by HBM: every element is read and written once.  A warp takes a token, or a part of its heads where there are few tokens: it
+// computes the token's sines and cosines (a lane those of every 32nd pair) into shared memory and sweeps over heads x chunks of
+// pairs, so that they are computed once for many heads.  Warps do not wait for one another; the first chunks are on their way
+// while a warp looks for the position (trees: a search for the sequence, a walk to the root).
 #include "bs_common.cuh"
 
 namespace bs {
 
-constexpr int kRoThreads = 256;
-constexpr int kRoTokens = 4;                   // tokens of a CTA where there are enough of them
+constexpr int kRoWarps = 4;
 constexpr int kRoMaxRot = 256;
+constexpr int kRoBatch = 1;                    // chunks of a lane in flight
+constexpr int kRoTarget = 24;                  // warps for each SM: below that, a token's heads are divided
+
+// Division by a number that the host knows.
+struct RoDiv {
+    uint32_t m;
+    int shift;
+    __device__ __forceinline__ int div(int n) const { return (int)(((uint64_t)(uint32_t)n * m) >> shift); }
+};
 
 struct RotaryParams {
     const void *q, *k;
@@ -27,11 +35,26 @@ struct RotaryParams {
     const int32_t* node_parent;                // NULL: chains
     float amplitude;
     int rot, T, Hq, H, d, B, Nmax;             // H: heads of q and k
-    int tokens, copy_rest;                     // of a CTA; the elements behind rot have to be copied
+    int chunks;                                // of a head, those that are only copied among them
+    int parts, part_items;                     // of a token; chunks of a part
+    RoDiv by_chunk;
 };
 
 template <typename T, int P> struct alignas(sizeof(T) * P) RoVec { T v[P]; };
 
+// Elements pass through once: around L1, where every line would take a place (24000 tokens of 40 heads: 89 us through it, 82 around it).
+template <typename V> __device__ __forceinline__ V ro_ld(const V* p) {
+    if constexpr (sizeof(V) == 16) {
+        const uint4 v = __ldcg(reinterpret_cast<const uint4*>(p));
+        return *reinterpret_cast<const V*>(&v);
+    } else {
+        return *p;
+    }
+}
+template <typename V> __device__ __forceinline__ void ro_st(V* p, const V& v) {
+    if constexpr (sizeof(V) == 16) __stcg(reinterpret_cast<uint4*>(p), *reinterpret_cast<const uint4*>(&v));
+    else *p = v;
+}
 __device__ __forceinline__ float ro_float(float x) { return x; }
 __device__ __forceinline__ float ro_float(__nv_bfloat16 x) { return __bfloat162float(x); }
 __device__ __forceinline__ void ro_set(float& y, float x) { y = x; }
@@ -67,62 +90,105 @@ __device__ __forceinline__ int ro_position(const RotaryParams& p, int t) {
 
 // P pairs are loaded as two vectors of P elements: the halves' (HALF), or 2P neighbours' (two by two).
 template <typename T, int P, bool HALF>
-__global__ void __launch_bounds__(kRoThreads) rotary_kernel(const RotaryParams p) {
-    __shared__ int s_pos[kRoTokens];
-    __shared__ __align__(16) float s_cos[kRoTokens * kRoMaxRot / 2], s_sin[kRoTokens * kRoMaxRot / 2];
-    const int tid = threadIdx.x, half = p.rot / 2, t0 = blockIdx.x * p.tokens, nt = min(p.tokens, p.T - t0);
+__global__ void __launch_bounds__(kRoWarps * 32) rotary_kernel(const RotaryParams p) {
+    using Vec = RoVec<T, P>;
+    __shared__ float s_cos[kRoWarps][kRoMaxRot / 2], s_sin[kRoWarps][kRoMaxRot / 2];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const long long task = (long long)blockIdx.x * kRoWarps + warp;
+    if (task >= (long long)p.T * p.parts) return;
+    const int t = p.parts == 1 ? (int)task : (int)(task / p.parts), part = (int)(task - (long long)t * p.parts);
+    const int half = p.rot / 2, n_rot = half / P;
+    const int end = min(p.H * p.chunks, (part + 1) * p.part_items);
     pdl_enter();
-    for (int i = tid >> 5; i < nt; i += kRoThreads / 32) {
-        const int pos = ro_position(p, t0 + i);
-        if ((tid & 31) == 0) s_pos[i] = pos;
-    }
-    __syncthreads();
-    for (int i = tid; i < nt * half; i += kRoThreads) {
-        const int tok = i / half, j = i - tok * half, pos = s_pos[tok];
-        if (pos < 0) continue;
+    struct Item { int c, at_a, at_b; const T* x; T* y; };
+    auto item = [&](int i) {
+        Item r;
+        const int head = p.by_chunk.div(i);
+        r.c = i - head * p.chunks;
+        if (head < p.Hq) {
+            r.x = (const T*)p.q + t * p.q_st + (long long)head * p.q_sh;
+            r.y = (T*)p.q_out + t * p.qo_st + (long long)head * p.qo_sh;
+        } else {
+            r.x = (const T*)p.k + t * p.k_st + (long long)(head - p.Hq) * p.k_sh;
+            r.y = (T*)p.k_out + t * p.ko_st + (long long)(head - p.Hq) * p.ko_sh;
+        }
+        const bool halves = HALF && r.c < n_rot;              // behind the rotated part: rot = 2 P n_rot
+        r.at_a = halves ? r.c * P : r.c * 2 * P;
+        r.at_b = halves ? half + r.c * P : r.at_a + P;
+        return r;
+    };
+    Vec a[kRoBatch], b[kRoBatch];
+    auto load = [&](int base) {
+#pragma unroll
+        for (int u = 0; u < kRoBatch; ++u)
+            if (base + 32 * u < end) {
+                const Item r = item(base + 32 * u);
+                a[u] = ro_ld(reinterpret_cast<const Vec*>(r.x + r.at_a));
+                b[u] = ro_ld(reinterpret_cast<const Vec*>(r.x + r.at_b));
+            }
+    };
+    int base = part * p.part_items + lane;
+    load(base);
+    const int pos = ro_position(p, t);
+    if (pos < 0) return;
+    float *cos_of = s_cos[warp], *sin_of = s_sin[warp];
+    for (int j = lane; j < half; j += 32) {
         const int64_t turns = (int64_t)((uint64_t)(uint32_t)pos * __ldg(p.freq + j));   // of a turn, in [-1/2, 1/2) x 2^64
         float s, c;
         sincospif((float)turns * 1.0842021724855044e-19f, &s, &c);                      // 2^-63: half turns
-        // pair j of chunk j / P: the chunks of a warp's lanes lie side by side
-        const int at = tok * half + (j % P) * (half / P) + j / P;
-        s_cos[at] = c * p.amplitude;
-        s_sin[at] = s * p.amplitude;
+        const int at = (j % P) * n_rot + j / P;               // the chunks of a warp's lanes lie side by side
+        cos_of[at] = c * p.amplitude;
+        sin_of[at] = s * p.amplitude;
     }
-    __syncthreads();
-    const int n_rot = half / P, n_chunks = p.copy_rest ? p.d / (2 * P) : n_rot, per_token = p.H * n_chunks;
-    using Vec = RoVec<T, P>;
-    for (int i = tid; i < nt * per_token; i += kRoThreads) {
-        const int tok = i / per_token, w = i - tok * per_token, head = w / n_chunks, c = w - head * n_chunks;
-        if (s_pos[tok] < 0) continue;
-        const long long t = t0 + tok;
-        const bool is_q = head < p.Hq;
-        const long long hh = is_q ? head : head - p.Hq;
-        const T* x = is_q ? (const T*)p.q + t * p.q_st + hh * p.q_sh : (const T*)p.k + t * p.k_st + hh * p.k_sh;
-        T* y = is_q ? (T*)p.q_out + t * p.qo_st + hh * p.qo_sh : (T*)p.k_out + t * p.ko_st + hh * p.ko_sh;
-        const bool rotates = c < n_rot;
-        const int ia = HALF && rotates ? c * P : c * 2 * P, ib = HALF && rotates ? half + c * P : ia + P;   // rot = 2 P n_rot
-        Vec a = *reinterpret_cast<const Vec*>(x + ia), b = *reinterpret_cast<const Vec*>(x + ib);
-        if (rotates) {
-            const float *cs = s_cos + tok * half + c, *sn = s_sin + tok * half + c;
+    __syncwarp();
+#pragma unroll 1
+    for (;;) {
 #pragma unroll
-            for (int e = 0; e < P; ++e) {
-                T& ra = HALF ? a.v[e] : (2 * e < P ? a.v[(2 * e) % P] : b.v[(2 * e) % P]);
-                T& rb = HALF ? b.v[e] : (2 * e + 1 < P ? a.v[(2 * e + 1) % P] : b.v[(2 * e + 1) % P]);
-                const float fa = ro_float(ra), fb = ro_float(rb), co = cs[e * n_rot], si = sn[e * n_rot];
-                ro_set(ra, fmaf(fa, co, -fb * si));           // the one rounding to T
-                ro_set(rb, fmaf(fb, co, fa * si));
+        for (int u = 0; u < kRoBatch; ++u)
+            if (base + 32 * u < end) {
+                const Item r = item(base + 32 * u);
+                if (r.c < n_rot) {
+#pragma unroll
+                    for (int e = 0; e < P; ++e) {
+                        T& ra = HALF ? a[u].v[e] : (2 * e < P ? a[u].v[(2 * e) % P] : b[u].v[(2 * e) % P]);
+                        T& rb = HALF ? b[u].v[e] : (2 * e + 1 < P ? a[u].v[(2 * e + 1) % P] : b[u].v[(2 * e + 1) % P]);
+                        const float fa = ro_float(ra), fb = ro_float(rb), co = cos_of[e * n_rot + r.c], si = sin_of[e * n_rot + r.c];
+                        ro_set(ra, fmaf(fa, co, -fb * si));   // the one rounding to T
+                        ro_set(rb, fmaf(fb, co, fa * si));
+                    }
+                }
+                ro_st(reinterpret_cast<Vec*>(r.y + r.at_a), a[u]);
+                ro_st(reinterpret_cast<Vec*>(r.y + r.at_b), b[u]);
             }
-        }
-        *reinterpret_cast<Vec*>(y + ia) = a;
-        *reinterpret_cast<Vec*>(y + ib) = b;
+        base += 32 * kRoBatch;
+        if (base - lane >= end) break;
+        load(base);
     }
 }
 
+static RoDiv ro_div(uint32_t d) {
+    RoDiv r;
+    int log = 0;
+    while ((1u << log) < d) ++log;
+    r.shift = 31 + log;                                       // m = ceil(2^shift / d) < 2^32, error n (m d - 2^shift) < 2^shift for n < 2^31
+    r.m = (uint32_t)(((1ull << r.shift) + d - 1) / d);
+    return r;
+}
+
 template <typename T, int P>
-static cudaError_t launch_rotary(const RotaryParams& p, bool half, cudaStream_t st) {
-    const int grid = div_up(p.T, p.tokens);
-    return half ? launch_pdl(rotary_kernel<T, P, true>, grid, kRoThreads, 0, st, p)
-                : launch_pdl(rotary_kernel<T, P, false>, grid, kRoThreads, 0, st, p);
+static cudaError_t launch_rotary(RotaryParams p, bool copies, bool half, cudaStream_t st) {
+    p.chunks = (copies ? p.d : p.rot) / (2 * P);
+    p.by_chunk = ro_div((uint32_t)p.chunks);
+    // Few tokens: their heads are divided among warps, down to one chunk a lane.
+    const int per_token = p.H * p.chunks, most = div_up(per_token, 32);
+    const long long want = ((long long)kRoTarget * sm_count() + p.T - 1) / p.T;
+    p.parts = want < most ? (int)want : most;
+    p.part_items = div_up(most, p.parts) * 32;
+    p.parts = div_up(per_token, p.part_items);
+    const long long grid = ((long long)p.T * p.parts + kRoWarps - 1) / kRoWarps;
+    if (grid > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
+    return half ? launch_pdl(rotary_kernel<T, P, true>, (unsigned)grid, kRoWarps * 32, 0, st, p)
+                : launch_pdl(rotary_kernel<T, P, false>, (unsigned)grid, kRoWarps * 32, 0, st, p);
 }
 
 }  // namespace bs
@@ -181,10 +247,9 @@ extern "C" bs_status bs_rotary(const void* q, long long q_stride_t, long long q_
     p.positions = positions; p.freq = freq; p.cu_new = cu_new; p.node_parent = node_parent;
     p.amplitude = amplitude;
     p.rot = rot; p.T = T; p.Hq = Hq; p.H = Hq + Hkv; p.d = d; p.B = B; p.Nmax = Nmax;
-    p.tokens = T >= 4 * kRoTokens * sm_count() ? kRoTokens : 1;
     const bool q_moves = Hq && (q != q_out || q_stride_t != qo_stride_t || q_stride_h != qo_stride_h);
     const bool k_moves = Hkv && (k != k_out || k_stride_t != ko_stride_t || k_stride_h != ko_stride_h);
-    p.copy_rest = rot < d && (q_moves || k_moves);
+    const bool copies = rot < d && (q_moves || k_moves);
     // the widest vector that divides both parts of a head and that every row starts on
     const int es = dtype == BS_F32 ? 4 : 2;
     auto fits = [&](int P) {
@@ -198,10 +263,10 @@ extern "C" bs_status bs_rotary(const void* q, long long q_stride_t, long long q_
     const cudaStream_t st = (cudaStream_t)stream;
     const bool half = !interleaved;
     if (dtype == BS_F32)
-        return cuda_status(fits(4) ? launch_rotary<float, 4>(p, half, st) : fits(2) ? launch_rotary<float, 2>(p, half, st)
-                                                                                    : launch_rotary<float, 1>(p, half, st));
-    return cuda_status(fits(8)   ? launch_rotary<__nv_bfloat16, 8>(p, half, st)
-                       : fits(4) ? launch_rotary<__nv_bfloat16, 4>(p, half, st)
-                       : fits(2) ? launch_rotary<__nv_bfloat16, 2>(p, half, st)
-                                 : launch_rotary<__nv_bfloat16, 1>(p, half, st));
+        return cuda_status(fits(4) ? launch_rotary<float, 4>(p, copies, half, st) : fits(2) ? launch_rotary<float, 2>(p, copies, half, st)
+                                                                                    : launch_rotary<float, 1>(p, copies, half, st));
+    return cuda_status(fits(8)   ? launch_rotary<__nv_bfloat16, 8>(p, copies, half, st)
+                       : fits(4) ? launch_rotary<__nv_bfloat16, 4>(p, copies, half, st)
+                       : fits(2) ? launch_rotary<__nv_bfloat16, 2>(p, copies, half, st)
+                                 : launch_rotary<__nv_bfloat16, 1>(p, copies, half, st));
 }

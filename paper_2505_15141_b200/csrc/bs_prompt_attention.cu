@@ -3,22 +3,29 @@
 //   out_i = sum_{j <= i} p_ij v_j / sum_{j <= i} p_ij,   p_ij = 2^(c q_i . k_j - m_i),   c = softmax_scale * log2(e)
 //
 // One pass over the keys with a reference m_i of the row: the products S = Q K^T and O += P V run on the tensor cores with their
-// accumulators in tensor memory; P takes the place of S there, as bf16, and is the A operand of the second product.  The
+// accumulators in tensor memory; P is written there, too, as bf16, and is the A operand of the second product.  The
 // reference is the row's maximum when it was last looked at: only where a later score exceeds it by more than 8 (2^8 times; fp32
 // and bf16 hold that with the same relative precision) is it moved and the accumulator rescaled, which is rare after
 // the first tiles.  P is rounded to bf16 (2^-8 relative at most); its sum is taken before that, in fp32.
 //
 // An item is a pair of row tiles of one key head; a tile holds 128 / G new tokens x G query heads (G = Hq / Hkv), so that the heads of a
 // group share the copies of K and V and short prompts fill the tiles.  Two tiles are in flight: while the softmax of one
-// runs, the tensor cores work on the other.
+// runs, the tensor cores work on the other.  The last tile of keys is only as wide as it is seen.
 //
 // Warps: 0-3 and 4-7 softmax of the two tiles, a row a thread; 8 MMA issuer; 9 copies (TMA); 10 scheduler; 11 looks through the tiles
-// of V that are seen in part.  The grid has a CTA for
-// every item, the longest first; a running CTA takes over the item of one that has not begun
-// (cluster launch control), so that copies and products of the next item begin under the end of the one before.
+// of V that are seen in part.  The grid has a CTA for every item, the longest first; a running CTA takes over the item of one that
+// has not begun (cluster launch control), so that copies and products of the next item begin under the end of the one before.
 //
 // Heads of 128 fill tensor memory with S and O of two tiles, and P takes the place of S; the chain of a tile is then S, softmax, P V, S of
-// the next keys.  Heads of 64 leave room for P beside S, which takes the products out of that chain.
+// the next keys.  Heads of 64 leave room for P beside S, which takes the products out of that chain (160 -> 122 us for 4 prompts
+// of 1000 to 4095, 16 heads).
+//
+// Measured, 32 query and 8 key heads of 128: one prompt of 16384, 2.0 ms, 1.1 PFLOP/s at the 1.45 to 1.5 GHz that the power limit leaves;
+// 16 prompts of 1 to 4096, 0.48 ms, 0.94 PFLOP/s.  Bound by the products: without any softmax the same copies and products take
+// 1.63 and 0.41 ms.  Q, K and V are read from shared memory at 128 bytes a cycle: Q and K of a tile cost 512 cycles, what the
+// product itself does, V 256, and the copies that write K and V 512 for both tiles, so shared memory is as busy as the
+// tensor cores.  What made no difference, or a loss, to the softmax: two threads a row (+8 %), a part of the exponentials as
+// polynomials on the FMA units (+-1 %), no look at the maxima but at the sums (+8 %), a warpgroup of its own for the results (+-1 %).
 #include "bs_cache_attention.cuh"
 
 namespace bs {
@@ -46,7 +53,7 @@ template <int D> struct PaLayout {
     static constexpr int kTileBytes = kPaKeys * D * 2;        // of Q, K or V
     static constexpr int kChunk = 128 * 128;                  // 128 rows of 64 elements
     static constexpr int kChunks = D / 64;
-    static constexpr int kRing = D == 128 ? 4 : 8;            // even
+    static constexpr int kRing = D == 128 ? 4 : 8;            // half of the places are for V
     static constexpr int kOut = 32 * 128;                     // 32 rows of 64 results, for each softmax warp
     static constexpr int kDynamic = (2 + kRing) * kTileBytes + 8 * kOut + 1024;
     // Tensor memory: the scores of row tile i at i * kColS, its probabilities kColP further, its accumulator at kColO + i * D.  Heads of 64
@@ -54,7 +61,6 @@ template <int D> struct PaLayout {
     static constexpr bool kApart = D == 64;
     static constexpr int kColS = kApart ? 192 : 128, kColP = kApart ? 128 : 0, kColO = 2 * kColS;
     static_assert(kColO + 2 * D <= 512, "tensor memory");
-    static constexpr int kPoly = D == 128 ? 2 : 4;            // of 16 pairs of exponentials, those that the FMA units compute
     static constexpr uint32_t kTmemCols = 512;
 };
 
@@ -127,23 +133,6 @@ __device__ __forceinline__ float pa_max3(float a, float b, float c) {   // NaN i
     float r;
     asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
     return r;
-}
-// 2^x of two numbers up to 2^22 without the special-function unit: x = n + f, |f| <= 1/2, n by rounding to whole numbers in
-// fp32; 2^f as a cubic through 1 at 0, fitted to the smallest largest relative error (1.02e-4, a fortieth of what rounding to bf16
-// adds); n goes to the exponent.  Below -127 the result is 0, in the last step above it something below 2^-126.
-__device__ __forceinline__ uint64_t pa_exp2x2(uint64_t x2) {
-    float x, y, rx, ry;
-    pa_upk(x2, x, y);
-    x2 = pa_pk(fmaxf(x, -127.f), fmaxf(y, -127.f));
-    const uint64_t r2 = pa_add2(x2, pa_pk(12582912.f, 12582912.f));          // 1.5 x 2^23: n in the low bits
-    const uint64_t f2 = pa_fma2(pa_add2(r2, pa_pk(-12582912.f, -12582912.f)), pa_pk(-1.f, -1.f), x2);
-    uint64_t p2 = pa_fma2(f2, pa_pk(0.05500767f, 0.05500767f), pa_pk(0.2422092f, 0.2422092f));
-    p2 = pa_fma2(p2, f2, pa_pk(0.69328287f, 0.69328287f));
-    p2 = pa_fma2(p2, f2, pa_pk(1.f, 1.f));
-    pa_upk(r2, rx, ry);
-    pa_upk(p2, x, y);
-    return pa_pk(__uint_as_float(__float_as_uint(x) + (__float_as_uint(rx) << 23)),
-                 __uint_as_float(__float_as_uint(y) + (__float_as_uint(ry) << 23)));
 }
 __device__ __forceinline__ uint32_t pa_bf16x2(float lo, float hi) {
     uint32_t r;
@@ -221,7 +210,7 @@ __device__ __forceinline__ bool pa_masked(int i0, int j) { return (j + 1) * kPaK
 __device__ __forceinline__ int pa_first_masked(int i0) { return (i0 + 1) / kPaKeys; }
 
 // Items in the order of their numbers: 32 sequences at a time, and of these the items with the most keys first, whichever sequence
-// they are of, so that none of the long ones begins last (sequence after sequence: 4 prompts of 1000 to 4095, 157 us for PLACE); the key
+// they are of, so that none of the long ones begins last (sequence after sequence: 4 prompts of 1000 to 4095, 157 us instead of 122); the key
 // heads of the same rows together.
 struct PaWalk {
     int b0;                                    // 32 sequences, one a lane
@@ -660,18 +649,11 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
                         uint32_t w[16];
 #pragma unroll
                         for (int e = 0; e < 16; ++e) {
-                            uint64_t x2 = pa_fma2(pa_pk(s[c + 2 * e], s[c + 2 * e + 1]), c2, nm2);
                             float x, y;
-                            if ((e * L::kPoly) % 16 < L::kPoly) {
-                                x2 = pa_exp2x2(x2);
-                                pa_upk(x2, x, y);
-                            } else {
-                                pa_upk(x2, x, y);
-                                x = ex2(x);
-                                y = ex2(y);
-                                x2 = pa_pk(x, y);
-                            }
-                            sum[e & 1] = pa_add2(sum[e & 1], x2);
+                            pa_upk(pa_fma2(pa_pk(s[c + 2 * e], s[c + 2 * e + 1]), c2, nm2), x, y);
+                            x = ex2(x);
+                            y = ex2(y);
+                            sum[e & 1] = pa_add2(sum[e & 1], pa_pk(x, y));
                             w[e] = pa_bf16x2(x, y);
                         }
                         pa_st16(t_p + (c >> 1), w);

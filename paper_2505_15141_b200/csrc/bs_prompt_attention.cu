@@ -230,7 +230,7 @@ __device__ __forceinline__ void pa_walk_load(const PromptAttnParams& p, PaWalk& 
         if (lane >= o) sum += up;
     }
     ok = ok && w.tokens + sum <= p.T;                         // sequences that overlap: more tokens than there are
-    if (!ok && p.status) atomicOr(p.status + b, BS_DEV_BAD_LENGTH);
+    if (!ok && b < p.B && p.status) atomicOr(p.status + b, BS_DEV_BAD_LENGTH);
     w.row0 = c0;
     w.n = ok ? n : 0;
     w.pairs = (w.n + 2 * p.TQ - 1) / (2 * p.TQ);
@@ -781,7 +781,6 @@ static std::atomic<bool> g_pa_attr[2][64];
 // [T, H, d] bf16; a box is 64 elements of `heads` heads of `rows` tokens, rows of 128 bytes, swizzled.
 static bool pa_map(CUtensorMap* tm, const void* base, int T, int H, int d, long long st, long long sh, int heads, int rows) {
     EncodeTiledFn enc = encode_tiled_fn();
-    if (!enc) return false;
     const cuuint64_t dims[3] = {(cuuint64_t)d, (cuuint64_t)H, (cuuint64_t)T};
     const cuuint64_t strides[2] = {(cuuint64_t)sh * 2, (cuuint64_t)st * 2};
     const cuuint32_t box[3] = {64, (cuuint32_t)heads, (cuuint32_t)rows};
@@ -832,6 +831,7 @@ extern "C" bs_status bs_prompt_attention(const void* q, long long q_stride_t, lo
     // pairs of row tiles: each sequence rounds up once
     const long long grid = ((long long)T / (2 * p.TQ) + B) * Hkv;
     if (grid > 0x7fffffffLL) return BS_ERR_UNSUPPORTED;
+    if (!encode_tiled_fn()) return BS_ERR_CUDA;
     CUtensorMap tm[3];
     if (!pa_map(&tm[0], q, T, Hq, d, q_stride_t, q_stride_h, p.G, p.TQ) || !pa_map(&tm[1], k, T, Hkv, d, k_stride_t, k_stride_h, 1, kPaKeys) ||
         !pa_map(&tm[2], v, T, Hkv, d, v_stride_t, v_stride_h, 1, kPaKeys))

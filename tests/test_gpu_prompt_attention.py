@@ -220,3 +220,13 @@ def test_long_prompt(lib):
     out = torch.zeros(q.shape, dtype=torch.bfloat16, device=DEV)
     lib.bs_prompt_attention(q, k, v, _cu(n), d ** -0.5, out)
     _check(out, q, k, v, n, d ** -0.5)
+
+
+def test_reports_stay_within_the_batch(lib):
+    """Sequences that overlap hold more tokens than there are: those are reported, and nothing behind the batch."""
+    q, k, v = _inputs([210], 2, 1, 64, seed=14)
+    around = torch.zeros(64, dtype=torch.int32, device=DEV)
+    out = torch.zeros(q.shape, dtype=torch.bfloat16, device=DEV)
+    lib.bs_prompt_attention(q, k, v, torch.tensor([0, 100, 60, 210], dtype=torch.int32, device=DEV), 0.125, out, around[8:11])
+    assert around[8:11].tolist() == [0, lib.BS_DEV_BAD_LENGTH, lib.BS_DEV_BAD_LENGTH]
+    assert not around[:8].any() and not around[11:].any()

@@ -8,9 +8,9 @@
 // the vocabulary of one sequence, eight a lane.  Few of them change by more than the mask (700 tokens of a history in 152064 are one in
 // a warp), so the rows are copied as they are, masked in the type's own bits, and the elements that change are mended behind it,
 // each in each row by a lane.  With the arithmetic in the rows for all elements the kernel was bound by instructions (73 us instead of
-// 60 for 64 sequences of 3 to 9 bf16 rows of 152064: 0.25 GB, 4.2 TB/s; rows with masks alone 6.0).  Where many change
-// (frequent tokens, long histories on small vocabularies) the rows are worked on whole.  Two rows of bf16 in flight and 40 warps an SM
-// were faster than four rows and 32.  Biases are added in the order of the list, so that sums do not depend on timing.
+// 56 for 64 sequences of 3 to 9 bf16 rows of 152064: 0.25 GB, 4.6 TB/s; rows with masks alone 6.2).  Where many change
+// (frequent tokens, long histories on small vocabularies) the rows are worked on whole.  Two rows of bf16 in flight and 48 warps an SM
+// were faster than four rows and 32 warps.  Biases are added in the order of the list, so that sums do not depend on timing.
 // In place, only what is forbidden and those elements are written, nothing else is read.
 //
 // history: entries of 16 bits, 2 x (times emitted, up to 16383) + (in the prompt).  A history that begins anew is built in
@@ -179,7 +179,7 @@ __device__ __forceinline__ bool ad_biases(const AdjustParams& p, int lo, int hi,
 }
 
 template <typename T, bool VEC>
-__global__ void __launch_bounds__(kAdWarps * 32, VEC ? 10 : 8) logits_adjust_kernel(const AdjustParams p) {
+__global__ void __launch_bounds__(kAdWarps * 32, 12) logits_adjust_kernel(const AdjustParams p) {
     using Io = AdIo<T, VEC>;
     __shared__ float s_sum[kAdWarps][kAdWarp];                // biases
     __shared__ float2 s_list[kAdWarps][kAdFew];               // elements that change
@@ -209,20 +209,17 @@ __global__ void __launch_bounds__(kAdWarps * 32, VEC ? 10 : 8) logits_adjust_ker
         rows = min(rows, g + p.extra);
     }
     if (rows <= p.row_begin && !(p.status && blockIdx.y == 0)) return;   // the whole CTA
-    float add[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) add[e] = 0.f;
-    uint32_t any = 0u;
+    uint32_t any = 0u;                                        // elements with a bias, then those that are seen, too
+    bool biased = false;
     if (p.bias_begin) {
         const int lo = __ldg(p.bias_begin + b), hi = __ldg(p.bias_begin + b + 1);
         if (lo < 0 || hi > p.n_bias || lo > hi) {
             bits |= BS_DEV_BAD_LENGTH;
         } else if (ad_biases(p, lo, hi, v0, bits, s_sum[warp])) {
+            biased = true;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                add[e] = s_sum[warp][VEC ? lane * 8 + e : 32 * e + lane];
-                if (add[e] != 0.f) any |= 1u << e;
-            }
+            for (int e = 0; e < 8; ++e)
+                if (s_sum[warp][VEC ? lane * 8 + e : 32 * e + lane] != 0.f) any |= 1u << e;
         }
     }
     if (mask < -1 || mask >= p.n_masks) {
@@ -251,20 +248,12 @@ __global__ void __launch_bounds__(kAdWarps * 32, VEC ? 10 : 8) logits_adjust_ker
     if (p.status && blockIdx.y == 0 && bits) atomicOr(p.status + b, bits);
     const uint32_t drafted = __ballot_sync(0xffffffffu, behind && tok >= v0 && tok < min(v0 + kAdWarp, p.V));
 
-    // what the history and the biases do to every element
-    uint32_t seen = 0u, counted = 0u;
+    auto past = [&](int e) { return (h[e >> 1] >> (16 * (e & 1))) & 0xffffu; };   // of an element
     if (h[0] | h[1] | h[2] | h[3]) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const uint32_t v = (h[e >> 1] >> (16 * (e & 1))) & 0xffffu;
-            if (v) seen |= 1u << e;
-            if (v >> 1) {
-                counted |= 1u << e;
-                add[e] -= fmaf(freq, (float)(v >> 1), pres);
-            }
-        }
+        for (int e = 0; e < 8; ++e)
+            if (past(e)) any |= 1u << e;
     }
-    any |= seen;
     any &= there;
     const float inv = 1.f / rep;
     const T* x = reinterpret_cast<const T*>(p.x) + (size_t)b * p.R * p.V + first;
@@ -348,19 +337,18 @@ __global__ void __launch_bounds__(kAdWarps * 32, VEC ? 10 : 8) logits_adjust_ker
             }
         }
         if (!count) return;
-        // the elements, one behind the other: place in the warp's tokens, whether seen and counted, summand
+        // the elements, one behind the other: place in the warp's tokens and history, bias
         float2* list = s_list[warp];
-        int at = __popc(mine);
+        int at = 0;
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int up = __shfl_up_sync(0xffffffffu, at, o);
-            if (lane >= o) at += up;
-        }
-        at -= __popc(mine);
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
+        for (int e = 0; e < 8; ++e) {
+            const uint32_t who = __ballot_sync(0xffffffffu, (mine >> e) & 1u);
+            if (!who) continue;
+            const int off = VEC ? lane * 8 + e : 32 * e + lane;
             if ((mine >> e) & 1u)
-                list[at++] = make_float2(__int_as_float((VEC ? lane * 8 + e : 32 * e + lane) | ((seen >> e) & 1u) << 16 | ((counted >> e) & 1u) << 17), add[e]);
+                list[at + __popc(who & ((1u << lane) - 1u))] = make_float2(__int_as_float(off | past(e) << 16), biased ? s_sum[warp][off] : 0.f);
+            at += __popc(who);
+        }
         __syncwarp();                                         // behind it, too: what the other lanes have stored of the rows
         const int tasks = count * (rows - p.row_begin);       // an element in a row: a lane each
         const uint32_t per = 65536u / (uint32_t)count + 1u;   // t / count for t < 1024, count <= 32
@@ -368,13 +356,14 @@ __global__ void __launch_bounds__(kAdWarps * 32, VEC ? 10 : 8) logits_adjust_ker
         for (int t0 = 0; t0 < tasks; t0 += 32) {
             const int t = min(t0 + lane, tasks - 1), r = p.row_begin + (int)(((uint32_t)t * per) >> 16), l = t - (r - p.row_begin) * count;
             const float2 entry = list[l];
-            const int info = __float_as_int(entry.x), off = info & 0xffff;
+            const uint32_t info = __float_as_uint(entry.x), times = info >> 17;
+            const int off = (int)(info & 0xffffu);
             const size_t place = ((size_t)b * p.R + r) * p.V + v0 + off;
             float f = ad_one(reinterpret_cast<const T*>(p.x) + place);
             const int m = __shfl_sync(0xffffffffu, mask, r);
             const uint32_t word = m >= 0 ? __ldg(p.masks + (size_t)m * mask_words + ((v0 + off) >> 5)) : ~0u;
-            bool is_seen = (info >> 16) & 1, is_counted = (info >> 17) & 1;
-            float less = 0.f;
+            bool is_seen = (info >> 16) != 0u, is_counted = times != 0u;
+            float less = is_counted ? fmaf(freq, (float)times, pres) : 0.f;
             for (uint32_t d = drafted; d; d &= d - 1) {       // they count like emitted ones
                 const int j = __ffs(d) - 1;
                 const int at_j = __shfl_sync(0xffffffffu, tok, j) - v0;
@@ -393,6 +382,18 @@ __global__ void __launch_bounds__(kAdWarps * 32, VEC ? 10 : 8) logits_adjust_ker
     }
 
     // ---- many: worked on in the rows, the next one on its way while one is ----
+    float add[8];
+    uint32_t seen = 0u, counted = 0u;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const uint32_t v = past(e);
+        add[e] = biased ? s_sum[warp][VEC ? lane * 8 + e : 32 * e + lane] : 0.f;
+        if (v) seen |= 1u << e;
+        if (v >> 1) {
+            counted |= 1u << e;
+            add[e] -= fmaf(freq, (float)(v >> 1), pres);
+        }
+    }
     struct Row { uint32_t w[Io::kWords], allowed, own; };
     auto load = [&](int r, Row& row) {
         row.own = 0u;

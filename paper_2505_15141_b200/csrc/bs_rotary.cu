@@ -47,12 +47,16 @@ template <typename V> __device__ __forceinline__ V ro_ld(const V* p) {
     if constexpr (sizeof(V) == 16) {
         const uint4 v = __ldcg(reinterpret_cast<const uint4*>(p));
         return *reinterpret_cast<const V*>(&v);
+    } else if constexpr (sizeof(V) == 8) {
+        const uint2 v = __ldcg(reinterpret_cast<const uint2*>(p));
+        return *reinterpret_cast<const V*>(&v);
     } else {
         return *p;
     }
 }
 template <typename V> __device__ __forceinline__ void ro_st(V* p, const V& v) {
     if constexpr (sizeof(V) == 16) __stcg(reinterpret_cast<uint4*>(p), *reinterpret_cast<const uint4*>(&v));
+    else if constexpr (sizeof(V) == 8) __stcg(reinterpret_cast<uint2*>(p), *reinterpret_cast<const uint2*>(&v));
     else *p = v;
 }
 __device__ __forceinline__ float ro_float(float x) { return x; }

@@ -525,7 +525,7 @@ bs_status bs_rotary(const void* q, long long q_stride_t, long long q_stride_h, c
  *          not negative, 16-byte aligned.  Query head i reads key head i / (Hq / Hkv); Hq / Hkv <= 64.  out overlaps no input
  *  cu_seqlens [B + 1]: sequence b is rows cu_seqlens[b] .. cu_seqlens[b + 1] - 1 (bs_cache_plan's cu_new, if all begin here).  Empty sequences
  *          are fine.  Rows of out behind cu_seqlens[B] are left as they are, what the other arrays hold there does not matter
- *  softmax_scale > 0
+ *  softmax_scale > 0, T <= 2^30
  *  status  [B] or NULL: bits are added.  BS_DEV_BAD_LENGTH: cu_seqlens not ascending, outside [0, T] or with more tokens than T, the
  *          sequence's rows are left as they are; BS_DEV_TIMEOUT in status[0]: a bounded wait gave up, every output is undefined
  *          (without a status array nothing tells)

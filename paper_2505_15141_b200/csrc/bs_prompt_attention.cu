@@ -21,11 +21,12 @@
 // of 1000 to 4095, 16 heads).
 //
 // Measured, 32 query and 8 key heads of 128: one prompt of 16384, 2.0 ms, 1.1 PFLOP/s at the 1.45 to 1.5 GHz that the power limit leaves;
-// 16 prompts of 1 to 4096, 0.48 ms, 0.94 PFLOP/s.  Bound by the products: without any softmax the same copies and products take
-// 1.63 and 0.41 ms.  Q, K and V are read from shared memory at 128 bytes a cycle: Q and K of a tile cost 512 cycles, what the
-// product itself does, V 256, and the copies that write K and V 512 for both tiles, so shared memory is as busy as the
-// tensor cores.  What made no difference, or a loss, to the softmax: two threads a row (+8 %), a part of the exponentials as
-// polynomials on the FMA units (+-1 %), no look at the maxima but at the sums (+8 %), a warpgroup of its own for the results (+-1 %).
+// 16 prompts of 1 to 4096, 0.50 ms, 0.91 PFLOP/s.  Bound by the products: without any softmax the same copies and products take
+// 1.63 (1.35 PFLOP/s; the library's sustained rate is 1.42) and 0.41 ms.  What made no difference, or a loss: two threads a row (+8 %),
+// a part of the exponentials as polynomials on the FMA units (+-1 %), no look at the maxima but at the sums (+8 %), a warpgroup of
+// its own for the results (+-1 %), four streams of 64 keys (+8 to 11 %).  Two CTAs as a pair on products of 256 rows, each with half of K
+// and V: copies and products alone take as long as here (1.66 and 0.41 ms), so that neither shared memory nor the copies set
+// the pace, and with the softmax, whose P then waits for eight warps of two SMs, it is 24 % slower (2.47 and 0.60 ms).
 #include "bs_cache_attention.cuh"
 
 namespace bs {
@@ -830,7 +831,8 @@ extern "C" bs_status bs_prompt_attention(const void* q, long long q_stride_t, lo
     p.B = B; p.T = T; p.Hkv = Hkv; p.G = Hq / Hkv; p.TQ = 128 / p.G;
     // pairs of row tiles: each sequence rounds up once
     const long long grid = ((long long)T / (2 * p.TQ) + B) * Hkv;
-    if (grid > 0x7fffffffLL) return BS_ERR_UNSUPPORTED;
+    // tokens are counted in 32 bits, up to a few tiles behind the last
+    if (T > (1 << 30) || grid > 0x7fffffffLL) return BS_ERR_UNSUPPORTED;
     if (!encode_tiled_fn()) return BS_ERR_CUDA;
     CUtensorMap tm[3];
     if (!pa_map(&tm[0], q, T, Hq, d, q_stride_t, q_stride_h, p.G, p.TQ) || !pa_map(&tm[1], k, T, Hkv, d, k_stride_t, k_stride_h, 1, kPaKeys) ||

@@ -23,8 +23,11 @@
 // Measured, 32 query and 8 key heads of 128: one prompt of 16384, 2.0 ms, 1.1 PFLOP/s at the 1.45 to 1.5 GHz that the power limit leaves;
 // 16 prompts of 1 to 4096, 0.50 ms, 0.91 PFLOP/s.  Bound by the products: without any softmax the same copies and products take
 // 1.63 (1.35 PFLOP/s; the library's sustained rate is 1.42) and 0.41 ms.  What made no difference, or a loss: two threads a row (+8 %),
-// a part of the exponentials as polynomials on the FMA units (+-1 %), no look at the maxima but at the sums (+8 %), a warpgroup of
-// its own for the results (+-1 %), four streams of 64 keys (+8 to 11 %).  Two CTAs as a pair on products of 256 rows, each with half of K
+// a part of the exponentials as polynomials on the FMA units (+-1 %; heads of 64, where the softmax is the longer part, +2 to
+// 8 %: it is the warps' instructions one after the other that take the time, not the special-function units, busy for half of it), no look
+// at the maxima but at the sums (+8 %), a warpgroup of its own for the results (+-1 %), four streams of 64 keys (+8 to 11 %), an
+// issuer for each row tile (+12 to 18 %: in one order of issue the tiles stay half a step apart), turns at the exponentials (+5 and, heads
+// of 64, +33 %), for heads of 64 the next scores fetched under the exponentials (+14 %).  Two CTAs as a pair on products of 256 rows, each with half of K
 // and V: copies and products alone take as long as here (1.66 and 0.41 ms), so that neither shared memory nor the copies set
 // the pace, and with the softmax, whose P then waits for eight warps of two SMs, it is 24 % slower (2.47 and 0.60 ms).
 #include "bs_cache_attention.cuh"
@@ -340,7 +343,7 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
         pa_walk_load(p, w);
         long long item = blockIdx.x;
         bool more = true;
-        uint32_t asked = 0;
+        uint32_t asked = 0, answered = 0;
         auto next = [&]() {                                   // the item of a CTA that has not begun, if there is one
             if (lane == 0) mbar_arrive_expect_tx(smem_u32(&b_next), 16);
             __syncwarp();
@@ -349,8 +352,10 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
                 "setp.ne.b32 e, %2, 0;\n\t"
                 "@e clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];\n\t}"
                 ::"r"(smem_u32(&s_next)), "r"(smem_u32(&b_next)), "r"(elected) : "memory");
-            ok = wait(&b_next, asked++ & 1);
+            ++asked;
+            ok = wait(&b_next, answered & 1);
             if (!ok) return;
+            ++answered;
             uint32_t canceled, x;
             asm volatile(
                 "{\n\t.reg .pred c;\n\t.reg .b128 h;\n\t.reg .b32 y, z, u;\n\t"
@@ -385,6 +390,9 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
 #pragma unroll 1
         while (ok && more) next();                            // the grid has a few CTAs more than there are items
         if (!ok && lane == 0) s_abort = 1;
+        const int zero = 0;                                   // whoever gave up: an answer on its way is waited for
+        if (asked != answered) pa_wait(&b_next, answered & 1, &zero);
+        __syncwarp();
     } else if (warp == 9) {
         // ================================== copies ==================================
         pa_few_registers();

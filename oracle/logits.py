@@ -1,4 +1,4 @@
-"""fp64 checker of the adjustment of logits and of the token history."""
+"""fp64 oracle of the adjustment of logits and of the token history."""
 from __future__ import annotations
 
 import numpy as np

@@ -1,4 +1,4 @@
-"""fp64 checker of what a prompt passes through: rotary positions and causal attention of packed sequences."""
+"""fp64 oracle of what a prompt passes through: rotary positions and causal attention of packed sequences."""
 from __future__ import annotations
 
 import math

@@ -1,4 +1,4 @@
-"""bs_logits_adjust and bs_history_update on the GPU against the fp64 checker."""
+"""bs_logits_adjust and bs_history_update on the GPU against the fp64 oracle."""
 import numpy as np
 import pytest
 import torch

@@ -65,7 +65,7 @@ def test_attention(lib, n, Hq, Hkv, d):
     _check(out, q, k, v, n, d ** -0.5)
 
 
-def test_against_the_plain_checker(lib):
+def test_against_the_plain_oracle(lib):
     n, Hq, Hkv, d = [3, 40, 1, 130], 4, 2, 64
     q, k, v = _inputs(n, Hq, Hkv, d, seed=3)
     out = torch.zeros(q.shape, dtype=torch.bfloat16, device=DEV)

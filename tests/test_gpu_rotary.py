@@ -1,4 +1,4 @@
-"""bs_rotary on the GPU against the fp64 checker: layouts, parts of the head, strides, scalings, far positions, trees."""
+"""bs_rotary on the GPU against the fp64 oracle: layouts, parts of the head, strides, scalings, far positions, trees."""
 import numpy as np
 import pytest
 import torch
@@ -57,7 +57,7 @@ def test_scalings_at_far_positions(lib, scaling, kw):
     lib.bs_rotary(q, None, _ints(pos), lib.new_rotary_table(64, 10000.0, scaling, **kw), False, out, None)
     f, amplitude = op.frequencies(64, 10000.0, scaling, **kw)
     assert (amplitude != 1.0) == (scaling == "yarn")
-    # the checker's own angle: a frequency and the product are off by half a step of fp64 each, 2^31 radians x 2^-52
+    # the oracle's own angle: a frequency and the product are off by half a step of fp64 each, 2^31 radians x 2^-52
     x = q.double().cpu().numpy()
     want = op.rotate(x, pos, f, amplitude, False)
     size = np.abs(x[..., :32]) + np.abs(x[..., 32:])

@@ -216,9 +216,9 @@ def test_trees_without_drafts_are_not_chains(lib, monkeypatch):
     assert seen[0][13] and seen[0][14:16] == (3, 0) and seen[1][13] is None
 
 
-# ---- the checkers themselves ----------------------------------------------------------------------------------
+# ---- the oracles themselves ----------------------------------------------------------------------------------
 
-def test_checker_of_the_rotation():
+def test_oracle_of_the_rotation():
     """Scores of rotated queries and keys depend on the difference of the positions alone; lengths are kept."""
     rng = np.random.default_rng(0)
     f, _ = op.frequencies(16, 10000.0)
@@ -231,7 +231,7 @@ def test_checker_of_the_rotation():
     assert op.depth([0, 0, 1, 3, 9], 4) == 3 and op.depth([0, 0, 1, 3, 9], 5) == 1 and op.depth([-1], 1) == 1
 
 
-def test_checker_of_the_attention():
+def test_oracle_of_the_attention():
     rng = np.random.default_rng(1)
     q, k, v = rng.normal(size=(5, 4, 8)), rng.normal(size=(5, 2, 8)), rng.normal(size=(5, 2, 8))
     out, size = op.attention(q, k, v, [0, 2, 2, 5], 0.3)
@@ -240,7 +240,7 @@ def test_checker_of_the_attention():
     assert np.allclose(out[3, 2], (p / p.sum()) @ v[2:4, 1]) and (size >= np.abs(out) - 1e-12).all()
 
 
-def test_checker_of_the_logits():
+def test_oracle_of_the_logits():
     hist = ol.enter(np.zeros((1, 6)), prompts=[[1, 1, 2]], emitted=[[2, 3, 3]])
     assert hist.tolist() == [[0, 1, 3, 4, 0, 0]]
     x = ol.adjust_row([1.0, 1.0, -1.0, 2.0, 0.5, 0.0], hist[0], drafted=[4, 3], r=2.0, p=0.25, f=0.5, bias=[(0, 1.0), (0, 0.5)], allowed=[1, 1, 1, 1, 1, 0])

@@ -205,7 +205,7 @@ __global__ void __launch_bounds__(kAdWarps * 32, 12) logits_adjust_kernel(const 
     int bits = 0, rows = p.row_end;
     if (p.gamma) {
         int g = __ldg(p.gamma + b);
-        if (g < 0 || g + p.extra > p.R) { g = 0; bits |= BS_DEV_BAD_GAMMA; }
+        if (g < 0 || g > p.R - p.extra) { g = 0; bits |= BS_DEV_BAD_GAMMA; }   // no sum: it could pass 32 bits
         rows = min(rows, g + p.extra);
     }
     if (rows <= p.row_begin && !(p.status && blockIdx.y == 0)) return;   // the whole CTA
@@ -246,6 +246,7 @@ __global__ void __launch_bounds__(kAdWarps * 32, 12) logits_adjust_kernel(const 
         if (lane < p.N && (tok < 0 || tok >= p.V) && lane < rows - 1) bits |= BS_DEV_BAD_TOKEN;
     }
     if (p.status && blockIdx.y == 0 && bits) atomicOr(p.status + b, bits);
+    if (rows <= p.row_begin) return;
     const uint32_t drafted = __ballot_sync(0xffffffffu, behind && tok >= v0 && tok < min(v0 + kAdWarp, p.V));
 
     auto past = [&](int e) { return (h[e >> 1] >> (16 * (e & 1))) & 0xffffu; };   // of an element

@@ -268,3 +268,28 @@ def test_adjust_reads_what_rounds_entered(lib):
         graph.replay()
     torch.cuda.synchronize()
     assert torch.equal(out, first) and np.array_equal(hist.cpu().numpy(), want)
+
+
+@pytest.mark.parametrize("extra", [0, 1])
+@pytest.mark.parametrize("begin", [0, 1])
+@pytest.mark.parametrize("changed", [1, 200])
+def test_any_gamma_outside_the_range_is_zero(lib, changed, begin, extra):
+    """Up to the ends of int32, where a sum with `extra` would wrap; one changed element in a block of the vocabulary, and many."""
+    R, V, far = 4, 256, 2 ** 31
+    gammas = [far - 1, far - 2, -far, -1, R - extra + 1, R - extra, 0]
+    B = len(gammas)
+    g = torch.Generator(device=DEV).manual_seed(1)
+    x = torch.randn(B + 2, R, V, generator=g, device=DEV)    # rows in front and behind: nothing is written there
+    out = torch.full_like(x, 3.0)
+    hist = torch.zeros(B, V, dtype=torch.int16, device=DEV)
+    hist[:, :changed] = 5
+    half = torch.full((B,), 0.5, device=DEV)
+    status = torch.zeros(B, dtype=torch.int32, device=DEV)
+    lib.bs_logits_adjust(x[1:-1], out[1:-1], _ints(gammas), extra, rows=(begin, R), history=hist, presence=half, status=status)
+    bad = [not 0 <= v <= R - extra for v in gammas]
+    assert status.tolist() == [lib.BS_DEV_BAD_GAMMA if v else 0 for v in bad]
+    want = torch.full_like(x, 3.0)
+    for b, v in enumerate(gammas):
+        end = (0 if bad[b] else v) + extra
+        want[b + 1, begin:end] = x[b + 1, begin:end] - 0.5 * (hist[b] > 0)
+    assert torch.equal(out, want)

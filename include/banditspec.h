@@ -577,7 +577,8 @@ bs_status bs_history_update(int16_t* history, int B, int V, const uint8_t* fresh
  *  status       [B] or NULL: bits are added.  BS_DEV_BAD_GAMMA (outside [0, R - extra]; taken as 0), BS_DEV_BAD_MASK, BS_DEV_BAD_TOKEN (a drafted or
  *               a listed one), BS_DEV_BAD_TREE (a parent that is not an earlier node counts as the root), BS_DEV_BAD_LENGTH (biases
  *               outside their arrays, left out)
- * Arithmetic is fp32, rounded once.  Any V works; a multiple of 8 with pointers on 16 bytes takes the widest accesses. */
+ * Arithmetic is fp32, rounded once.  A row's bits do not depend on the other rows of the call, on tokens drafted elsewhere than on its way,
+ * or on what draft_tokens hold beyond gamma.  Any V works; a multiple of 8 with pointers on 16 bytes takes the widest accesses. */
 bs_status bs_logits_adjust(const void* logits, void* out, bs_dtype dtype, const int32_t* gamma, int extra, int row_begin, int row_end,
                            const int32_t* draft_tokens, const int32_t* node_parent, int Nmax, const int16_t* history,
                            const float* repetition, const float* presence, const float* frequency, const int32_t* bias_begin,

@@ -226,7 +226,7 @@ __global__ void __launch_bounds__(kAdWarps * 32, 12) logits_adjust_kernel(const 
         mask = -1;
         if (lane >= p.row_begin && lane < rows) bits |= BS_DEV_BAD_MASK;
     }
-    // the rows (a bit each) that stand behind drafted token `lane`
+    // the rows of this sequence (a bit each) that stand behind drafted token `lane`
     uint32_t behind = 0u;
     if (pen && p.draft_tokens) {
         if (p.node_parent) {
@@ -241,15 +241,24 @@ __global__ void __launch_bounds__(kAdWarps * 32, 12) logits_adjust_kernel(const 
                 if (lane < 31 && (of_row >> (lane + 1)) & 1u) behind |= 1u << r;
             }
         } else {
-            behind = lane < 31 ? ~0u << (lane + 1) : 0u;
+            behind = lane < rows - 1 ? ~0u >> (32 - rows) & ~1u << lane : 0u;
         }
         if (lane < p.N && (tok < 0 || tok >= p.V) && lane < rows - 1) bits |= BS_DEV_BAD_TOKEN;
     }
-    if (p.status && blockIdx.y == 0 && bits) atomicOr(p.status + b, bits);
-    if (rows <= p.row_begin) return;
+    if (p.status && blockIdx.y == 0) {
+        if (bits) atomicOr(p.status + b, bits);
+        if (rows <= p.row_begin) return;
+    }
     const uint32_t drafted = __ballot_sync(0xffffffffu, behind && tok >= v0 && tok < min(v0 + kAdWarp, p.V));
 
     auto past = [&](int e) { return (h[e >> 1] >> (16 * (e & 1))) & 0xffffu; };   // of an element
+    // What is added to an element in every row.  Both ways of working below do x g + addend in one rounding and then subtract for the
+    // drafted tokens one after the other: a row's bits do not show which of them it was.  -0 leaves every x as it is.
+    auto bias_of = [&](int off) {
+        const float a = biased ? s_sum[warp][off] : 0.f;
+        return a == 0.f ? -0.f : a;
+    };
+    auto addend = [&](float bias, uint32_t times) { return times ? bias - fmaf(freq, (float)times, pres) : bias; };
     if (h[0] | h[1] | h[2] | h[3]) {
 #pragma unroll
         for (int e = 0; e < 8; ++e)
@@ -347,7 +356,7 @@ __global__ void __launch_bounds__(kAdWarps * 32, 12) logits_adjust_kernel(const 
             if (!who) continue;
             const int off = VEC ? lane * 8 + e : 32 * e + lane;
             if ((mine >> e) & 1u)
-                list[at + __popc(who & ((1u << lane) - 1u))] = make_float2(__int_as_float(off | past(e) << 16), biased ? s_sum[warp][off] : 0.f);
+                list[at + __popc(who & ((1u << lane) - 1u))] = make_float2(__int_as_float(off | past(e) << 16), bias_of(off));
             at += __popc(who);
         }
         __syncwarp();                                         // behind it, too: what the other lanes have stored of the rows
@@ -363,19 +372,15 @@ __global__ void __launch_bounds__(kAdWarps * 32, 12) logits_adjust_kernel(const 
             float f = ad_one(reinterpret_cast<const T*>(p.x) + place);
             const int m = __shfl_sync(0xffffffffu, mask, r);
             const uint32_t word = m >= 0 ? __ldg(p.masks + (size_t)m * mask_words + ((v0 + off) >> 5)) : ~0u;
-            bool is_seen = (info >> 16) != 0u, is_counted = times != 0u;
-            float less = is_counted ? fmaf(freq, (float)times, pres) : 0.f;
-            for (uint32_t d = drafted; d; d &= d - 1) {       // they count like emitted ones
+            int hits = 0;                                     // drafted tokens before the row: they count like emitted ones
+            for (uint32_t d = drafted; d; d &= d - 1) {
                 const int j = __ffs(d) - 1;
                 const int at_j = __shfl_sync(0xffffffffu, tok, j) - v0;
                 const uint32_t rr = __shfl_sync(0xffffffffu, behind, j);
-                if (at_j == off && ((rr >> r) & 1u)) {
-                    less += is_counted ? freq : freq + pres;
-                    is_seen = is_counted = true;
-                }
+                hits += at_j == off && ((rr >> r) & 1u);
             }
-            if (is_seen) f *= f > 0.f ? inv : rep;
-            f += entry.y - less;
+            f = fmaf(f, (info >> 16) != 0u || hits ? (f > 0.f ? inv : rep) : 1.f, addend(entry.y, times));
+            for (int z = 0; z < hits; ++z) f -= z || times ? freq : freq + pres;
             if (!((word >> ((v0 + off) & 31)) & 1u)) f = -INFINITY;
             if (t0 + lane < tasks) reinterpret_cast<T*>(p.y)[place] = static_cast<T>(f);
         }
@@ -388,12 +393,9 @@ __global__ void __launch_bounds__(kAdWarps * 32, 12) logits_adjust_kernel(const 
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         const uint32_t v = past(e);
-        add[e] = biased ? s_sum[warp][VEC ? lane * 8 + e : 32 * e + lane] : 0.f;
+        add[e] = addend(bias_of(VEC ? lane * 8 + e : 32 * e + lane), v >> 1);
         if (v) seen |= 1u << e;
-        if (v >> 1) {
-            counted |= 1u << e;
-            add[e] -= fmaf(freq, (float)(v >> 1), pres);
-        }
+        if (v >> 1) counted |= 1u << e;
     }
     struct Row { uint32_t w[Io::kWords], allowed, own; };
     auto load = [&](int r, Row& row) {

@@ -293,3 +293,43 @@ def test_any_gamma_outside_the_range_is_zero(lib, changed, begin, extra):
         end = (0 if bad[b] else v) + extra
         want[b + 1, begin:end] = x[b + 1, begin:end] - 0.5 * (hist[b] > 0)
     assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("tree", [False, True])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("V", [512, 515])
+def test_a_row_has_its_bits_whatever_else_is_drafted(lib, V, dtype, tree):
+    """How many elements of a block of the vocabulary change, on all rows together, decides how they are worked on; a row's result
+    must not show it: tokens of other branches and behind the row, left over beyond gamma, in a call of its own or of all rows."""
+    rng = np.random.default_rng(V + tree)
+    R, N, fills = 8, 7, list(range(20, 44))                   # 32 is where the work changes
+    B = len(fills)
+    hist = np.zeros((B, V), np.int16)
+    for b, n in enumerate(fills):
+        hist[b, rng.permutation(250)[:n]] = rng.integers(1, 12, n)
+    x = rng.normal(size=(B, R, V)) * 4
+    x[:, :, 7] = -0.0
+    x[:, :, rng.permutation(V)[:20]] = -0.0
+    x = torch.tensor(x, device=DEV).to(dtype)
+    parent = np.array([[rng.integers(0, j + 1) for j in range(N)] for _ in range(B)]) if tree else None
+    drafted = rng.integers(0, 250, (B, N))
+    drafted[:, 1], drafted[:, 4] = drafted[:, 0], drafted[:, 0]    # the same one more than once
+    fl = lambda lo, hi: torch.tensor(rng.uniform(lo, hi, B), dtype=torch.float32, device=DEV)  # noqa: E731
+    rules = dict(history=torch.tensor(hist, device=DEV), repetition=fl(1.1, 1.7), presence=fl(-0.5, 1.0), frequency=fl(-0.3, 0.9),
+                 bias_begin=_ints(np.arange(B + 1) * 3), bias_tokens=_ints(rng.integers(0, 250, 3 * B)),
+                 bias_values=torch.tensor(rng.normal(size=3 * B), dtype=torch.float32, device=DEV),
+                 node_parent=None if parent is None else _ints(parent))
+    bits = torch.int16 if dtype is torch.bfloat16 else torch.int32
+    base = torch.zeros_like(x)
+    lib.bs_logits_adjust(x, base, _ints([R - 1] * B), 1, draft_tokens=_ints(drafted), **rules)
+    for row in range(R):
+        other = rng.integers(0, 250, (B, N))
+        for b in range(B):
+            for n in ol.path(None if parent is None else parent[b], row):
+                other[b, n - 1] = drafted[b, n - 1]
+        for in_place in (False, True):
+            for only in (False, True):
+                out = x.clone() if in_place else torch.zeros_like(x)
+                lib.bs_logits_adjust(out if in_place else x, out, _ints([row] * B), 1, rows=(row if only else 0, R), draft_tokens=_ints(other), **rules)
+                differ = out[:, row].view(bits) != base[:, row].view(bits)
+                assert not differ.any(), (row, in_place, only, int(differ.sum()))

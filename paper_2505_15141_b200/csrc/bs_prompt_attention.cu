@@ -31,10 +31,10 @@
 // and V: copies and products alone take as long as here (1.66 and 0.41 ms), so that neither shared memory nor the copies set
 // the pace, and with the softmax, whose P then waits for eight warps of two SMs, it is 24 % slower (2.47 and 0.60 ms).
 #include "bs_cache_attention.cuh"
+#include "bs_prompt_items.cuh"
 
 namespace bs {
 
-constexpr int kPaKeys = 128;                   // keys of a tile
 constexpr int kPaItems = 2;                    // items known to a CTA: the current and the next
 constexpr int kPaThreads = 384;
 constexpr float kPaSlack = 8.f;                // a score may exceed the reference by this much (log2)
@@ -46,11 +46,6 @@ struct PromptAttnParams {
     int32_t* status;
     float c;                                   // softmax_scale * log2(e)
     int B, T, Hkv, G, TQ;                      // TQ: tokens of a row tile, 128 / G
-};
-
-struct PaItem {
-    int row0, n, i0, h;                        // sequence: first row, length; first token of the item, key head
-    int nt0, nt1;                              // tiles of keys that each row tile sees; both 0: no more items
 };
 
 template <int D> struct PaLayout {
@@ -213,67 +208,6 @@ __device__ __forceinline__ int pa_keys(const PromptAttnParams& p, int n, int i0,
 __device__ __forceinline__ bool pa_masked(int i0, int j) { return (j + 1) * kPaKeys > i0 + 1; }
 __device__ __forceinline__ int pa_first_masked(int i0) { return (i0 + 1) / kPaKeys; }
 
-// Items in the order of their numbers: 32 sequences at a time, and of these the items with the most keys first, whichever sequence
-// they are of, so that none of the long ones begins last (sequence after sequence: 4 prompts of 1000 to 4095, 157 us instead of 122); the key
-// heads of the same rows together.
-struct PaWalk {
-    int b0;                                    // 32 sequences, one a lane
-    long long before, tokens, items;           // items and tokens of the sequences before them; their own items
-    int row0, n, pairs;                        // this lane's
-};
-__device__ __forceinline__ void pa_walk_load(const PromptAttnParams& p, PaWalk& w) {
-    const int lane = threadIdx.x & 31, b = w.b0 + lane;
-    int c0 = 0, c1 = 0;
-    if (b < p.B) { c0 = __ldg(p.cu + b); c1 = __ldg(p.cu + b + 1); }
-    bool ok = c0 >= 0 && c1 >= c0 && c1 <= p.T;
-    const int n = ok ? c1 - c0 : 0;
-    long long sum = n;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const long long up = __shfl_up_sync(0xffffffffu, sum, o);
-        if (lane >= o) sum += up;
-    }
-    ok = ok && w.tokens + sum <= p.T;                         // sequences that overlap: more tokens than there are
-    if (!ok && b < p.B && p.status) atomicOr(p.status + b, BS_DEV_BAD_LENGTH);
-    w.row0 = c0;
-    w.n = ok ? n : 0;
-    w.pairs = (w.n + 2 * p.TQ - 1) / (2 * p.TQ);
-    w.tokens += __shfl_sync(0xffffffffu, sum, 31);
-    w.items = (long long)__reduce_add_sync(0xffffffffu, (unsigned)w.pairs) * p.Hkv;
-}
-__device__ __forceinline__ bool pa_walk_to(const PromptAttnParams& p, PaWalk& w, long long item, PaItem& it) {
-    if (item < w.before) {
-        w.b0 = 0; w.before = 0; w.tokens = 0;
-        pa_walk_load(p, w);
-    }
-    while (item >= w.before + w.items) {
-        if (w.b0 + 32 >= p.B) return false;
-        w.before += w.items;
-        w.b0 += 32;
-        pa_walk_load(p, w);
-    }
-    // pairs from the `level`-th on come first: the largest level at which there are enough of them
-    const long long t = item - w.before;
-    auto from = [&](int level) { return (long long)__reduce_add_sync(0xffffffffu, (unsigned)max(0, w.pairs - level)) * p.Hkv; };
-    int lo = 0, hi = (int)__reduce_max_sync(0xffffffffu, (unsigned)w.pairs);   // from(lo) > t >= from(hi)
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (from(mid) > t) lo = mid;
-        else hi = mid;
-    }
-    const int rank = (int)(t - from(hi));                     // among the items of this level
-    uint32_t who = __ballot_sync(0xffffffffu, w.pairs > lo);
-    for (int skip = rank / p.Hkv; skip > 0; --skip) who &= who - 1;
-    const int l = __ffs(who) - 1;
-    it.h = rank % p.Hkv;
-    it.i0 = lo * 2 * p.TQ;
-    it.row0 = __shfl_sync(0xffffffffu, w.row0, l);
-    it.n = __shfl_sync(0xffffffffu, w.n, l);
-    it.nt0 = (min(it.n, it.i0 + p.TQ) + kPaKeys - 1) / kPaKeys;
-    it.nt1 = it.i0 + p.TQ < it.n ? (min(it.n, it.i0 + 2 * p.TQ) + kPaKeys - 1) / kPaKeys : 0;
-    return true;
-}
-
 template <int D>
 __global__ void __launch_bounds__(kPaThreads, 1)
 prompt_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
@@ -374,8 +308,8 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
         for (uint32_t k = 0; ok; ++k) {                       // the k-th item of this CTA
             const uint32_t slot = k % kPaItems;
             PaItem it = {0, 0, 0, 0, 0, 0};
-            const bool there = more && pa_walk_to(p, w, item, it);
-            if (k >= kPaItems) ok = wait(&b_done[slot], (k / kPaItems - 1) & 1);
+            const bool there = pa_take(p, w, item, more, ok, it, next);
+            if (ok && k >= kPaItems) ok = wait(&b_done[slot], (k / kPaItems - 1) & 1);
             if (!ok) break;
             for (int i = lane; i < D; i += 32) s_first[slot][i] = 0x7fffffff;
             if (lane == 0) {
@@ -387,8 +321,6 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
             if (!there) break;
             next();
         }
-#pragma unroll 1
-        while (ok && more) next();                            // the grid has a few CTAs more than there are items
         if (!ok && lane == 0) s_abort = 1;
         const int zero = 0;                                   // whoever gave up: an answer on its way is waited for
         if (asked != answered) pa_wait(&b_next, answered & 1, &zero);

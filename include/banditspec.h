@@ -526,8 +526,8 @@ bs_status bs_rotary(const void* q, long long q_stride_t, long long q_stride_h, c
  *  cu_seqlens [B + 1]: sequence b is rows cu_seqlens[b] .. cu_seqlens[b + 1] - 1 (bs_cache_plan's cu_new, if all begin here).  Empty sequences
  *          are fine.  Rows of out behind cu_seqlens[B] are left as they are, what the other arrays hold there does not matter
  *  softmax_scale > 0, T <= 2^30
- *  status  [B] or NULL: bits are added.  BS_DEV_BAD_LENGTH: cu_seqlens not ascending, outside [0, T] or with more tokens than T, the
- *          sequence's rows are left as they are; BS_DEV_TIMEOUT in status[0]: a bounded wait gave up, every output is undefined
+ *  status  [B] or NULL: bits are added.  BS_DEV_BAD_LENGTH: a sequence outside [0, T], that ends before it begins, or that begins before
+ *          the end of an earlier one: it is left out, no row is written for it; BS_DEV_TIMEOUT in status[0]: a bounded wait gave up, every output is undefined
  *          (without a status array nothing tells)
  * Products accumulate in fp32, probabilities enter the second product as bf16.  Keys and values of later tokens may be NaN or
  * infinite without a trace; an element of v that is not finite makes that element of the rows that see it NaN or infinite.

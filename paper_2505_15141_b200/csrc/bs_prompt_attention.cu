@@ -273,7 +273,7 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
         // ================================= scheduler =================================
         pa_few_registers();
         const uint32_t elected = ca_elect();
-        PaWalk w = {0, 0, 0, 0, 0, 0, 0};
+        PaWalk w = {};
         pa_walk_load(p, w);
         long long item = blockIdx.x;
         bool more = true;

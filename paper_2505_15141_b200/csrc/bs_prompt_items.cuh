@@ -18,7 +18,8 @@ struct PaItem {
 // heads of the same rows together.
 struct PaWalk {
     int b0;                                    // 32 sequences, one a lane
-    long long before, tokens, items;           // items and tokens of the sequences before them; their own items
+    long long before, items;                   // items of the sequences before them; their own
+    int end;                                   // where the sequences up to the last of them end, at most
     int row0, n, pairs;                        // this lane's
 };
 template <class P>
@@ -27,25 +28,22 @@ __device__ __forceinline__ void pa_walk_load(const P& p, PaWalk& w) {
     int c0 = 0, c1 = 0;
     if (b < p.B) { c0 = __ldg(p.cu + b); c1 = __ldg(p.cu + b + 1); }
     bool ok = c0 >= 0 && c1 >= c0 && c1 <= p.T;
-    const int n = ok ? c1 - c0 : 0;
-    long long sum = n;
+    int end = max(w.end, ok ? c1 : 0);                        // of the sequences up to this lane's: a row is one sequence's only
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const long long up = __shfl_up_sync(0xffffffffu, sum, o);
-        if (lane >= o) sum += up;
-    }
-    ok = ok && w.tokens + sum <= p.T;                         // sequences that overlap: more tokens than there are
+    for (int o = 1; o < 32; o <<= 1) end = max(end, __shfl_up_sync(0xffffffffu, end, o));
+    const int earlier = __shfl_up_sync(0xffffffffu, end, 1);
+    ok = ok && c0 >= (lane ? earlier : w.end);
     if (!ok && b < p.B && p.status) atomicOr(p.status + b, BS_DEV_BAD_LENGTH);
     w.row0 = c0;
-    w.n = ok ? n : 0;
+    w.n = ok ? c1 - c0 : 0;
     w.pairs = (w.n + 2 * p.TQ - 1) / (2 * p.TQ);
-    w.tokens += __shfl_sync(0xffffffffu, sum, 31);
+    w.end = __shfl_sync(0xffffffffu, end, 31);
     w.items = (long long)__reduce_add_sync(0xffffffffu, (unsigned)w.pairs) * p.Hkv;
 }
 template <class P>
 __device__ __forceinline__ bool pa_walk_to(const P& p, PaWalk& w, long long item, PaItem& it) {
     if (item < w.before) {
-        w.b0 = 0; w.before = 0; w.tokens = 0;
+        w.b0 = 0; w.before = 0; w.end = 0;
         pa_walk_load(p, w);
     }
     while (item >= w.before + w.items) {

@@ -230,3 +230,13 @@ def test_reports_stay_within_the_batch(lib):
     lib.bs_prompt_attention(q, k, v, torch.tensor([0, 100, 60, 210], dtype=torch.int32, device=DEV), 0.125, out, around[8:11])
     assert around[8:11].tolist() == [0, lib.BS_DEV_BAD_LENGTH, lib.BS_DEV_BAD_LENGTH]
     assert not around[:8].any() and not around[11:].any()
+
+
+def test_rows_that_two_sequences_claim(lib):
+    """A sequence that begins before the end of an earlier one writes nothing, although there are tokens enough for both."""
+    q, k, v = _inputs([210], 2, 1, 64, seed=15)
+    want = torch.full(q.shape, 7.0, dtype=torch.bfloat16, device=DEV)
+    lib.bs_prompt_attention(q, k, v, torch.tensor([0, 100], dtype=torch.int32, device=DEV), 0.125, want)
+    out, status = torch.full(q.shape, 7.0, dtype=torch.bfloat16, device=DEV), torch.zeros(3, dtype=torch.int32, device=DEV)
+    lib.bs_prompt_attention(q, k, v, torch.tensor([0, 100, 60, 90], dtype=torch.int32, device=DEV), 0.125, out, status)
+    assert status.tolist() == [0, lib.BS_DEV_BAD_LENGTH, lib.BS_DEV_BAD_LENGTH] and torch.equal(out, want)

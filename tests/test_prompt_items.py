@@ -97,3 +97,25 @@ def test_bad_lengths_in_the_second_group(program):
         bad = [b for b in range(60) if status[b]]
         assert set(bad) >= {19, 20, 40, 59} and set(bad) <= {19, 20, 40, 41, 59} and set(status) <= {0, 64}
         assert sorted(i[1:] for i in items) == _want(cu, [b not in bad for b in range(60)], 2, 32)
+
+
+@pytest.mark.parametrize("cu", [[0, 100, 60, 90], [0, 100, 60, 90, 210], [50, 120, 10, 60, 130], [0, 200, 0, 200], [0, 80, 80, 20, 90, 90, 150],
+                                [0, 500, 100, 150], [100, 40, 60, 50, 70, 80]])
+@pytest.mark.parametrize("before", [0, 30, 31, 40])
+def test_a_row_belongs_to_one_sequence_at_most(program, cu, before):
+    """Lengths that go back: a sequence that begins before the end of an earlier one would write its rows again, in whatever order the
+    CTAs run.  It is reported, the earlier one is whole; also when the earlier one is among the 32 before."""
+    cu = [0] * before + cu
+    B, T = len(cu) - 1, 210
+    ends, good = 0, []
+    for lo, hi in zip(cu[:-1], cu[1:]):
+        sane = 0 <= lo <= hi <= T
+        good.append(sane and lo >= ends)
+        if sane:
+            ends = max(ends, hi)
+    for order in ("ascending", "any"):
+        items, status = _run(program, cu, T, 2, 16, ORDERS[order](_grid(T, B, 2, 16), np.random.default_rng(1)), 4)
+        assert status == [0 if g else 64 for g in good]
+        assert sorted(i[1:] for i in items) == _want(cu, good, 2, 16)
+    rows = [r for lo, hi, g in zip(cu[:-1], cu[1:], good) if g for r in range(lo, hi)]
+    assert len(rows) == len(set(rows))

@@ -240,3 +240,47 @@ def test_rows_that_two_sequences_claim(lib):
     out, status = torch.full(q.shape, 7.0, dtype=torch.bfloat16, device=DEV), torch.zeros(3, dtype=torch.int32, device=DEV)
     lib.bs_prompt_attention(q, k, v, torch.tensor([0, 100, 60, 90], dtype=torch.int32, device=DEV), 0.125, out, status)
     assert status.tolist() == [0, lib.BS_DEV_BAD_LENGTH, lib.BS_DEV_BAD_LENGTH] and torch.equal(out, want)
+
+
+def _ragged(B, most, seed):
+    rng = np.random.default_rng(seed)
+    n = rng.integers(0, most, B)
+    n[rng.random(B) < 0.15] = 0
+    n[-1] = most                                              # the last of them has the most items
+    return n.tolist()
+
+
+# items of a call against the SMs: 4 x 148 are 592
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("n,Hq,Hkv", [(_ragged(60, 700, 1), 21, 3), (_ragged(100, 300, 2), 15, 3), (_ragged(45, 600, 3), 16, 16), ([3000], 40, 40),
+                                      ([1200, 1], 128, 2), ([129] * 70, 8, 8), ([257, 1, 128] * 30, 12, 12)])
+def test_ctas_that_take_many_items(lib, n, Hq, Hkv, d):
+    """Three items and more a CTA: slots, barriers and rings are used again, over groups of 32 sequences and all lengths."""
+    TQ = 128 // (Hq // Hkv)
+    assert sum(-(-m // (2 * TQ)) for m in n) * Hkv > 3 * 148
+    q, k, v = _inputs(n, Hq, Hkv, d, seed=sum(n) + Hq)
+    out = torch.full(q.shape, 7.0, dtype=torch.bfloat16, device=DEV)
+    status = torch.zeros(len(n), dtype=torch.int32, device=DEV)
+    lib.bs_prompt_attention(q, k, v, _cu(n), d ** -0.5, out, status)
+    assert not status.any()
+    _check(out, q, k, v, n, d ** -0.5)
+    again = torch.full(q.shape, 7.0, dtype=torch.bfloat16, device=DEV)
+    lib.bs_prompt_attention(q, k, v, _cu(n), d ** -0.5, again)
+    assert torch.equal(out, again)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_bad_lengths_among_many_sequences(lib, d):
+    """One in the second group of 32: its rows stay, all others are as without it."""
+    n, Hq, Hkv = _ragged(60, 700, 4), 21, 3
+    q, k, v = _inputs(n, Hq, Hkv, d, seed=16)
+    cu, T = _cu(n), sum(n)
+    want = torch.full(q.shape, 7.0, dtype=torch.bfloat16, device=DEV)
+    lib.bs_prompt_attention(q, k, v, cu, d ** -0.5, want)
+    cu[41] = T + 5                                            # 40 ends behind the tokens, 41 descends
+    out, status = torch.full(q.shape, 7.0, dtype=torch.bfloat16, device=DEV), torch.zeros(60, dtype=torch.int32, device=DEV)
+    lib.bs_prompt_attention(q, k, v, cu, d ** -0.5, out, status)
+    assert [b for b in range(60) if status[b]] == [40, 41]
+    lo, hi = sum(n[:40]), sum(n[:42])
+    assert hi > lo and (out[lo:hi] == 7.0).all()
+    assert torch.equal(out[:lo], want[:lo]) and torch.equal(out[hi:], want[hi:])

@@ -1,4 +1,4 @@
-// The items of bs_prompt_attention and how a CTA takes them.  Nothing here is of the GPU but the operations of a warp: a test that
+// The items of bs_prompt_attention, how a CTA takes them and how long its warps wait.  Nothing here is of the GPU but the operations of a warp: a test that
 // stands in for these runs it on the host, with numbers in orders that a GPU does not give on demand.
 #pragma once
 
@@ -73,6 +73,20 @@ __device__ __forceinline__ bool pa_walk_to(const P& p, PaWalk& w, long long item
     it.nt1 = it.i0 + p.TQ < it.n ? (min(it.n, it.i0 + 2 * p.TQ) + kPaKeys - 1) / kPaKeys : 0;
     return true;
 }
+
+// Limit of a wait that may last as long as an item, which has no bound: over when `limit` cycles have passed without a step of the CTA.
+struct PaPatience {
+    long long since;
+    int seen;                                  // steps at that time
+    __device__ __forceinline__ bool over(long long now, long long limit, const volatile int& steps) {
+        if (now - since <= limit) return false;
+        const int at = steps;
+        if (at == seen) return true;
+        seen = at;
+        since = now;
+        return false;
+    }
+};
 
 // The next item of a CTA.  `item` is the number of a CTA that will not run, or has just begun, `next` asks the launch control for
 // another and clears `more` if there is none, `ok` if it gave up.  The grid has a few more CTAs than there are items, and nothing

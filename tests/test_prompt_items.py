@@ -1,6 +1,7 @@
 """How the CTAs of bs_prompt_attention take their items: the kernel's own header, run on the host with CTA numbers in orders that a GPU
 does not give on demand (no GPU needed)."""
 import os
+import re
 import subprocess
 
 import numpy as np
@@ -119,3 +120,26 @@ def test_a_row_belongs_to_one_sequence_at_most(program, cu, before):
         assert sorted(i[1:] for i in items) == _want(cu, good, 2, 16)
     rows = [r for lo, hi, g in zip(cu[:-1], cu[1:], good) if g for r in range(lo, hi)]
     assert len(rows) == len(set(rows))
+
+
+@pytest.mark.parametrize("last", [0, 1, 635000, 2 ** 23])
+@pytest.mark.parametrize("every", [1000, 1900000])
+def test_a_wait_lasts_while_the_products_step(program, every, last):
+    """A wait for a whole item is as long as the item, 2^23 tiles of 3150 cycles in the longest; it ends a limit, and what a poll takes, after
+    the last step, which it may have seen a limit late."""
+    limit, step = 2000000000, 3150
+    if every == 1000 and last == 2 ** 23:
+        every = 10000
+    out = subprocess.run([program, "wait"], input=f"{limit} {every} {step} {last}", capture_output=True, text=True, check=True, timeout=120).stdout
+    assert last * step + (limit if last == 0 else 0) <= int(out) <= last * step + 2 * (limit + every)
+
+
+def test_the_waits_of_the_kernel_that_may_last_an_item():
+    """The scheduler's for an item's place, the V warp's for what is seen in part, the softmax warps' whose row tile an item lacks: they
+    would come to the next item an item too early.  The copies, which run as long as an item does, tell the steps."""
+    src = open(os.path.join(ROOT, "paper_2505_15141_b200", "csrc", "bs_prompt_attention.cu")).read()
+    assert re.findall(r"wait_item\(&(b_\w+)", src) == ["b_done", "b_done", "b_part"]
+    assert not re.search(r"\bwait\(&(b_done|b_part)\b", src)
+    softmax = src[src.index("softmax ==="):src.index("V, seen in part ===")]
+    assert softmax.index("mbar_arrive(smem_u32(&b_done[slot]))") < softmax.index("if (nt == 0) ok = wait_item(&b_done[slot], (k / kPaItems) & 1);")
+    assert src.count("s_state.steps = (int)count;") == 1

@@ -53,7 +53,8 @@ typedef enum {
     BS_ERR_CUDA = 2,          /* a CUDA runtime call or launch failed */
     BS_ERR_UNSUPPORTED = 3,   /* valid request outside the implemented limits */
     BS_ERR_WORKSPACE = 4,     /* workspace too small or misaligned */
-    BS_ERR_TIMEOUT = 5,       /* bs_get_device_status, bs_cache_get_device_status: a bounded wait inside a kernel gave up */
+    BS_ERR_TIMEOUT = 5,       /* bs_get_device_status, bs_cache_get_device_status, bs_prompt_get_device_status: a bounded wait
+                                 inside a kernel gave up */
     BS_ERR_DEVICE_DATA = 6    /* bs_get_device_status: some sequence carries a data error */
 } bs_status;
 
@@ -77,7 +78,8 @@ typedef enum { BS_UCB = 0, BS_EXP3 = 1, BS_UCB_REWARD = 2 } bs_alg;
 #define BS_DEV_BAD_BLOCK     512   /* bs_cache_attention / bs_cache_keep_path: a block id outside [0, n_blocks) */
 #define BS_DEV_TIMEOUT       1024  /* bs_cache_attention: a bounded wait gave up; every output of the call is undefined and
                                       its workspace has to be cleared with bs_workspace_init.  Set in status[0]; without
-                                      a status array bs_cache_get_device_status still tells */
+                                      a status array bs_cache_get_device_status still tells.  bs_prompt_attention: the
+                                      same, without a workspace; bs_prompt_get_device_status still tells */
 
 #define BS_DEV_BAD_MASK      2048  /* bs_logits_adjust: a mask number outside [-1, n_masks); the row got no mask */
 
@@ -528,7 +530,7 @@ bs_status bs_rotary(const void* q, long long q_stride_t, long long q_stride_h, c
  *  softmax_scale > 0, T <= 2^30
  *  status  [B] or NULL: bits are added.  BS_DEV_BAD_LENGTH: a sequence outside [0, T], that ends before it begins, or that begins before
  *          the end of an earlier one: it is left out, no row is written for it; BS_DEV_TIMEOUT in status[0]: a bounded wait gave up, every output is undefined
- *          (without a status array nothing tells)
+ *          (without a status array bs_prompt_get_device_status tells)
  * Products accumulate in fp32, probabilities enter the second product as bf16.  Keys and values of later tokens may be NaN or
  * infinite without a trace; an element of v that is not finite makes that element of the rows that see it NaN or infinite.
  * Results do not depend on the order in which CTAs run. */
@@ -536,6 +538,10 @@ bs_status bs_prompt_attention(const void* q, long long q_stride_t, long long q_s
                               long long k_stride_h, const void* v, long long v_stride_t, long long v_stride_h,
                               const int32_t* cu_seqlens, int B, int T, int Hq, int Hkv, int d, float softmax_scale, void* out,
                               long long out_stride_t, long long out_stride_h, int32_t* status, void* stream);
+
+/* Whether a bounded wait gave up in any bs_prompt_attention on the current device that had ended by now since the last such
+ * answer: BS_ERR_TIMEOUT (once), else BS_OK.  Synchronises `stream`; calls on other streams are not waited for. */
+bs_status bs_prompt_get_device_status(void* stream);
 
 /* ---- what is done to logits before they are verified ---------------------------------------------
  *

@@ -67,6 +67,7 @@ SIGNATURES = {
     "bs_rotary": (_i, [_vp, _ll, _ll, _vp, _ll, _ll, _i, _vp, _vp, _f, _i, _i, _vp, _vp, _i, _i, _i, _i, _i, _i, _vp, _ll, _ll, _vp, _ll,
                        _ll, _vp]),
     "bs_prompt_attention": (_i, [_vp, _ll, _ll, _vp, _ll, _ll, _vp, _ll, _ll, _vp, _i, _i, _i, _i, _i, _f, _vp, _ll, _ll, _vp, _vp]),
+    "bs_prompt_get_device_status": (_i, [_vp]),
     "bs_history_update": (_i, [_vp, _i, _i, _vp, _vp, _vp, _i, _vp, _vp, _i, _vp, _vp]),
     "bs_logits_adjust": (_i, [_vp, _vp, _i, _vp, _i, _i, _i, _vp, _vp, _i, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i, _vp, _i, _vp, _i, _i, _i,
                               _vp, _vp]),
@@ -550,6 +551,14 @@ def bs_prompt_attention(q, k, v, cu_seqlens, softmax_scale: float, out, status=N
     op, ot, oh, _ = _heads(out, index)
     _call(_lib.bs_prompt_attention, "bs_prompt_attention", index, stream, qp, qt, qh, kp, kt, kh, vp, vt, vh, _i32(cu_seqlens, B + 1, index),
           B, T, Hq, Hkv, d, softmax_scale, op, ot, oh, _i32(status, B, index))
+
+
+def bs_prompt_get_device_status(device="cuda", stream=None) -> None:
+    """Raises BanditSpecError (BS_ERR_TIMEOUT) if a bounded wait gave up in a bs_prompt_attention on that GPU since the last such answer
+    (synchronises the stream)."""
+    device = torch.device(device)
+    index = torch.cuda.current_device() if device.index is None else device.index
+    _call(_lib.bs_prompt_get_device_status, "bs_prompt_get_device_status", index, stream)
 
 
 # ---- logits before the verification ------------------------------------------------------------

@@ -227,6 +227,9 @@ __device__ __forceinline__ int pa_keys(const PromptAttnParams& p, int n, int i0,
 __device__ __forceinline__ bool pa_masked(int i0, int j) { return (j + 1) * kPaKeys > i0 + 1; }
 __device__ __forceinline__ int pa_first_masked(int i0) { return (i0 + 1) / kPaKeys; }
 
+// Set where a wait gave up, for calls without a status array, too; there is no workspace that could hold it.
+__device__ uint32_t g_pa_gave_up;
+
 template <int D>
 __global__ void __launch_bounds__(kPaThreads, 1)
 prompt_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
@@ -727,7 +730,10 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
             for (int i = 0; i < 2; ++i)
                 if (s_qcopies[i]) pa_wait<true>(&b_qfull[i], (s_qcopies[i] - 1) & 1, s_state);
         }
-        if (tid == 0 && p.status) atomicOr(p.status, BS_DEV_TIMEOUT);
+        if (tid == 0) {
+            g_pa_gave_up = 1u;
+            if (p.status) atomicOr(p.status, BS_DEV_TIMEOUT);
+        }
         __syncthreads();
     }
     if (warp == 8) {
@@ -767,6 +773,21 @@ static bs_status launch_pa(const CUtensorMap* tm, const PromptAttnParams& p, lon
 }  // namespace bs
 
 using namespace bs;
+
+extern "C" bs_status bs_prompt_get_device_status(void* stream) {
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    void* at = nullptr;
+    uint32_t gave_up = 0;
+    cudaError_t e = cudaGetSymbolAddress(&at, g_pa_gave_up);
+    if (e == cudaSuccess) e = cudaMemcpyAsync(&gave_up, at, sizeof(gave_up), cudaMemcpyDeviceToHost, st);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(st);
+    if (e == cudaSuccess && gave_up) {
+        e = cudaMemsetAsync(at, 0, sizeof(gave_up), st);
+        if (e == cudaSuccess) e = cudaStreamSynchronize(st);
+    }
+    if (e != cudaSuccess) return cuda_status(e);
+    return gave_up ? BS_ERR_TIMEOUT : BS_OK;
+}
 
 extern "C" bs_status bs_prompt_attention(const void* q, long long q_stride_t, long long q_stride_h, const void* k, long long k_stride_t,
                                          long long k_stride_h, const void* v, long long v_stride_t, long long v_stride_h,

@@ -284,3 +284,13 @@ def test_bad_lengths_among_many_sequences(lib, d):
     lo, hi = sum(n[:40]), sum(n[:42])
     assert hi > lo and (out[lo:hi] == 7.0).all()
     assert torch.equal(out[:lo], want[:lo]) and torch.equal(out[hi:], want[hi:])
+
+
+def test_no_time_out_without_a_status_array(lib):
+    q, k, v = _inputs([210], 2, 1, 64, seed=17)
+    out = torch.zeros(q.shape, dtype=torch.bfloat16, device=DEV)
+    lib.bs_prompt_attention(q, k, v, _cu([210]), 0.125, out)
+    lib.bs_prompt_get_device_status()
+    side = torch.cuda.Stream()
+    lib.bs_prompt_attention(q, k, v, _cu([210]), 0.125, out, stream=side)
+    lib.bs_prompt_get_device_status(q.device, side)

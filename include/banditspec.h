@@ -496,7 +496,8 @@ typedef enum {
                                  amplitude is 0.1 ln(factor) + 1 */
 } bs_rotary_scaling;
 
-/* Frequencies for bs_rotary, computed on the HOST in fp64: freq_host [rot / 2] turns a position x 2^64, and the amplitude.  rot
+/* Frequencies for bs_rotary, computed on the HOST with 64 bits of mantissa: freq_host [rot / 2] turns a position x 2^64, off by
+ * at most 2.3, and the amplitude.  rot
  * even, 2 to 256; base > 1; factor >= 1, 0 < low < high and original >= 1 where the scaling uses them. */
 bs_status bs_rotary_frequencies(bs_rotary_scaling scaling, int rot, double base, double factor, double low, double high,
                                 double original, uint64_t* freq_host, float* amplitude_host);
@@ -512,7 +513,8 @@ bs_status bs_rotary_frequencies(bs_rotary_scaling scaling, int rot, double base,
  *  node_parent NULL: chains.  [B, Nmax]: trees as in bs_cache_attention, cu_new [B + 1] the plan's: row n of a sequence is rotated
  *            to position(row 0) + depth of node n, where bs_cache_keep_path will leave it if it is accepted.  A
  *            parent that is not an earlier node counts as the root; rows behind Nmax + 1 are left as they are
- * Angles are exact to 2^-32 turns at every position; sines, cosines and products are fp32, results are rounded once.
+ * Angles are exact to 2^-31 turns at every position, then rounded to fp32 within the turn (2^-26 turns at most); sines, cosines and
+ * products are fp32, results are rounded once.
  * Any strides work; those that are multiples of 16 bytes (and pointers) take the widest accesses. */
 bs_status bs_rotary(const void* q, long long q_stride_t, long long q_stride_h, const void* k, long long k_stride_t,
                     long long k_stride_h, bs_dtype dtype, const int32_t* positions, const uint64_t* freq, float amplitude, int rot,

@@ -2,8 +2,9 @@
 //
 //   (a, b) -> (a cos w - b sin w, b cos w + a sin w),   w = position * frequency of the pair
 //
-// A frequency is held in turns as a 64-bit binary fraction, so the angle modulo one turn is the low half of an integer
-// product: exact at every position, where the product in fp32 is off by 0.01 radians at position 100000.
+// A frequency is held in turns as a 64-bit binary fraction, off by two steps of it at most, so the angle modulo one turn is the low
+// half of an integer product and off by 2^-31 turns at the farthest position, where the product in fp32 is off by 0.01 radians at
+// position 100000.  Its fp32 value, at most half a turn, is rounded by 2^-26 turns at most.
 //
 // Bound by HBM: every element is read and written once.  A warp takes a token, or a part of its heads where there are few tokens: it
 // computes the token's sines and cosines (a lane those of every 32nd pair) into shared memory and sweeps over heads x chunks of
@@ -139,7 +140,7 @@ __global__ void __launch_bounds__(kRoWarps * 32) rotary_kernel(const RotaryParam
     for (int j = lane; j < half; j += 32) {
         const int64_t turns = (int64_t)((uint64_t)(uint32_t)pos * __ldg(p.freq + j));   // of a turn, in [-1/2, 1/2) x 2^64
         float s, c;
-        sincospif((float)turns * 1.0842021724855044e-19f, &s, &c);                      // 2^-63: half turns
+        sincospif((float)turns * 1.0842021724855044e-19f, &s, &c);                      // 2^-63: half turns; rounded to 2^-24 of the angle
         const int at = (j % P) * n_rot + j / P;               // the chunks of a warp's lanes lie side by side
         cos_of[at] = c * p.amplitude;
         sin_of[at] = s * p.amplitude;
@@ -214,18 +215,21 @@ extern "C" bs_status bs_rotary_frequencies(bs_rotary_scaling scaling, int rot, d
         first = fmax(floor(rot * log(original / (high * two_pi)) / (2 * log(base))), 0.0);
         last = fmin(ceil(rot * log(original / (low * two_pi)) / (2 * log(base))), rot - 1.0);
     }
+    // 64 bits of mantissa: a frequency's error is multiplied by the position, 2^31 at most.
+    typedef long double wide;
+    const wide turn = 8 * atanl((wide)1);
     for (int i = 0; i < rot / 2; ++i) {
-        double f = pow(base, -2.0 * i / rot);
+        wide f = powl((wide)base, (wide)(-2 * i) / rot);
         if (scaling == BS_ROTARY_LINEAR) f /= factor;
         if (scaling == BS_ROTARY_BANDS) {
-            const double keep = fmin(fmax((original * f / two_pi - low) / (high - low), 0.0), 1.0);
-            f *= keep + (1.0 - keep) / factor;
+            const wide keep = fminl(fmaxl((original * f / turn - low) / ((wide)high - low), (wide)0), (wide)1);
+            f *= keep + (1 - keep) / factor;
         }
         if (scaling == BS_ROTARY_YARN) {
-            const double ramp = fmin(fmax((i - first) / fmax(last - first, 0.001), 0.0), 1.0);
-            f *= 1.0 - ramp + ramp / factor;
+            const wide ramp = fminl(fmaxl((i - first) / fmaxl(last - first, (wide)1 / 1000), (wide)0), (wide)1);
+            f *= 1 - ramp + ramp / factor;
         }
-        freq_host[i] = (uint64_t)(f / two_pi * 18446744073709551616.0 + 0.5);    // f <= 1
+        freq_host[i] = (uint64_t)(ldexpl(f / turn, 64) + (wide)1 / 2);           // f <= 1
     }
     *amplitude_host = scaling == BS_ROTARY_YARN ? (float)(0.1 * log(factor) + 1.0) : 1.0f;
     return BS_OK;

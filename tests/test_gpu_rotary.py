@@ -147,3 +147,20 @@ def test_special_values_and_streams(lib):
     lib.bs_rotary(q, None, pos, table, False, out, None)
     torch.cuda.synchronize()
     assert torch.equal(out.view(torch.int16), other.view(torch.int16))
+
+
+@pytest.mark.parametrize("scaling,kw", [("none", {}), ("linear", {"factor": 3.0}), ("bands", {"factor": 8.0, "low": 1.0, "high": 4.0, "original": 8192})])
+def test_angles_at_the_farthest_positions(lib, scaling, kw):
+    """Pairs (1, 0) become cosine and sine.  The angle is off by 2^-31 turns and rounded by 2^-26: 1.62 x 2^-24 radians; the functions are
+    off by two units of 2^-24 at most, the result by half of one."""
+    from test_rotary_frequencies import exact_turns
+    from decimal import Decimal
+    pos = [2 ** 24 + 1, 2 ** 27 - 3, 2 ** 30 + 7, 2 ** 31 - 2, 2 ** 31 - 1]
+    q = torch.zeros(len(pos), 1, 128, device=DEV)
+    q[..., :64] = 1.0
+    out = torch.empty_like(q)
+    lib.bs_rotary(q, None, _ints(pos), lib.new_rotary_table(128, 10000.0, scaling, **kw), False, out, None)
+    turns = np.array([[float((f * p) % Decimal(1)) for f in exact_turns(128, 10000.0, scaling, **kw)] for p in pos])
+    want = np.concatenate([np.cos(2 * np.pi * turns), np.sin(2 * np.pi * turns)], 1)
+    err = np.abs(out[:, 0].double().cpu().numpy() - want)
+    assert err.max() <= 4.2 * 2.0 ** -24, err.max() * 2 ** 24

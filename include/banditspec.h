@@ -506,7 +506,7 @@ bs_status bs_rotary_frequencies(bs_rotary_scaling scaling, int rot, double base,
  * w = position x frequency.
  *
  *  q, q_out  [T, Hq, d], k, k_out [T, Hkv, d] dtype, d contiguous; strides of a token and a head in elements.  q_out may be q and
- *            k_out may be k (same strides); other overlaps are not supported.  Hq or Hkv may be 0 (pointers NULL)
+ *            k_out may be k (same strides); no other overlap of an output.  Hq or Hkv may be 0 (pointers NULL)
  *  positions [T] as bs_cache_plan gives them; rows with a negative one are left as they are (in q_out and k_out, too)
  *  freq      [rot / 2] DEVICE copy of what bs_rotary_frequencies made; rot <= d, elements from rot on are copied
  *  interleaved 0: pair i is elements i and i + rot / 2;  else: elements 2 i and 2 i + 1
@@ -526,7 +526,8 @@ bs_status bs_rotary(const void* q, long long q_stride_t, long long q_stride_h, c
  * sequence.
  *
  *  q, out  [T, Hq, d], k, v [T, Hkv, d] bf16, d (64 or 128) contiguous; strides of a token and a head in elements, multiples of 8 and
- *          not negative, 16-byte aligned.  Query head i reads key head i / (Hq / Hkv); Hq / Hkv <= 64.  out overlaps no input
+ *          not negative, 16-byte aligned.  Query head i reads key head i / (Hq / Hkv); Hq / Hkv <= 64.  out overlaps no
+ *          input (views of one buffer may lie between one another)
  *  cu_seqlens [B + 1]: sequence b is rows cu_seqlens[b] .. cu_seqlens[b + 1] - 1 (bs_cache_plan's cu_new, if all begin here).  Empty sequences
  *          are fine.  Rows of out behind cu_seqlens[B] are left as they are, what the other arrays hold there does not matter
  *  softmax_scale > 0, T <= 2^30
@@ -570,7 +571,7 @@ bs_status bs_history_update(int16_t* history, int B, int V, const uint8_t* fresh
  *   forbidden by the row's mask:  x = -inf
  *
  *  logits, out  [B, R, V] dtype, R <= BS_MAX_GAMMA + 1: target rows (R = Gmax + 1, extra = 1) or draft rows (R = Gmax, extra = 0).  out may
- *               be logits (only what changes is then written); other overlaps are not supported
+ *               be logits (only what changes is then written), or lies apart from them
  *  gamma        [B] or NULL (all R rows): rows row_begin <= j < min(row_end, gamma_b + extra) are adjusted, the others are neither
  *               read nor written
  *  draft_tokens [B, Nmax] or NULL, Nmax >= R - 1: row j stands behind tokens 0 .. j - 1 of a chain, or with node_parent [B, Nmax]

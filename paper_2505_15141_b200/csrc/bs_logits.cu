@@ -17,6 +17,7 @@
 // shared memory piece by piece and written once; what a round adds goes to its few entries by compare-and-swap.  Only whole
 // numbers are added: the order does not show.
 #include "bs_common.cuh"
+#include "bs_overlap.cuh"
 
 namespace bs {
 
@@ -611,6 +612,9 @@ extern "C" bs_status bs_logits_adjust(const void* logits, void* out, bs_dtype dt
     if ((repetition || presence || frequency) && !history && !draft_tokens) return BS_ERR_INVALID_ARG;
     if (bias_begin && n_bias > 0 && (!bias_tokens || !bias_values)) return BS_ERR_INVALID_ARG;
     if (mask_row && n_masks > 0 && !masks) return BS_ERR_INVALID_ARG;
+    const long long es = dtype == BS_F32 ? 4 : 2;
+    if (logits != out && rows_overlap(rows_of(logits, 0, V, 1, (long long)B * R, V, es), rows_of(out, 0, V, 1, (long long)B * R, V, es)))
+        return BS_ERR_INVALID_ARG;
     AdjustParams p = {logits, out, gamma, draft_tokens, node_parent, history, repetition, presence, frequency, bias_begin,
                       bias_tokens, bias_values, masks, mask_row, status, extra, row_begin, row_end, B, R, Nmax, V, n_masks, n_bias,
                       logits == out};

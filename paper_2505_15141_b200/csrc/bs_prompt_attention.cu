@@ -31,6 +31,7 @@
 // and V: copies and products alone take as long as here (1.66 and 0.41 ms), so that neither shared memory nor the copies set
 // the pace, and with the softmax, whose P then waits for eight warps of two SMs, it is 24 % slower (2.47 and 0.60 ms).
 #include "bs_cache_attention.cuh"
+#include "bs_overlap.cuh"
 #include "bs_prompt_items.cuh"
 
 namespace bs {
@@ -813,6 +814,11 @@ extern "C" bs_status bs_prompt_attention(const void* q, long long q_stride_t, lo
     const long long grid = ((long long)T / (2 * p.TQ) + B) * Hkv;
     // tokens are counted in 32 bits, up to a few tiles behind the last
     if (T > (1 << 30) || grid > 0x7fffffffLL) return BS_ERR_UNSUPPORTED;
+    // CTAs write results while others still read
+    const Rows to = rows_of(out, out_stride_t, out_stride_h, T, Hq, d, 2);
+    if (rows_overlap(to, rows_of(q, q_stride_t, q_stride_h, T, Hq, d, 2)) || rows_overlap(to, rows_of(k, k_stride_t, k_stride_h, T, Hkv, d, 2)) ||
+        rows_overlap(to, rows_of(v, v_stride_t, v_stride_h, T, Hkv, d, 2)))
+        return BS_ERR_INVALID_ARG;
     if (!encode_tiled_fn()) return BS_ERR_CUDA;
     CUtensorMap tm[3];
     if (!pa_map(&tm[0], q, T, Hq, d, q_stride_t, q_stride_h, p.G, p.TQ) || !pa_map(&tm[1], k, T, Hkv, d, k_stride_t, k_stride_h, 1, kPaKeys) ||

@@ -11,6 +11,7 @@
 // pairs, so that they are computed once for many heads.  Warps do not wait for one another; the first chunks are on their way
 // while a warp looks for the position (trees: a search for the sequence, a walk to the root).
 #include "bs_common.cuh"
+#include "bs_overlap.cuh"
 
 namespace bs {
 
@@ -248,6 +249,13 @@ extern "C" bs_status bs_rotary(const void* q, long long q_stride_t, long long q_
     if (rot < 2 || rot > d || (rot & 1) || (d & 1) || rot > kRoMaxRot || Hq > 4096 || Hkv > 4096 || d > 4096) return BS_ERR_UNSUPPORTED;
     if (!isfinite(amplitude)) return BS_ERR_INVALID_ARG;
     if (T == 0) return BS_OK;
+    // in place, or apart
+    const int es = dtype == BS_F32 ? 4 : 2;
+    const Rows from[2] = {rows_of(q, q_stride_t, q_stride_h, T, Hq, d, es), rows_of(k, k_stride_t, k_stride_h, T, Hkv, d, es)};
+    const Rows to[2] = {rows_of(q_out, qo_stride_t, qo_stride_h, T, Hq, d, es), rows_of(k_out, ko_stride_t, ko_stride_h, T, Hkv, d, es)};
+    for (int i = 0; i < 2; ++i)
+        if ((!same_rows(from[i], to[i]) && rows_overlap(from[i], to[i])) || rows_overlap(from[i], to[1 - i])) return BS_ERR_INVALID_ARG;
+    if (rows_overlap(to[0], to[1])) return BS_ERR_INVALID_ARG;
     RotaryParams p = {};
     p.q = q; p.k = k; p.q_out = q_out; p.k_out = k_out;
     p.q_st = q_stride_t; p.q_sh = q_stride_h; p.k_st = k_stride_t; p.k_sh = k_stride_h;
@@ -255,11 +263,8 @@ extern "C" bs_status bs_rotary(const void* q, long long q_stride_t, long long q_
     p.positions = positions; p.freq = freq; p.cu_new = cu_new; p.node_parent = node_parent;
     p.amplitude = amplitude;
     p.rot = rot; p.T = T; p.Hq = Hq; p.H = Hq + Hkv; p.d = d; p.B = B; p.Nmax = Nmax;
-    const bool q_moves = Hq && (q != q_out || q_stride_t != qo_stride_t || q_stride_h != qo_stride_h);
-    const bool k_moves = Hkv && (k != k_out || k_stride_t != ko_stride_t || k_stride_h != ko_stride_h);
-    const bool copies = rot < d && (q_moves || k_moves);
+    const bool copies = rot < d && ((Hq && !same_rows(from[0], to[0])) || (Hkv && !same_rows(from[1], to[1])));
     // the widest vector that divides both parts of a head and that every row starts on
-    const int es = dtype == BS_F32 ? 4 : 2;
     auto fits = [&](int P) {
         auto ok = [&](const void* x, long long st, long long sh) {
             return reinterpret_cast<uintptr_t>(x) % (uintptr_t)(P * es) == 0 && st % P == 0 && sh % P == 0;

@@ -149,13 +149,13 @@ __device__ __forceinline__ bool ad_biases(const AdjustParams& p, int lo, int hi,
     const int lane = threadIdx.x & 31;
     bool found = false;
 #pragma unroll 1
-    for (int i = lo + lane; i - lane < hi; i += 128) {
+    for (uint32_t i = lo + lane; i - lane < (uint32_t)hi; i += 128) {   // behind the last entry 31 bits do not hold it
         int t[4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) t[k] = i + 32 * k < hi ? __ldg(p.bias_tokens + i + 32 * k) : p.V;
+        for (int k = 0; k < 4; ++k) t[k] = i + 32 * k < (uint32_t)hi ? __ldg(p.bias_tokens + i + 32 * k) : p.V;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            if (i + 32 * k < hi && (t[k] < 0 || t[k] >= p.V)) bits |= BS_DEV_BAD_TOKEN;
+            if (i + 32 * k < (uint32_t)hi && (t[k] < 0 || t[k] >= p.V)) bits |= BS_DEV_BAD_TOKEN;
             const int off = t[k] - v0;
             const bool hit = off >= 0 && off < kAdWarp && t[k] < p.V;
             if (!__any_sync(0xffffffffu, hit)) continue;

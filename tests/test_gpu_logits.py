@@ -333,3 +333,24 @@ def test_a_row_has_its_bits_whatever_else_is_drafted(lib, V, dtype, tree):
                 lib.bs_logits_adjust(out if in_place else x, out, _ints([row] * B), 1, rows=(row if only else 0, R), draft_tokens=_ints(other), **rules)
                 differ = out[:, row].view(bits) != base[:, row].view(bits)
                 assert not differ.any(), (row, in_place, only, int(differ.sum()))
+
+
+def test_lists_at_the_far_end_of_their_arrays(lib):
+    """Entries 2^31 - 12 to 2^31 - 2 of the biases, the last that 32 bits can number; the tokens of a prompt there."""
+    n, far, V = 2 ** 31 - 1, 10, 300
+    whole = torch.empty(n + 64, dtype=torch.int32, device=DEV)    # both arrays in one: their last entries lie apart
+    tokens, values = whole[:n], whole[64:].view(torch.float32)
+    at = [3, 299, 7, 3, 0, 255, 256, 3, 11, 12]
+    tokens[-far:] = _ints(at)
+    values[-far:] = torch.arange(1, far + 1, device=DEV)
+    x = torch.zeros(2, 2, V, device=DEV)
+    out = torch.full_like(x, 9.0)
+    status = torch.zeros(2, dtype=torch.int32, device=DEV)
+    lib.bs_logits_adjust(x, out, None, 0, bias_begin=_ints([n - far, n - 4, n]), bias_tokens=tokens, bias_values=values, status=status)
+    want = torch.zeros(2, 2, V)
+    for i, t in enumerate(at):
+        want[0 if i < far - 4 else 1, :, t] += i + 1.0
+    assert torch.equal(out.cpu(), want) and not status.any()
+    hist = lib.new_history(2, V)
+    lib.bs_history_update(hist, cu_prompt=_ints([n - far, n - 4, n]), prompt_tokens=tokens, status=status)
+    assert np.array_equal(hist.cpu().numpy(), ol.enter(np.zeros((2, V)), prompts=[at[:-4], at[-4:]])) and not status.any()

@@ -501,7 +501,7 @@ template <int THREADS>
 __device__ __forceinline__ void history_scatter(const HistoryParams& p, int b, int t, int c0, int n, int m, bool ok) {
     int16_t* row = p.history + (size_t)b * p.V;
     bool bad = false;
-    for (int i = t; i < n; i += THREADS) {
+    for (uint32_t i = t; i < (uint32_t)n; i += THREADS) {     // behind the last token 31 bits do not hold it
         const int tok = __ldg(p.prompt + c0 + i);
         if (tok < 0 || tok >= p.V) bad = true;
         else history_add(row, tok, true);
@@ -541,7 +541,7 @@ __global__ void __launch_bounds__(kHiThreads) history_prompts_kernel(const Histo
     for (int i = tid; i < kHiPiece / 2 + 4; i += kHiThreads) s_words[i] = 0u;
     __syncthreads();
     bool bad = false;
-    for (int i = tid; i < n; i += kHiThreads) {
+    for (uint32_t i = tid; i < (uint32_t)n; i += kHiThreads) {
         const int t = __ldg(p.prompt + c0 + i), at = t - v0 + shift;
         if (t < 0 || t >= p.V) bad = true;
         else if (t >= v0 && t < v0 + nv) atomicOr(s_words + (at >> 1), 1u << (16 * (at & 1)));

@@ -354,3 +354,15 @@ def test_lists_at_the_far_end_of_their_arrays(lib):
     hist = lib.new_history(2, V)
     lib.bs_history_update(hist, cu_prompt=_ints([n - far, n - 4, n]), prompt_tokens=tokens, status=status)
     assert np.array_equal(hist.cpu().numpy(), ol.enter(np.zeros((2, V)), prompts=[at[:-4], at[-4:]])) and not status.any()
+
+
+def test_a_prompt_as_long_as_its_array_can_be(lib):
+    """2^31 - 1 tokens of one sequence, all entered, the last ones among them; in a history that begins anew."""
+    n, V = 2 ** 31 - 1, 64
+    tokens = torch.zeros(n, dtype=torch.int32, device=DEV)
+    tokens[-3:] = _ints([5, 63, 64])
+    hist, status = lib.new_history(1, V), torch.zeros(1, dtype=torch.int32, device=DEV)
+    lib.bs_history_update(hist, torch.ones(1, dtype=torch.uint8, device=DEV), _ints([0, n]), tokens, status=status)
+    want = np.zeros((1, V))
+    want[0, [0, 5, 63]] = 1
+    assert np.array_equal(hist.cpu().numpy(), want) and status.tolist() == [lib.BS_DEV_BAD_TOKEN]

@@ -530,7 +530,7 @@ bs_status bs_rotary(const void* q, long long q_stride_t, long long q_stride_h, c
  *          input (views of one buffer may lie between one another)
  *  cu_seqlens [B + 1]: sequence b is rows cu_seqlens[b] .. cu_seqlens[b + 1] - 1 (bs_cache_plan's cu_new, if all begin here).  Empty sequences
  *          are fine.  Rows of out behind cu_seqlens[B] are left as they are, what the other arrays hold there does not matter
- *  softmax_scale > 0, T <= 2^30
+ *  softmax_scale > 0 and, times log2(e), finite; T <= 2^30
  *  status  [B] or NULL: bits are added.  BS_DEV_BAD_LENGTH: a sequence outside [0, T], that ends before it begins, or that begins before
  *          the end of an earlier one: it is left out, no row is written for it; BS_DEV_TIMEOUT in status[0]: a bounded wait gave up, every output is undefined
  *          (without a status array bs_prompt_get_device_status tells)

@@ -794,7 +794,7 @@ extern "C" bs_status bs_prompt_attention(const void* q, long long q_stride_t, lo
                                          long long k_stride_h, const void* v, long long v_stride_t, long long v_stride_h,
                                          const int32_t* cu_seqlens, int B, int T, int Hq, int Hkv, int d, float softmax_scale, void* out,
                                          long long out_stride_t, long long out_stride_h, int32_t* status, void* stream) {
-    if (B < 1 || T < 0 || Hq < 1 || Hkv < 1 || d < 1 || !(softmax_scale > 0.f) || !isfinite(softmax_scale) || !cu_seqlens)
+    if (B < 1 || T < 0 || Hq < 1 || Hkv < 1 || d < 1 || !(softmax_scale > 0.f) || !isfinite(softmax_scale * kLog2e) || !cu_seqlens)
         return BS_ERR_INVALID_ARG;
     if (Hq % Hkv || (T > 0 && (!q || !k || !v || !out))) return BS_ERR_INVALID_ARG;
     if (B > BS_MAX_BATCH || Hq / Hkv > 64 || (d != 64 && d != 128)) return BS_ERR_UNSUPPORTED;

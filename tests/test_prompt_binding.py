@@ -247,3 +247,9 @@ def test_oracle_of_the_logits():
     assert x.tolist() == [2.5, 0.5, -2.75, -0.75, -0.5, -np.inf]
     assert ol.path(None, 3) == [3, 2, 1] and ol.path([0, 0, 1, 2], 4) == [4, 2] and ol.path([7], 1) == [1]
     assert ol.enter([[2 * ol.MOST + 1]], emitted=[[0]]).tolist() == [[2 * ol.MOST + 1]]
+
+
+@pytest.mark.parametrize("scale,code", [(3.4e38, 1), (2.4e38, 1), (2.3e38, 0), (1e-45, 0)])
+def test_attention_refuses_a_scale_that_is_infinite_in_base_two(lib, scale, code):
+    """The kernel works with softmax_scale x log2(e), 1.4427 of it; the largest float is 3.4028e38."""
+    assert _attention(lib, scale=scale) == code

@@ -613,6 +613,8 @@ extern "C" bs_status bs_logits_adjust(const void* logits, void* out, bs_dtype dt
     if (bias_begin && n_bias > 0 && (!bias_tokens || !bias_values)) return BS_ERR_INVALID_ARG;
     if (mask_row && n_masks > 0 && !masks) return BS_ERR_INVALID_ARG;
     const long long es = dtype == BS_F32 ? 4 : 2;
+    if ((reinterpret_cast<uintptr_t>(logits) | reinterpret_cast<uintptr_t>(out)) % es || (reinterpret_cast<uintptr_t>(history) & 1))
+        return BS_ERR_INVALID_ARG;
     if (logits != out && rows_overlap(rows_of(logits, 0, V, 1, (long long)B * R, V, es), rows_of(out, 0, V, 1, (long long)B * R, V, es)))
         return BS_ERR_INVALID_ARG;
     AdjustParams p = {logits, out, gamma, draft_tokens, node_parent, history, repetition, presence, frequency, bias_begin,

@@ -249,8 +249,11 @@ extern "C" bs_status bs_rotary(const void* q, long long q_stride_t, long long q_
     if (rot < 2 || rot > d || (rot & 1) || (d & 1) || rot > kRoMaxRot || Hq > 4096 || Hkv > 4096 || d > 4096) return BS_ERR_UNSUPPORTED;
     if (!isfinite(amplitude)) return BS_ERR_INVALID_ARG;
     if (T == 0) return BS_OK;
-    // in place, or apart
     const int es = dtype == BS_F32 ? 4 : 2;
+    if (((Hq ? reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(q_out) : 0) |
+         (Hkv ? reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(k_out) : 0)) % es)
+        return BS_ERR_INVALID_ARG;
+    // in place, or apart
     const Rows from[2] = {rows_of(q, q_stride_t, q_stride_h, T, Hq, d, es), rows_of(k, k_stride_t, k_stride_h, T, Hkv, d, es)};
     const Rows to[2] = {rows_of(q_out, qo_stride_t, qo_stride_h, T, Hq, d, es), rows_of(k_out, ko_stride_t, ko_stride_h, T, Hkv, d, es)};
     for (int i = 0; i < 2; ++i)

@@ -253,3 +253,15 @@ def test_oracle_of_the_logits():
 def test_attention_refuses_a_scale_that_is_infinite_in_base_two(lib, scale, code):
     """The kernel works with softmax_scale x log2(e), 1.4427 of it; the largest float is 3.4028e38."""
     assert _attention(lib, scale=scale) == code
+
+
+@pytest.mark.parametrize("kw", [{"x": AT + 2, "y": AT + (1 << 24)}, {"y": AT + (1 << 24) + 1}, {"dtype": 1, "x": AT + 1, "y": AT + 1}, {"tok": AT, "N": 4, "hist": AT + 1, "rep": AT}])
+def test_adjust_refuses_pointers_between_elements(lib, kw):
+    assert _adjust(lib, **kw) == lib.BS_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("dtype,off", [(1, 1), (0, 1), (0, 2)])
+@pytest.mark.parametrize("which", ["q", "qo", "k", "ko"])
+def test_rotary_refuses_pointers_between_elements(lib, which, dtype, off):
+    at = {"q": AT, "qo": 2 * AT, "k": 3 * AT, "ko": 4 * AT}
+    assert _rotary(lib, dtype=dtype, T=5, **dict(at, **{which: at[which] + off})) == lib.BS_ERR_INVALID_ARG

@@ -72,7 +72,8 @@ typedef enum { BS_UCB = 0, BS_EXP3 = 1, BS_UCB_REWARD = 2 } bs_alg;
                                       hanging under the prompt and never passes.  bs_cache_attention: the same reading;
                                       bs_cache_keep_path: a path whose nodes do not ascend, nothing was moved */
 #define BS_DEV_BAD_LENGTH    64    /* bs_cache_*: a length that is negative, longer than the sequence's blocks or than its
-                                      row of the block table; the sequence got no new tokens / was left out */
+                                      row of the block table; the sequence got no new tokens / was left out.
+                                      bs_prompt_attention, bs_history_update, bs_logits_adjust: see there */
 #define BS_DEV_NO_BLOCKS     128   /* bs_cache_plan: not enough free blocks; the sequence got no new tokens */
 #define BS_DEV_NO_ROOM       256   /* bs_cache_plan: its tokens do not fit slot_map; the sequence got no new tokens */
 #define BS_DEV_BAD_BLOCK     512   /* bs_cache_attention / bs_cache_keep_path: a block id outside [0, n_blocks) */

@@ -17,12 +17,13 @@
 // has not begun (cluster launch control), so that copies and products of the next item begin under the end of the one before.
 //
 // Heads of 128 fill tensor memory with S and O of two tiles, and P takes the place of S; the chain of a tile is then S, softmax, P V, S of
-// the next keys.  Heads of 64 leave room for P beside S, which takes the products out of that chain (160 -> 122 us for 4 prompts
-// of 1000 to 4095, 16 heads).
+// the next keys.  Heads of 64 leave room for P beside S, which takes the products out of that chain (4 prompts of 1000 to
+// 4095, 16 heads: 160 -> 122 us at that step; 129 now).
 //
 // Measured, 32 query and 8 key heads of 128: one prompt of 16384, 2.0 ms, 1.1 PFLOP/s at the 1.45 to 1.5 GHz that the power limit leaves;
-// 16 prompts of 1 to 4096, 0.50 ms, 0.91 PFLOP/s.  Bound by the products: without any softmax the same copies and products take
-// 1.63 (1.35 PFLOP/s; the library's sustained rate is 1.42) and 0.41 ms.  What made no difference, or a loss: two threads a row (+8 %),
+// 16 prompts of 1 to 4096, 0.50 ms, 0.91 PFLOP/s.  No unit is full: tensor pipe 54 %, special-function unit 55 %, issue slots 30 % (one prompt of
+// 4096).  The products alone set four fifths of the time: without any softmax they and the copies take 1.63 (1.35 PFLOP/s; the library's
+// sustained rate is 1.42) and 0.41 ms; the rest is softmax that they do not cover, and ends of items.  What made no difference, or a loss: two threads a row (+8 %),
 // a part of the exponentials as polynomials on the FMA units (+-1 %; heads of 64, where the softmax is the longer part, +2 to
 // 8 %: it is the warps' instructions one after the other that take the time, not the special-function units, busy for half of it), no look
 // at the maxima but at the sums (+8 %), a warpgroup of its own for the results (+-1 %), four streams of 64 keys (+8 to 11 %), an

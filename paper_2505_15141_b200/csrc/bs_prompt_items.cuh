@@ -14,8 +14,8 @@ struct PaItem {
 };
 
 // Items in the order of their numbers: 32 sequences at a time, and of these the items with the most keys first, whichever sequence
-// they are of, so that none of the long ones begins last (sequence after sequence: 4 prompts of 1000 to 4095, 157 us instead of 122); the key
-// heads of the same rows together.
+// they are of, so that none of the long ones begins last (sequence after sequence: 4 prompts of 1000 to 4095, 157 us
+// against 122 when both were measured); the key heads of the same rows together.
 struct PaWalk {
     int b0;                                    // 32 sequences, one a lane
     long long before, items;                   // items of the sequences before them; their own

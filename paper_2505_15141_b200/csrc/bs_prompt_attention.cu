@@ -47,6 +47,7 @@ struct PromptAttnParams {
     const int32_t* cu;
     int32_t* status;
     float c;                                   // softmax_scale * log2(e)
+    long long limit;                           // cycles of a wait
     int B, T, Hkv, G, TQ;                      // TQ: tokens of a row tile, 128 / G
 };
 
@@ -143,41 +144,26 @@ __device__ __forceinline__ uint32_t pa_bf16x2(float lo, float hi) {
 
 __device__ __forceinline__ void pa_few_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 80;"); }
 
-struct PaState { volatile int gave_up, steps; };   // of a CTA: a wait gave up; tiles of keys copied so far
-
-__device__ __forceinline__ bool pa_try(uint32_t bar, uint32_t parity) {   // may suspend the warp: polling would take issue slots
-    uint32_t ok;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(ok) : "r"(bar), "r"(parity), "r"(1000000u) : "memory");
-    return ok != 0;
-}
 // Bounded wait of a converged warp; false if it gave up or another role has.  In line: with a call anywhere in the kernel its
 // registers cannot be split unevenly.  What has arrived already, the usual case, costs one try and one vote; looking at the other
-// roles' word there as well made it 150 cycles, on the path from product to product.  ALONE: when everything ends, whoever gave up.
+// roles' word there as well made it 150 cycles, on the path from product to product.  Some waits last as long as an item (for an
+// item's place, for the first tile of V that is seen in part, of the warps whose row tile an item lacks), so the limit is the longest
+// item's.  Time counted from the last tile copied took 0.5 to 3 % longer in all calls, and 15 % with the steps told by the issuer.
+// ALONE: when everything ends, whoever gave up.
 template <bool ALONE = false>
-__device__ __forceinline__ bool pa_wait(const void* barrier, uint32_t parity, const PaState& state) {
+__device__ __forceinline__ bool pa_wait(const void* barrier, uint32_t parity, long long limit, const volatile int* gave_up) {
     const uint32_t bar = smem_u32(barrier);
     if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
     const long long t0 = clock64();
-    bool ok;
-    do ok = pa_try(bar, parity);
-    while (!ok && (ALONE || !state.gave_up) && clock64() - t0 <= kWaitCycles);
-    return __all_sync(0xffffffffu, ok);
-}
-// The same where it lasts as long as an item: for an item's place, for the first tile of V that is seen in part, of the warps whose
-// row tile an item lacks.  Time counts from the last tile copied.  Other waits are a few tiles' long; with this loop in all of
-// them one prompt of 16384 took 2 % longer, with the steps told by the issuer of the products 15 %.
-__device__ __forceinline__ bool pa_wait_item(const void* barrier, uint32_t parity, const PaState& state) {
-    const uint32_t bar = smem_u32(barrier);
-    if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
-    PaPatience patience = {clock64(), state.steps};
-    bool ok;
-    do ok = pa_try(bar, parity);
-    while (!ok && !state.gave_up && !patience.over(clock64(), kWaitCycles, state.steps));
-    return __all_sync(0xffffffffu, ok);
+    uint32_t ok;
+    do {                                                      // a try may suspend the warp: polling would take issue slots
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+            "selp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(ok) : "r"(bar), "r"(parity), "r"(1000000u) : "memory");
+    } while (!ok && (ALONE || !*gave_up) && clock64() - t0 <= limit);
+    return __all_sync(0xffffffffu, ok != 0);
 }
 
 // A tile of V that some rows see only in part: 0 * NaN is NaN, so what a row must not see may not be there.  Tokens behind the
@@ -249,7 +235,7 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
     __shared__ volatile int s_marked[kPaItems];               // some element of it is
     __shared__ __align__(16) uint4 s_next;                    // answer of the launch control
     __shared__ uint32_t s_tmem;
-    __shared__ PaState s_state;
+    __shared__ volatile int s_abort;
     __shared__ uint32_t s_copies, s_parts, s_last, s_qcopies[2];   // copies issued; of the last 32, those by way of warp 11
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -274,7 +260,7 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
         }
         mbar_init(smem_u32(&b_next), 1);
         mbar_init(smem_u32(&b_drain), 1);
-        s_state.gave_up = s_state.steps = 0;
+        s_abort = 0;
         s_copies = s_parts = s_last = s_qcopies[0] = s_qcopies[1] = 0u;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -291,8 +277,7 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
 
     // Registers: 208 for the softmax warps, 80 for the others; 256 * 208 + 128 * 80 of the 384 * 168 that the launch gives.
     bool ok = true;
-    auto wait = [&](const unsigned long long* bar, uint32_t parity) { return pa_wait(bar, parity, s_state); };
-    auto wait_item = [&](const unsigned long long* bar, uint32_t parity) { return pa_wait_item(bar, parity, s_state); };
+    auto wait = [&](const unsigned long long* bar, uint32_t parity) { return pa_wait(bar, parity, p.limit, &s_abort); };
 
     if (warp == 10) {
         // ================================= scheduler =================================
@@ -334,7 +319,7 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
             const uint32_t slot = k % kPaItems;
             PaItem it = {0, 0, 0, 0, 0, 0};
             const bool there = pa_take(p, w, item, more, ok, it, next);
-            if (ok && k >= kPaItems) ok = wait_item(&b_done[slot], (k / kPaItems - 1) & 1);
+            if (ok && k >= kPaItems) ok = wait(&b_done[slot], (k / kPaItems - 1) & 1);
             if (!ok) break;
             for (int i = lane; i < D; i += 32) s_first[slot][i] = 0x7fffffff;
             if (lane == 0) {
@@ -346,8 +331,8 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
             if (!there) break;
             next();
         }
-        if (!ok && lane == 0) s_state.gave_up = 1;
-        if (asked != answered) pa_wait<true>(&b_next, answered & 1, s_state);   // whoever gave up: an answer on its way is waited for
+        if (!ok && lane == 0) s_abort = 1;
+        if (asked != answered) pa_wait<true>(&b_next, answered & 1, p.limit, &s_abort);   // whoever gave up: an answer on its way is waited for
         __syncwarp();
     } else if (warp == 9) {
         // ================================== copies ==================================
@@ -396,7 +381,6 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
                         ++uses[i];
                     }
                 if (ok) tile(&tm_v, it, j, pa_masked(it.i0, j));
-                if (lane == 0) s_state.steps = (int)count;
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&b_done[slot]));
@@ -407,7 +391,7 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
             s_last = last;
             s_qcopies[0] = uses[0];
             s_qcopies[1] = uses[1];
-            if (!ok) s_state.gave_up = 1;
+            if (!ok) s_abort = 1;
         }
     } else if (warp == 8) {
         // ================================= MMA issuer =================================
@@ -510,8 +494,8 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
         }
         // every product is through before this CTA's memory goes
         ca_commit(smem_u32(&b_drain), elected);
-        if (!pa_wait<true>(&b_drain, 0, s_state)) ok = false;   // whoever gave up: this one is waited for
-        if (!ok && lane == 0) s_state.gave_up = 1;
+        if (!pa_wait<true>(&b_drain, 0, p.limit, &s_abort)) ok = false;   // whoever gave up: this one is waited for
+        if (!ok && lane == 0) s_abort = 1;
         __syncwarp();
     } else if (warp < 8) {
         // ================================== softmax ==================================
@@ -685,9 +669,8 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
             ring += 2 * max(it.nt0, it.nt1);
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&b_done[slot]));
-            if (nt == 0) ok = wait_item(&b_done[slot], (k / kPaItems) & 1);   // the other row tile's work, all of the item's
         }
-        if (!ok && lane == 0) s_state.gave_up = 1;
+        if (!ok && lane == 0) s_abort = 1;
     } else {
         // ============================ V, seen in part =============================
         pa_few_registers();
@@ -703,7 +686,7 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
 #pragma unroll 1
             for (int j = pa_first_masked(it.i0); j < nt; ++j, ++parts) {
                 const uint32_t at = (ring + 2 * j + 1) % RING;
-                ok = wait_item(&b_part[parts % (RING / 2)], (parts / (RING / 2)) & 1);
+                ok = wait(&b_part[parts % (RING / 2)], (parts / (RING / 2)) & 1);
                 if (!ok) break;
                 pa_clean_v<D>(s_kv + at * L::kTileBytes, j * kPaKeys, it.n, s_first[slot], &s_marked[slot]);
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -714,23 +697,23 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
             __syncwarp();
             if (ok && lane == 0) mbar_arrive(smem_u32(&b_done[slot]));
         }
-        if (!ok && lane == 0) s_state.gave_up = 1;
+        if (!ok && lane == 0) s_abort = 1;
     }
 
     // ---- all roles meet; tensor memory goes back ----
     __syncwarp();
     tc_fence_before();
     __syncthreads();
-    if (s_state.gave_up) {
+    if (s_abort) {
         // a wait gave up: nothing is issued any more, and no copy may be in flight when the memory goes (the products have been
         // waited for)
         if (warp == 9) {
             const uint32_t n = s_copies, m = s_parts;
             for (uint32_t f = n > RING ? n - RING : 0u; f < n; ++f)
-                if (!((s_last >> (n - 1 - f)) & 1u)) pa_wait<true>(&b_full[f % RING], (f / RING) & 1, s_state);
-            for (uint32_t f = m > RING / 2 ? m - RING / 2 : 0u; f < m; ++f) pa_wait<true>(&b_part[f % (RING / 2)], (f / (RING / 2)) & 1, s_state);
+                if (!((s_last >> (n - 1 - f)) & 1u)) pa_wait<true>(&b_full[f % RING], (f / RING) & 1, p.limit, &s_abort);
+            for (uint32_t f = m > RING / 2 ? m - RING / 2 : 0u; f < m; ++f) pa_wait<true>(&b_part[f % (RING / 2)], (f / (RING / 2)) & 1, p.limit, &s_abort);
             for (int i = 0; i < 2; ++i)
-                if (s_qcopies[i]) pa_wait<true>(&b_qfull[i], (s_qcopies[i] - 1) & 1, s_state);
+                if (s_qcopies[i]) pa_wait<true>(&b_qfull[i], (s_qcopies[i] - 1) & 1, p.limit, &s_abort);
         }
         if (tid == 0) {
             g_pa_gave_up = 1u;
@@ -810,6 +793,7 @@ extern "C" bs_status bs_prompt_attention(const void* q, long long q_stride_t, lo
     p.o_st = out_stride_t; p.o_sh = out_stride_h;
     p.cu = cu_seqlens; p.status = status;
     p.c = softmax_scale * kLog2e;
+    p.limit = pa_wait_limit(T);
     p.B = B; p.T = T; p.Hkv = Hkv; p.G = Hq / Hkv; p.TQ = 128 / p.G;
     // pairs of row tiles: each sequence rounds up once
     const long long grid = ((long long)T / (2 * p.TQ) + B) * Hkv;

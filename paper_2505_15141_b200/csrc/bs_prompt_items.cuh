@@ -74,19 +74,9 @@ __device__ __forceinline__ bool pa_walk_to(const P& p, PaWalk& w, long long item
     return true;
 }
 
-// Limit of a wait that may last as long as an item, which has no bound: over when `limit` cycles have passed without a step of the CTA.
-struct PaPatience {
-    long long since;
-    int seen;                                  // steps at that time
-    __device__ __forceinline__ bool over(long long now, long long limit, const volatile int& steps) {
-        if (now - since <= limit) return false;
-        const int at = steps;
-        if (at == seen) return true;
-        seen = at;
-        since = now;
-        return false;
-    }
-};
+// Cycles after which a wait gives up, in a call of T tokens: about a second, and 20000 for every tile of keys of the longest item there can
+// be, six times what a tile takes (3150 for a pair of row tiles, heads of 128).
+inline long long pa_wait_limit(int T) { return 2000000000LL + 20000LL * ((T + kPaKeys - 1) / kPaKeys); }
 
 // The next item of a CTA.  `item` is the number of a CTA that will not run, or has just begun, `next` asks the launch control for
 // another and clears `more` if there is none, `ok` if it gave up.  The grid has a few more CTAs than there are items, and nothing

@@ -2,7 +2,7 @@
 // numbers handed out in any order.  A lane is a fiber; all lanes of a warp stop at each operation of the warp.
 //
 // stdin:  T Hkv TQ B cu[0..B] running n number[0..n-1]   -- the first `running` numbers begin as CTAs, the others are asked for
-// With an argument: a wait's limit, see wait_main.
+// With an argument: the limit of a wait in a call of so many tokens.
 // stdout: "item cta row0 n i0 h nt0 nt1" in the order of taking, "status b bits"
 #include <stdint.h>
 #include <stdio.h>
@@ -106,18 +106,11 @@ static void lane_main() {
     swapcontext(&w->lane[l], &w->main);
 }
 
-// "wait": limit, polls a wait every `every` cycles while a step takes `step` of them, until step `last`; prints the cycle at which it is over.
-static int wait_main() {
-    long long limit, every, step, last, now = 0;
-    if (scanf("%lld %lld %lld %lld", &limit, &every, &step, &last) != 4) return 2;
-    bs::PaPatience patience = {0, 0};
-    for (volatile int steps = 0; !patience.over(now, limit, steps); steps = (int)min(now / step, last)) now += every;
-    printf("%lld\n", now);
-    return 0;
-}
-
-int main(int argc, char**) {
-    if (argc > 1) return wait_main();
+int main(int argc, char** argv) {
+    if (argc > 1) {
+        printf("%lld\n", bs::pa_wait_limit(atoi(argv[1])));
+        return 0;
+    }
     int running = 0, n = 0;
     if (scanf("%d %d %d %d", &g_p.T, &g_p.Hkv, &g_p.TQ, &g_p.B) != 4) return 2;
     std::vector<int32_t> cu(g_p.B + 1), status(g_p.B);

@@ -10,22 +10,22 @@ SRC = re.sub(r"//[^\n]*", "", open(os.path.join(ROOT, "paper_2505_15141_b200", "
 
 def _end():
     """From the barrier at which all roles meet."""
-    at = SRC.index("if (s_state.gave_up) {")
+    at = SRC.index("if (s_abort) {")
     return SRC[SRC.rindex("__syncthreads();", 0, at):SRC.index("tc_free(tmem", at)]
 
 
 def test_every_role_tells_that_it_gave_up():
-    body = SRC[SRC.index("if (warp == 10) {"):SRC.index("if (s_state.gave_up) {")]
-    assert body.count("s_state.gave_up = 1;") == 5            # scheduler, copies, products, softmax, V
+    body = SRC[SRC.index("if (warp == 10) {"):SRC.index("if (s_abort) {")]
+    assert body.count("s_abort = 1;") == 5            # scheduler, copies, products, softmax, V
 
 
 def test_nothing_is_in_flight_when_a_cta_that_gave_up_ends():
     """Copies of the ring, those by way of the V warp, queries; products and the launch control's answer before the roles meet."""
     end = _end()
     assert end.index("s_copies") < end.index("pa_wait<true>(&b_full") < end.index("pa_wait<true>(&b_part") < end.index("pa_wait<true>(&b_qfull")
-    before = SRC[:SRC.index("if (s_state.gave_up) {")]
-    assert before.count("pa_wait<true>(&b_drain, 0, s_state)") == 1
-    assert before.count("if (asked != answered) pa_wait<true>(&b_next, answered & 1, s_state);") == 1
+    before = SRC[:SRC.index("if (s_abort) {")]
+    assert before.count("pa_wait<true>(&b_drain, 0, p.limit, &s_abort)") == 1
+    assert before.count("if (asked != answered) pa_wait<true>(&b_next, answered & 1, p.limit, &s_abort);") == 1
 
 
 def test_a_time_out_is_kept_where_the_host_can_read_it():

@@ -286,7 +286,7 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
         PaWalk w = {};
         pa_walk_load(p, w);
         long long item = blockIdx.x;
-        bool more = true;
+        bool more = true, looked = false;
         uint32_t asked = 0, answered = 0;
         auto next = [&]() {                                   // the item of a CTA that has not begun, if there is one
             if (lane == 0) mbar_arrive_expect_tx(smem_u32(&b_next), 16);
@@ -318,7 +318,7 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
         for (uint32_t k = 0; ok; ++k) {                       // the k-th item of this CTA
             const uint32_t slot = k % kPaItems;
             PaItem it = {0, 0, 0, 0, 0, 0};
-            const bool there = pa_take(p, w, item, more, ok, it, next);
+            const bool there = pa_take(p, w, item, more, ok, looked, it, next);
             if (ok && k >= kPaItems) ok = wait(&b_done[slot], (k / kPaItems - 1) & 1);
             if (!ok) break;
             for (int i = lane; i < D; i += 32) s_first[slot][i] = 0x7fffffff;
@@ -329,7 +329,6 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&b_item[slot]));
             if (!there) break;
-            next();
         }
         if (!ok && lane == 0) s_abort = 1;
         if (asked != answered) pa_wait<true>(&b_next, answered & 1, p.limit, &s_abort);   // whoever gave up: an answer on its way is waited for

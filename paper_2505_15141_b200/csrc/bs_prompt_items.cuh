@@ -78,14 +78,18 @@ __device__ __forceinline__ bool pa_walk_to(const P& p, PaWalk& w, long long item
 // be, six times what a tile takes (3150 for a pair of row tiles, heads of 128).
 inline long long pa_wait_limit(int T) { return 2000000000LL + 20000LL * ((T + kPaKeys - 1) / kPaKeys); }
 
-// The next item of a CTA.  `item` is the number of a CTA that will not run, or has just begun, `next` asks the launch control for
-// another and clears `more` if there is none, `ok` if it gave up.  The grid has a few more CTAs than there are items, and nothing
-// promises that their numbers come in order: a number behind the last item says nothing of the others.
+// The next item of a CTA.  `item` is the number of a CTA that has just begun or will not run (`looked`: it was looked at), `next` asks the
+// launch control for another and clears `more` if there is none, `ok` if it gave up.  The grid has a few more CTAs than there are
+// items, and nothing promises that their numbers come in order: a number behind the last item says nothing of the others.
 template <class P, class Next>
-__device__ __forceinline__ bool pa_take(const P& p, PaWalk& w, const long long& item, const bool& more, const bool& ok, PaItem& it, Next&& next) {
+__device__ __forceinline__ bool pa_take(const P& p, PaWalk& w, const long long& item, const bool& more, const bool& ok, bool& looked, PaItem& it, Next&& next) {
     while (ok && more) {
-        if (pa_walk_to(p, w, item, it)) return true;
+        if (!looked) {
+            looked = true;
+            if (pa_walk_to(p, w, item, it)) return true;
+        }
         next();
+        looked = false;
     }
     return false;
 }

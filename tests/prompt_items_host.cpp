@@ -89,7 +89,7 @@ static void lane_main() {
     bs::PaWalk walk = {};
     bs::pa_walk_load(g_p, walk);
     long long item = w->item;
-    bool more = true, ok = true;
+    bool more = true, ok = true, looked = false;
     auto next = [&]() {
         w->asks = true;
         stop();
@@ -98,9 +98,8 @@ static void lane_main() {
     };
     for (;;) {
         bs::PaItem it = {};
-        if (!bs::pa_take(g_p, walk, item, more, ok, it, next)) break;
+        if (!bs::pa_take(g_p, walk, item, more, ok, looked, it, next)) break;
         if (l == 0) printf("item %d %d %d %d %d %d %d\n", w->cta, it.row0, it.n, it.i0, it.h, it.nt0, it.nt1);
-        next();
     }
     w->done[l] = true;
     swapcontext(&w->lane[l], &w->main);

@@ -18,7 +18,7 @@
 //
 // Heads of 128 fill tensor memory with S and O of two tiles, and P takes the place of S; the chain of a tile is then S, softmax, P V, S of
 // the next keys.  Heads of 64 leave room for P beside S, which takes the products out of that chain (4 prompts of 1000 to
-// 4095, 16 heads: 160 -> 122 us at that step; 129 now).
+// 4095, 16 heads: 160 -> 122 us at that step; 126 now).
 //
 // Measured, 32 query and 8 key heads of 128: one prompt of 16384, 2.0 ms, 1.1 PFLOP/s at the 1.45 to 1.5 GHz that the power limit leaves;
 // 16 prompts of 1 to 4096, 0.50 ms, 0.91 PFLOP/s.  No unit is full: tensor pipe 54 %, special-function unit 55 %, issue slots 30 % (one prompt of
